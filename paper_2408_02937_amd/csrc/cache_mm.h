@@ -1,0 +1,178 @@
+// Codes of the cache as operands of the matrix instructions, and what the attention kernels share.
+#pragma once
+#include "cache.h"
+
+namespace rtams {
+
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+union HalfWords {
+  half8 h;
+  half2v p[4];
+  uint32_t w[4];
+};
+
+// The eight codes of a word as halves.  Or'ed into the low bits of 1024 a code c is 1024 + c, four bits further up 1024 + 16 c: exact, and
+// so is what is taken off again.
+__device__ inline HalfWords codes_of(uint32_t w) {
+  HalfWords x;
+  const uint32_t w8 = w >> 8;
+  x.w[0] = (w & 0x000f000fu) | 0x64006400u;
+  x.w[1] = (w & 0x00f000f0u) | 0x64006400u;
+  x.w[2] = (w8 & 0x000f000fu) | 0x64006400u;
+  x.w[3] = (w8 & 0x00f000f0u) | 0x64006400u;
+  const half2v k1024 = {(_Float16)1024.0f, (_Float16)1024.0f}, k16 = {(_Float16)0.0625f, (_Float16)0.0625f}, k64 = {(_Float16)-64.0f, (_Float16)-64.0f};
+  x.p[0] = x.p[0] - k1024;
+  x.p[1] = __builtin_elementwise_fma(x.p[1], k16, k64);
+  x.p[2] = x.p[2] - k1024;
+  x.p[3] = __builtin_elementwise_fma(x.p[3], k16, k64);
+  return x;
+}
+
+__device__ inline _Float16 half_at(uint32_t w, int high) {
+  const uint16_t u = (uint16_t)(high ? w >> 16 : w);
+  _Float16 h;
+  __builtin_memcpy(&h, &u, 2);
+  return h;
+}
+
+// 16 tokens of a block's keys, 16 (i / 8) + i % 8 + 8 tile for i of 0..15, as the left operand: lane i + 16 b holds the b-th quarter of
+// token i's channels.
+template <int D>
+struct KeyTile {
+  static constexpr int NJ = D / 32;
+  uint32_t code[NJ];
+  uint32_t meta[D == 96 ? 3 : (NJ + 3) / 4];
+
+  __device__ void load(const unsigned char *blk, int tile, int lane) {
+    const int i = lane & 15, b = lane >> 4, token = 16 * (i >> 3) + (i & 7) + 8 * tile;
+    const uint32_t *p = reinterpret_cast<const uint32_t *>(blk + token * (D / 2)) + b * NJ;
+    const uint32_t *mp = reinterpret_cast<const uint32_t *>(blk + 16 * D) + token * (D / 32);
+    if constexpr (D == 96) {  // three words, a group each
+#pragma unroll
+      for (int j = 0; j < 3; ++j) {
+        code[j] = p[j];
+        meta[j] = mp[(3 * b + j) >> 2];
+      }
+    } else if constexpr (D == 64) {
+      const uint2 x = *reinterpret_cast<const uint2 *>(p);
+      code[0] = x.x;
+      code[1] = x.y;
+      meta[0] = mp[b >> 1];
+    } else {
+#pragma unroll
+      for (int j = 0; j < NJ; j += 4) {
+        const uint4 x = *reinterpret_cast<const uint4 *>(p + j);
+        code[j] = x.x;
+        code[j + 1] = x.y;
+        code[j + 2] = x.z;
+        code[j + 3] = x.w;
+        meta[j / 4] = mp[b * (NJ / 4) + j / 4];
+      }
+    }
+  }
+  // Eight channels, rounded once to a half.
+  __device__ half8 values(int j) const {
+    HalfWords x = codes_of(code[j]);
+    const uint32_t mt = meta[D == 96 ? j : j / 4];
+    const half2v step = {half_at(mt, 0), half_at(mt, 0)}, zero = {half_at(mt, 1), half_at(mt, 1)};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x.p[i] = __builtin_elementwise_fma(x.p[i], step, zero);
+    return x.h;
+  }
+};
+
+// A block's values as the left operand V^T: lane ch % 16 + 16 b holds 8 tokens of a channel (value_word).
+template <int D>
+struct ValueBlock {
+  static constexpr int NT = D / 16, VC = value_chunk(D);
+  uint32_t code[NT];
+  HalfWords step[D / 32], zero[D / 32];
+
+  __device__ void load(const unsigned char *blk, int lane) {
+    const uint32_t *p = reinterpret_cast<const uint32_t *>(blk + 20 * D);
+#pragma unroll
+    for (int q = 0; q < NT / VC; ++q) {
+      if constexpr (VC == 4) {
+        const uint4 x = reinterpret_cast<const uint4 *>(p)[q * 64 + lane];
+        code[4 * q] = x.x;
+        code[4 * q + 1] = x.y;
+        code[4 * q + 2] = x.z;
+        code[4 * q + 3] = x.w;
+      } else {
+        const uint2 x = reinterpret_cast<const uint2 *>(p)[q * 64 + lane];
+        code[2 * q] = x.x;
+        code[2 * q + 1] = x.y;
+      }
+    }
+    const uint4 *mp = reinterpret_cast<const uint4 *>(blk + 36 * D) + (lane >> 4);
+#pragma unroll
+    for (int g = 0; g < D / 32; ++g) {
+      const uint4 x = mp[g * 8], y = mp[g * 8 + 4];
+      __builtin_memcpy(&step[g], &x, 16);
+      __builtin_memcpy(&zero[g], &y, 16);
+    }
+  }
+  __device__ half8 values(int n) const {
+    HalfWords x = codes_of(code[n]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x.p[i] = __builtin_elementwise_fma(x.p[i], step[n / 2].p[i], zero[n / 2].p[i]);
+    return x.h;
+  }
+};
+
+__device__ inline half8 to_half8(const float p[8]) {
+  half8 h;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) h[e] = (_Float16)p[e];
+  return h;
+}
+
+// Eight channels of a row of q, times the scale of the scores and log2(e) in 32 bits, rounded to halves.
+__device__ inline half8 load_query(const uint16_t *p, bool half_type, bool vec, float scale) {
+  uint16_t raw[8];
+  if (vec) {
+    const uint4 x = *reinterpret_cast<const uint4 *>(p);
+    __builtin_memcpy(raw, &x, 16);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) raw[e] = p[e];
+  }
+  half8 h;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    _Float16 x;
+    __builtin_memcpy(&x, &raw[e], 2);
+    h[e] = (_Float16)((half_type ? (float)x : __uint_as_float((uint32_t)raw[e] << 16)) * scale);
+  }
+  return h;
+}
+
+// Channels c .. c + 3 of an output row: sums over the tokens, relative to the maximum `top` of the scores in powers of two.
+__device__ inline void store_row(const CacheQuery &q, int64_t row, int head, int c, f32x4 v, float top, float sum) {
+  const float by = sum == 0.0f ? 0.0f : 1.0f / sum;  // (a row that sees nothing: zeros)
+  uint16_t h[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float x = v[e] * by;
+    if (q.half_type) {
+      const _Float16 y = (_Float16)x;
+      __builtin_memcpy(&h[e], &y, 2);
+    } else {
+      const __bf16 y = (__bf16)x;
+      __builtin_memcpy(&h[e], &y, 2);
+    }
+  }
+  uint16_t *p = q.out + row * q.out_row + (int64_t)head * q.out_head + c;
+  if (q.vec) {
+    *reinterpret_cast<uint2 *>(p) = make_uint2((uint32_t)h[0] | (uint32_t)h[1] << 16, (uint32_t)h[2] | (uint32_t)h[3] << 16);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) p[e] = h[e];
+  }
+  if (q.lse && c == 0) q.lse[row * q.q_heads + head] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+}
+
+}  // namespace rtams

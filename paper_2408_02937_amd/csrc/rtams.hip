@@ -14,15 +14,16 @@
 #include <new>
 #include <shared_mutex>
 
+#include "host.h"
 #include "search_common.h"
 
 using namespace rtams;
 
 namespace {
-
 thread_local char g_err[512] = "";
+}
 
-int fail(int code, const char *fmt, ...) {
+int rtams::fail(int code, const char *fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
   vsnprintf(g_err, sizeof(g_err), fmt, ap);
@@ -30,14 +31,7 @@ int fail(int code, const char *fmt, ...) {
   return code;
 }
 
-#define HIP_TRY(expr)                                                                  \
-  do {                                                                                 \
-    hipError_t e_ = (expr);                                                            \
-    if (e_ != hipSuccess)                                                              \
-      return fail(RTAMS_EHIP, "%s failed: %s", #expr, hipGetErrorString(e_));          \
-  } while (0)
-
-inline size_t up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+namespace {
 
 // Byte offsets of everything in front of the blocks.
 struct Layout {

@@ -24,7 +24,7 @@ STORAGE = {"f32": 0, "f16": 1, "u8": 2}  # what flat lists keep of a coordinate
 _NAMES = {EINVAL: "EINVAL", ESTATE: "ESTATE", EPOOL: "EPOOL", EBUSY: "EBUSY", EHIP: "EHIP",
           ESCRATCH: "ESCRATCH", ENOSPARE: "ENOSPARE"}
 
-# every symbol include/rtams.h and include/rtams_measure.h declare
+# every symbol the headers in include/ declare
 SYMBOLS = [
     "rtams_pool_bytes_for", "rtams_scratch_bytes_for", "rtams_create", "rtams_destroy",
     "rtams_set_centroids", "rtams_add", "rtams_search", "rtams_rearrange", "rtams_ntotal",
@@ -34,6 +34,9 @@ SYMBOLS = [
     "rtams_copy_plain", "rtams_read_plain", "rtams_set_codebooks", "rtams_list_export_codes",
     "rtams_search_noalloc", "rtams_overflow_bytes_for", "rtams_scan_kernels",
     "rtams_request_trace", "rtams_halves_bytes", "rtams_set_halves", "rtams_scans_of_halves", "rtams_drop_halves",
+    "rtams_cache_pool_bytes_for", "rtams_cache_scratch_bytes_for", "rtams_cache_create", "rtams_cache_destroy", "rtams_cache_layout",
+    "rtams_cache_extend", "rtams_cache_write", "rtams_cache_read", "rtams_cache_attend", "rtams_cache_fork", "rtams_cache_trim",
+    "rtams_cache_compact", "rtams_cache_free_pages", "rtams_cache_poll_error", "rtams_cache_clear_error",
 ]
 
 
@@ -56,6 +59,24 @@ class Stats(C.Structure):
                 ("table_entries_total", C.c_int64), ("overflow_chunks", C.c_int64),
                 ("overflow_chunk_entries", C.c_int64), ("overflow_chunks_leased", C.c_int64),
                 ("rearrangement_state", C.c_int64), ("add_waits", C.c_int64)]
+
+
+class CacheConfig(C.Structure):  # (cache.py)
+    _fields_ = [("layers", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page_tokens", C.c_int32),
+                ("max_seqs", C.c_int32), ("max_pages", C.c_int32), ("d_pool", C.c_void_p), ("pool_bytes", C.c_size_t),
+                ("d_scratch", C.c_void_p), ("scratch_bytes", C.c_size_t)]
+
+
+class CacheView(C.Structure):
+    _fields_ = [("d_table", C.c_void_p), ("d_lengths", C.c_void_p), ("d_refs", C.c_void_p), ("d_pages", C.c_void_p),
+                ("pages", C.c_int64), ("page_bytes", C.c_int64)]
+
+
+class CacheQuery(C.Structure):
+    _fields_ = [("layer", C.c_int32), ("q_heads", C.c_int32), ("type", C.c_int32), ("causal", C.c_int32), ("window", C.c_int32),
+                ("max_new", C.c_int32), ("scale", C.c_float), ("d_q", C.c_void_p), ("q_row_stride", C.c_int64),
+                ("q_head_stride", C.c_int64), ("d_out", C.c_void_p), ("out_row_stride", C.c_int64),
+                ("out_head_stride", C.c_int64), ("d_lse", C.c_void_p)]
 
 
 class RtamsError(RuntimeError):
@@ -113,6 +134,24 @@ def lib():
         L.rtams_scan_kernels.argtypes = [vp, C.POINTER(i64), C.c_int]
         L.rtams_scans_of_halves.argtypes = [vp, C.POINTER(i64), C.c_int]
         L.rtams_request_trace.argtypes = [vp, i32, i64, vp, vp, C.POINTER(i32)]
+        cc = C.POINTER(CacheConfig)
+        L.rtams_cache_pool_bytes_for.restype = C.c_size_t
+        L.rtams_cache_pool_bytes_for.argtypes = [cc, i64]
+        L.rtams_cache_scratch_bytes_for.restype = C.c_size_t
+        L.rtams_cache_scratch_bytes_for.argtypes = [cc]
+        L.rtams_cache_create.argtypes = [cc, C.POINTER(vp)]
+        L.rtams_cache_destroy.argtypes = [vp]
+        L.rtams_cache_layout.argtypes = [vp, C.POINTER(CacheView)]
+        L.rtams_cache_extend.argtypes = [vp, i64, vp, vp, vp]
+        L.rtams_cache_write.argtypes = [vp, i32, i64, vp, vp, i64, i32, vp, vp, i64, i64, i32, vp]
+        L.rtams_cache_read.argtypes = [vp, i32, i64, vp, vp, i64, i32, vp, vp, i32, vp]
+        L.rtams_cache_attend.argtypes = [vp, C.POINTER(CacheQuery), i64, vp, vp, i64, vp]
+        L.rtams_cache_fork.argtypes = [vp, i64, vp, vp, i32, vp]
+        L.rtams_cache_trim.argtypes = [vp, i64, vp, vp, vp]
+        L.rtams_cache_compact.argtypes = [vp, vp]
+        L.rtams_cache_free_pages.argtypes = [vp, C.POINTER(i64)]
+        L.rtams_cache_poll_error.argtypes = [vp]
+        L.rtams_cache_clear_error.argtypes = [vp]
         L.rtams_copy_plain.argtypes = [vp, vp, C.c_size_t, vp]
         L.rtams_read_plain.argtypes = [vp, C.c_size_t, vp, vp]
         _lib = L

@@ -1,0 +1,652 @@
+"""The cache of keys and values in 4 bits against a plain implementation: the format in 32 bits (the definition's own), attention in 64,
+pages in Python integers.
+
+How far attention may be off is derived.  The kernels round to halves (u = 2^-11 of a value): scaled queries, keys, values and probabilities.
+A score is then off by at most s = 2.1 u * sum |q K| * scale, a row's weighted mean by (exp(2 s) - 1 + 3 u) * sum p |V|, and by 2^-24 of the largest |V|
+for each token whose probability is below a half's normal range; sums in 32 bits add 2^-16, the output's own rounding its
+unit.  The bounds are worst cases; nothing is left for luck."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2408_02937_amd import rtams
+from paper_2408_02937_amd.cache import Cache
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+U = 2.0 ** -11
+
+
+def ints(v):
+    return torch.tensor(list(v), dtype=torch.int32, device=DEV)
+
+
+def starts_of(counts):
+    return ints(np.concatenate([[0], np.cumsum(counts)]))
+
+
+def quantised(x):
+    """(codes, step, zero) of float32 rows [...][d], as the header says."""
+    x = np.asarray(x, dtype=np.float32)
+    x = np.clip(np.where(np.isnan(x), np.float32(0), x), np.float32(-60000), np.float32(60000)).reshape(*x.shape[:-1], -1, 32)
+    lo, hi = x.min(-1), x.max(-1)
+    step = ((hi - lo) / np.float32(15)).astype(np.float16)
+    zero = lo.astype(np.float16)
+    s = step.astype(np.float32)
+    inv = np.where(s > 0, np.float32(1) / np.where(s > 0, s, np.float32(1)), np.float32(0)).astype(np.float32)
+    code = np.clip(np.rint((x - zero.astype(np.float32)[..., None]) * inv[..., None]), 0, 15)
+    return code, step, zero
+
+
+def held(x):
+    """What the cache stands for, in 64 bits."""
+    code, step, zero = quantised(x)
+    return (zero.astype(np.float64)[..., None] + step.astype(np.float64)[..., None] * code).reshape(np.asarray(x).shape)
+
+
+def floats(t):
+    return t.detach().float().cpu().numpy()
+
+
+def plain_attention(q, k, v, share, scale, spans):
+    """Row by row in 64 bits: outputs, logarithms, and for each row what the derivation needs."""
+    rows, heads, d = q.shape
+    out, lse = np.zeros((rows, heads, d)), np.full((rows, heads), -np.inf)
+    off, mass = np.zeros((rows, heads)), np.zeros((rows, heads, d))
+    for r, (lo, hi) in enumerate(spans):
+        lo, hi = max(lo, 0), min(hi, k.shape[0])
+        if hi <= lo:
+            continue
+        for h in range(heads):
+            kk, vv = k[lo:hi, h // share], v[lo:hi, h // share]
+            s = scale * (kk @ q[r, h])
+            off[r, h] = 2.1 * U * abs(scale) * (np.abs(kk) @ np.abs(q[r, h])).max()
+            m = s.max()
+            p = np.exp(s - m)
+            out[r, h] = p @ vv / p.sum()
+            mass[r, h] = p @ np.abs(vv) / p.sum() + len(s) * 2.0 ** -24 * np.abs(vv).max(0)
+            lse[r, h] = m + math.log(p.sum())
+    return out, lse, off, mass
+
+
+def check_attention(got, lse, want, unit):
+    out, wl, off, mass = want
+    got = got.double().cpu().numpy()
+    bound = (np.expm1(2 * off)[..., None] + 3.2 * U + 2.0 ** -16) * mass + unit * np.abs(out) * 1.01 + 1e-7
+    worst = np.abs(got - out) / bound
+    assert np.isfinite(got).all() and worst.max() <= 1.0, f"off by {worst.max()} of what the roundings explain"
+    if lse is not None:
+        lse = lse.cpu().numpy()
+        seen = np.isfinite(wl)
+        assert np.array_equal(np.isfinite(lse), seen) and np.all(lse[~seen] == -np.inf)
+        # a sum of probabilities rounded to 32 bits; a probability a score is off by off
+        assert np.all(np.abs(lse - wl)[seen] <= (off + 2.0 ** -16 * (1 + np.abs(np.where(seen, wl, 0))))[seen])
+
+
+def unit_of(dtype):
+    return 2.0 ** -9 if dtype == torch.bfloat16 else 2.0 ** -11
+
+
+class Filled:
+    """A cache with sequences of given lengths, written in one go after extends in two turns (pages interleaved)."""
+
+    def __init__(self, lengths, kv_heads, dim, page=32, layers=1, layer=0, dtype=torch.bfloat16, seed=0, extra_pages=8, max_seqs=None, order=None):
+        g = torch.Generator(device=DEV).manual_seed(seed)
+        n = len(lengths)
+        self.lengths, self.kv_heads, self.dim, self.dtype = lengths, kv_heads, dim, dtype
+        self.cache = Cache(kv_heads, dim, layers=layers, page_tokens=page, pages=sum(-(-x // page) for x in lengths) + extra_pages, max_seqs=max_seqs or n,
+                           max_pages=max(-(-x // page) for x in lengths) + extra_pages, device=DEV)
+        self.seqs = list(range(n)) if order is None else order
+        rows = sum(lengths)
+        mean = torch.randn((kv_heads, dim), device=DEV, generator=g) * 0.5
+        self.k = (torch.randn((rows, kv_heads, dim), device=DEV, generator=g) * 1.2 + mean).to(dtype)
+        self.v = (torch.randn((rows, kv_heads, dim), device=DEV, generator=g) - mean).to(dtype)
+        s = ints(self.seqs)
+        self.cache.extend(s, starts_of([x // 2 for x in lengths]))
+        self.cache.extend(s, starts_of([x - x // 2 for x in lengths]))
+        if rows:
+            self.cache.write(layer, self.k, self.v, s, starts_of(lengths), max_new=max(lengths))
+        at = np.concatenate([[0], np.cumsum(lengths)])
+        k, v = held(floats(self.k)), held(floats(self.v))
+        self.plain = [(k[at[i]:at[i + 1]], v[at[i]:at[i + 1]]) for i in range(n)]
+
+    def query(self, counts, heads, seed=1, dtype=None, width=1.5):
+        g = torch.Generator(device=DEV).manual_seed(seed)
+        return (torch.randn((sum(counts), heads, self.dim), device=DEV, generator=g) * width).to(dtype or self.dtype)
+
+    def want(self, q, counts, scale, causal=True, window=0):
+        q = floats(q).astype(np.float64)
+        share, at, parts = q.shape[1] // self.kv_heads, 0, []
+        for (k, v), c in zip(self.plain, counts):
+            n = len(k)
+            spans = [(max(0, p - window + 1) if window else 0, p + 1) for p in range(n - c, n)] if causal else [(0, n)] * c
+            parts.append(plain_attention(q[at:at + c], k, v, share, scale, spans))
+            at += c
+        return [np.concatenate(x) for x in zip(*parts)]
+
+    def check(self, counts, heads, causal=True, window=0, scale=None, dtype=None, seed=1, width=1.5, tol_lse=True):
+        q = self.query(counts, heads, seed, dtype, width)
+        lse = torch.full(q.shape[:2], 123.0, device=DEV)
+        one = all(c == 1 for c in counts)
+        out = self.cache.attend(0, q, ints(self.seqs), None if one else starts_of(counts), None if one else max(counts), scale=scale, causal=causal,
+                                window=window, lse=lse)
+        torch.cuda.synchronize()
+        assert out.dtype == q.dtype
+        check_attention(out, lse, self.want(q, counts, self.dim ** -0.5 if scale is None else scale, causal, window), unit_of(q.dtype))
+        return q, out
+
+
+# ------------------------------------------------------------------ the format
+@pytest.mark.parametrize("dim", [64, 96, 128, 256])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_what_is_written_is_what_the_definition_says(dim, dtype):
+    lengths = [1, 31, 32, 33, 70, 5]
+    f = Filled(lengths, 3, dim, page=64, dtype=dtype, seed=dim)
+    # groups that are constant, tiny, huge, not finite
+    x = f.k.clone()
+    x[0, 0, :32] = 2.5
+    x[0, 1, :32] = 0.0
+    x[1, 0, 32:64] *= 1e-6
+    x[2, 2, :] = float("nan")
+    x[3, 1, 5] = float("inf")
+    x[4, 1, 9] = -float("inf")
+    x[5, 0, 3] = float("nan")
+    x[6, 0, :] = 65000.0
+    f.cache.write(0, x, f.v, starts=starts_of(lengths), max_new=70)
+    k, v = f.cache.read(0, sum(lengths), starts=starts_of(lengths), max_new=70)
+    assert f.cache.poll_error() == 0
+    for got, src in ((k, x), (v, f.v)):
+        want = held(floats(src))
+        got = got.cpu().numpy()
+        assert np.isfinite(got).all()
+        assert np.all(np.abs(got - want) <= np.spacing(np.abs(want).astype(np.float32)))  # one rounding to 32 bits
+
+
+@pytest.mark.parametrize("dim", [64, 96])
+def test_rows_written_one_at_a_time_are_those_written_at_once(dim):
+    g = torch.Generator(device=DEV).manual_seed(3)
+    k, v = (torch.randn((75, 2, dim), device=DEV, generator=g).bfloat16() for _ in range(2))
+    a, b = (Cache(2, dim, page_tokens=32, pages=8, max_seqs=2, device=DEV) for _ in range(2))
+    one = ints([1])
+    for t in range(75):
+        a.extend(one)
+        a.write(0, k[t:t + 1], v[t:t + 1], one)
+    for lo, hi in ((0, 3), (3, 40), (40, 75)):
+        b.extend(one, ints([0, hi - lo]))
+        b.write(0, k[lo:hi], v[lo:hi], one, ints([0, hi - lo]), max_new=hi - lo)
+    ra, rb = (c.read(0, 75, one, ints([0, 75]), max_new=75) for c in (a, b))
+    for x, y, src in zip(ra, rb, (k, v)):
+        assert torch.equal(x, y)
+        assert np.allclose(x.cpu().numpy(), held(floats(src)), rtol=1e-6, atol=1e-7)
+
+
+def test_strides_and_alignment_of_the_rows():
+    """Rows of a fused projection, heads transposed, and an odd address: the same values."""
+    g = torch.Generator(device=DEV).manual_seed(4)
+    rows, h, d = 41, 4, 64
+    fused = torch.randn((rows, 3 * h * d), device=DEV, generator=g).half()
+    views = [fused[:, i * h * d:(i + 1) * h * d].view(rows, h, d) for i in range(3)]
+    odd = torch.empty(rows * h * d + 1, dtype=torch.float16, device=DEV)
+    heads_first = torch.empty((h, rows, d), dtype=torch.float16, device=DEV)
+    st = ints([0, rows])
+    got = []
+    for how in range(3):
+        q, k, v = views
+        if how == 1:
+            q, k, v = (odd.clone()[1:].view(rows, h, d).copy_(t) for t in views)
+            assert k.data_ptr() % 16
+        if how == 2:
+            q, k, v = (heads_first.clone().permute(1, 0, 2).copy_(t) for t in views)
+        c = Cache(h, d, page_tokens=32, pages=3, max_seqs=1, device=DEV)
+        c.extend(starts=st)
+        c.write(0, k, v, starts=st, max_new=rows)
+        out = torch.empty((h, rows, d), dtype=torch.float16, device=DEV).permute(1, 0, 2) if how == 2 else odd.clone()[1:].view(rows, h, d) if how == 1 else None
+        got.append((*c.read(0, rows, starts=st, max_new=rows), c.attend(0, q, starts=st, max_new=rows, out=out).clone()))
+    for a in got[1:]:
+        assert all(torch.equal(x, y) for x, y in zip(a, got[0]))
+
+
+# ------------------------------------------------------------------ attention
+SHAPES = [  # query heads, kv heads, head_dim
+    (8, 8, 64), (8, 2, 64), (12, 12, 96), (6, 2, 96), (32, 8, 128), (16, 1, 128), (17, 1, 128), (28, 4, 128), (8, 2, 256), (10, 5, 256), (64, 2, 64),
+]
+
+
+@pytest.mark.parametrize("heads,kv,dim", SHAPES)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_single_tokens(heads, kv, dim, dtype):
+    f = Filled([1, 2, 31, 32, 33, 127, 128, 129, 300], kv, dim, page=64, dtype=dtype, seed=heads)
+    f.check([1] * 9, heads)
+    f.check([1] * 9, heads, causal=False)
+    f.check([1] * 9, heads, window=1)
+    f.check([1] * 9, heads, window=40)
+
+
+@pytest.mark.parametrize("heads,kv,dim", [(8, 2, 64), (12, 12, 96), (32, 8, 128), (8, 2, 256), (16, 1, 128)])
+@pytest.mark.parametrize("counts", [[2, 1, 3, 2], [5, 5, 0, 5], [9, 17, 4, 8], [40, 0, 64, 65], [130, 200, 1, 70]])
+def test_several_rows_of_each_sequence(heads, kv, dim, counts):
+    f = Filled([130, 200, 64, 333], kv, dim, page=32, seed=dim)
+    f.check(counts, heads)
+    f.check(counts, heads, causal=False)
+    f.check(counts, heads, window=50)
+
+
+@pytest.mark.parametrize("page", [32, 64, 96, 160, 1024])
+def test_page_sizes_and_orders_of_sequences(page):
+    f = Filled([257, 95, 1, 640], 2, 64, page=page, seed=page, max_seqs=9, order=[7, 0, 8, 3])
+    f.check([1, 1, 1, 1], 8)
+    f.check([33, 40, 1, 129], 8)
+
+
+@pytest.mark.parametrize("lengths,heads,kv,dim", [([20_011], 8, 2, 64), ([9_000, 17, 30_001], 4, 1, 128), ([4_097] * 3, 3, 3, 96), ([12_345], 16, 2, 256)])
+def test_long_sequences_are_split_and_joined(lengths, heads, kv, dim):
+    f = Filled(lengths, kv, dim, page=128, seed=5)
+    q, out = f.check([1] * len(lengths), heads)
+    for _ in range(3):  # in the same order every time
+        assert torch.equal(out, f.cache.attend(0, q))
+    f.check([1] * len(lengths), heads, window=5000)
+    f.check([7] * len(lengths), heads)
+
+
+def test_many_sequences():
+    """More of them than are numbered at a time, most of them short, some empty."""
+    lengths = [(i * 53) % 97 for i in range(700)]
+    f = Filled(lengths, 1, 64, page=32, seed=6)
+    f.check([1] * 700, 2, causal=False)
+    f.check([min(x, 2) for x in lengths], 2)
+
+
+def test_rows_that_see_nothing():
+    """Sequences without tokens: zeros and -inf, whatever the output held."""
+    f = Filled([0, 40, 0], 2, 64, seed=7)
+    q = f.query([1, 1, 1], 4)
+    lse = torch.zeros((3, 4), device=DEV)
+    out = f.cache.attend(0, q, causal=False, out=torch.full_like(q, 7.0), lse=lse)
+    check_attention(out, lse, f.want(q, [1] * 3, 0.125, causal=False), unit_of(q.dtype))
+    assert not out[0].any() and not out[2].any() and torch.isinf(lse[0]).all()
+    counts = [50, 3, 0]  # (many rows)
+    q = f.query(counts, 4)
+    lse = torch.zeros((53, 4), device=DEV)
+    out = f.cache.attend(0, q, starts=starts_of(counts), max_new=50, causal=False, out=torch.full_like(q, 7.0), lse=lse)
+    check_attention(out, lse, f.want(q, counts, 0.125, causal=False), unit_of(q.dtype))
+
+
+@pytest.mark.parametrize("count", [1, 3, 60])
+def test_scores_far_apart_and_far_from_zero(count):
+    """Peaked rows, and scores whose maximum keeps growing: the running maximum follows."""
+    f = Filled([500, 77], 2, 128, page=64, seed=8, dtype=torch.float16)
+    f.check([count, min(count, 77)], 4, scale=1.0, width=0.5)
+    f.check([count, min(count, 77)], 4, scale=2.0, width=0.3)
+    f.check([count, min(count, 77)], 4, scale=0.0)
+
+
+def test_a_row_that_is_not_finite_spoils_itself_only():
+    f = Filled([200, 90], 2, 64, seed=9)
+    for counts in ([1, 1], [3, 2], [40, 33]):
+        q = f.query(counts, 8)
+        clean = f.cache.attend(0, q, starts=starts_of(counts), max_new=max(counts))
+        q2 = q.clone()
+        q2[0, 3, 5] = float("nan")
+        q2[sum(counts) - 1, 0, 1] = float("inf")
+        out = f.cache.attend(0, q2, starts=starts_of(counts), max_new=max(counts))
+        assert not torch.isfinite(out[0, 3]).any() and not torch.isfinite(out[sum(counts) - 1, 0]).any()
+        same = torch.ones(q.shape[:2], dtype=torch.bool, device=DEV)
+        same[0, 3] = same[sum(counts) - 1, 0] = False
+        assert torch.equal(out[same], clean[same])
+
+
+def test_what_later_rows_hold_does_not_reach_earlier_ones():
+    """Positions a mask hides hold the largest values there are, NaN written among them."""
+    f = Filled([100], 1, 64, seed=10)
+    for counts in ([4], [60]):
+        c = counts[0]
+        q = f.query(counts, 2)
+        before = f.cache.attend(0, q, starts=starts_of(counts), max_new=c)
+        k, v = f.k.clone(), f.v.clone()
+        k[-1], v[-1] = float("nan"), float("inf")
+        f.cache.write(0, k[-1:], v[-1:])
+        after = f.cache.attend(0, q, starts=starts_of(counts), max_new=c)
+        assert torch.equal(before[:-1], after[:-1])
+        f.cache.write(0, f.k[-1:], f.v[-1:])
+    # ... nor does what a page held before it was freed
+    f.cache.write(0, torch.full_like(f.k, 6e4), torch.full_like(f.v, 6e4), starts=ints([0, 100]), max_new=100)
+    f.cache.trim(n=1)
+    f.cache.extend(starts=ints([0, 37]))
+    f.cache.write(0, f.k[:37], f.v[:37], starts=ints([0, 37]), max_new=37)
+    f.plain = [(f.plain[0][0][:37], f.plain[0][1][:37])]
+    f.check([1], 2)
+    f.check([35], 2)
+
+
+def test_layers_are_apart():
+    f = Filled([70, 20], 2, 64, layers=3, layer=1, seed=11)
+    q = f.query([1, 1], 4)
+    got = f.cache.attend(1, q)
+    check_attention(got, None, f.want(q, [1, 1], 0.125), unit_of(q.dtype))
+    assert not f.cache.attend(0, q).any() and not f.cache.attend(2, q).any()  # (cleared: every value is 0)
+
+
+# ------------------------------------------------------------------ pages
+class Book:
+    """The page table in Python integers: what the header says calls do."""
+
+    def __init__(self, seqs, pages, page):
+        self.rows, self.length, self.refs, self.page = [[] for _ in range(seqs)], [0] * seqs, [0] * pages, page
+        self.moves = []
+
+    def take(self, n):
+        free = [p for p, r in enumerate(self.refs) if r == 0]
+        return free[:n] if len(free) >= n else None
+
+    def extend(self, seqs, counts):
+        plan = []
+        for s, c in zip(seqs, counts):
+            have, want = -(-self.length[s] // self.page), -(-(self.length[s] + c) // self.page)
+            copy = c > 0 and self.length[s] % self.page != 0 and self.refs[self.rows[s][-1]] > 1
+            plan.append((s, c, copy, want - have))
+        got = self.take(sum(p[2] + p[3] for p in plan))
+        if got is None:
+            return False
+        self.moves = []
+        for s, c, copy, more in plan:
+            if copy:
+                old, new = self.rows[s][-1], got.pop(0)
+                self.refs[old] -= 1
+                self.refs[new] = 1
+                self.rows[s][-1] = new
+                self.moves.append((old, new))
+            for _ in range(more):
+                self.rows[s].append(got.pop(0))
+                self.refs[self.rows[s][-1]] = 1
+            self.length[s] += c
+        return True
+
+    def fork(self, src, dst, copy):
+        if copy:
+            got = self.take(sum(len(self.rows[s]) for s in src))
+            if got is None:
+                return False
+        self.moves = []
+        for s, t in zip(src, dst):
+            row = list(self.rows[s])
+            if copy:
+                row = [got.pop(0) for _ in row]
+                self.moves += list(zip(self.rows[s], row))
+            for p in row:
+                self.refs[p] += 1
+            self.rows[t], self.length[t] = row, self.length[s]
+        return True
+
+    def trim(self, seqs, lengths):
+        for s, n in zip(seqs, lengths):
+            keep = -(-n // self.page)
+            for p in self.rows[s][keep:]:
+                self.refs[p] -= 1
+            self.rows[s], self.length[s] = self.rows[s][:keep], n
+
+    def compact(self):
+        used = sum(r > 0 for r in self.refs)
+        holes = [p for p in range(used) if self.refs[p] == 0]
+        movers = [p for p in range(used, len(self.refs)) if self.refs[p] > 0]
+        to = dict(zip(movers, holes))
+        self.moves = list(to.items())
+        for a, b in to.items():
+            self.refs[b], self.refs[a] = self.refs[a], 0
+        self.rows = [[to.get(p, p) for p in row] for row in self.rows]
+
+    def check(self, c):
+        table = np.full(tuple(c.table.shape), -1)
+        for s, row in enumerate(self.rows):
+            table[s, :len(row)] = row
+        assert np.array_equal(c.table.cpu().numpy(), table)
+        assert c.lengths.tolist() == self.length and c.refs.tolist() == self.refs
+        assert c.free_pages == sum(r == 0 for r in self.refs)
+
+
+@pytest.mark.parametrize("seed,seqs,pages,page,layers,kv,dim", [(0, 6, 40, 32, 1, 1, 64), (1, 40, 300, 64, 2, 2, 96), (2, 1500, 3000, 32, 1, 1, 64),
+                                                                (3, 12, 33_000, 32, 1, 1, 64), (4, 9, 100, 96, 3, 1, 256)])
+def test_random_calls_leave_what_the_rules_say(seed, seqs, pages, page, layers, kv, dim):
+    """Tables, counts and the pages' bytes after every call."""
+    rng = np.random.default_rng(seed)
+    c = Cache(kv, dim, layers=layers, page_tokens=page, pages=pages, max_seqs=seqs, device=DEV)
+    b = Book(seqs, pages, page)
+    c.pages.copy_(torch.randint(0, 256, tuple(c.pages.shape), dtype=torch.uint8, device=DEV, generator=torch.Generator(device=DEV).manual_seed(seed)))
+    want = c.pages.clone()
+    most = max(1, 3 * pages * page // seqs // 4)
+    refused = 0
+    for step in range(60):
+        print(f"[case] seed {seed} step {step}", flush=True)
+        op = rng.choice(["extend", "extend", "extend", "fork", "copy", "trim", "free", "compact"])
+        pick = rng.permutation(seqs)[:rng.integers(1, seqs + 1)]
+        ok, b.moves = True, []
+        if op == "extend":
+            counts = [min(int(rng.integers(0, rng.choice([2, page + 1, most + 1]))), pages * page - b.length[s]) for s in pick]
+            if rng.random() < 0.3:
+                c.extend(ints(pick))
+                counts = [1] * len(pick)
+                if any(b.length[s] + 1 > pages * page for s in pick):
+                    ok = None
+            else:
+                c.extend(ints(pick), starts_of(counts))
+            ok = b.extend(pick, counts) if ok else ok
+        elif op in ("fork", "copy"):
+            dst = [s for s in pick if b.length[s] == 0]
+            src = [s for s in range(seqs) if b.length[s] > 0 and s not in dst]
+            if not dst or not src:
+                continue
+            src = list(rng.choice(src, len(dst)))
+            c.fork(ints(src), ints(dst), copy=op == "copy")
+            ok = b.fork(src, dst, op == "copy")
+        elif op == "trim":
+            lengths = [int(rng.integers(0, b.length[s] + 1)) for s in pick]
+            c.trim(ints(pick), ints(lengths))
+            b.trim(pick, lengths)
+        elif op == "free":
+            pick = pick[: max(1, len(pick) // 2)]
+            c.trim(ints(pick))
+            b.trim(pick, [0] * len(pick))
+        else:
+            c.compact()
+            b.compact()
+        for old, new in b.moves:
+            want[:, new] = want[:, old]
+        b.check(c)
+        assert torch.equal(c.pages, want)
+        if not ok:
+            assert c.poll_error() == rtams.EPOOL if ok is False else rtams.EINVAL
+            c.clear_error()
+            refused += 1
+        assert c.poll_error() == 0
+
+
+def test_branches_read_what_they_share_and_write_what_is_theirs():
+    f = Filled([45, 70], 2, 64, page=32, layers=2, seed=12, max_seqs=6, extra_pages=20)
+    c = f.cache
+    c.fork(ints([0, 0, 1]), ints([2, 3, 4]))
+    q1 = f.query([1], 4)
+    base = c.attend(0, q1, ints([0]))
+    assert all(torch.equal(base, c.attend(0, q1, ints([s]))) for s in (2, 3))
+    c.extend(ints([2, 3, 4]))
+    k, v = (torch.randn((3, 2, 64), device=DEV).bfloat16() for _ in range(2))
+    c.write(0, k, v, ints([2, 3, 4]))
+    assert torch.equal(base, c.attend(0, q1, ints([0])))
+    q = f.query([1, 1, 1], 4)
+    got = c.attend(0, q, ints([2, 3, 4]))
+    hk, hv = held(floats(k)), held(floats(v))
+    for i, parent in enumerate((0, 0, 1)):
+        kk = np.concatenate([f.plain[parent][0], hk[i:i + 1]])
+        vv = np.concatenate([f.plain[parent][1], hv[i:i + 1]])
+        want = plain_attention(floats(q[i:i + 1]).astype(np.float64), kk, vv, 2, 0.125, [(0, len(kk))])
+        check_attention(got[i:i + 1], None, want, unit_of(q.dtype))
+    assert c.poll_error() == 0
+
+
+def test_rows_of_a_shared_page_are_not_written():
+    f = Filled([40], 1, 64, page=32, max_seqs=2, seed=13)
+    f.cache.fork(ints([0]), ints([1]))
+    before = f.cache.pages.clone()
+    f.cache.write(0, f.k[:1], f.v[:1], ints([0]))
+    assert torch.equal(before, f.cache.pages) and f.cache.poll_error() == rtams.EINVAL
+    f.cache.clear_error()
+    f.cache.trim(ints([1]))
+    f.cache.write(0, f.k[:1], f.v[:1], ints([0]))
+    assert not torch.equal(before, f.cache.pages) and f.cache.poll_error() == 0
+
+
+def test_calls_that_the_device_refuses_change_nothing():
+    f = Filled([40, 33], 1, 64, page=32, max_seqs=4, extra_pages=2, seed=14)
+    c = f.cache
+    state = [x.clone() for x in (c.table, c.lengths, c.refs, c.pages)]
+
+    def refused(code):
+        assert all(torch.equal(x, y) for x, y in zip(state, (c.table, c.lengths, c.refs, c.pages)))
+        assert c.poll_error() == code
+        c.clear_error()
+        assert c.poll_error() == 0
+
+    for bad in ([0, 4], [-1], [1, 1]):  # outside, named twice
+        c.extend(ints(bad))
+        refused(rtams.EINVAL)
+        c.trim(ints(bad))
+        refused(rtams.EINVAL)
+    c.extend(starts=ints([0, -3]))
+    refused(rtams.EINVAL)
+    c.extend(ints([2]), ints([0, 32 * 5]))  # more pages than a sequence may have
+    refused(rtams.EINVAL)
+    c.extend(ints([2]), ints([0, 32 * 3]))  # more than are free
+    refused(rtams.EPOOL)
+    c.trim(ints([0]), ints([41]))
+    refused(rtams.EINVAL)
+    for src, dst in (([0], [1]), ([0], [0]), ([2], [2]), ([0, 0], [2, 2]), ([0, 2], [2, 3]), ([7], [2]), ([0], [-2])):
+        c.fork(ints(src), ints(dst))
+        refused(rtams.EINVAL)
+    c.trim(ints([1]))
+    c.extend(ints([1]), ints([0, 33]))
+    c.write(0, f.k[40:], f.v[40:], ints([1]), ints([0, 33]), max_new=33)
+    state = [x.clone() for x in (c.table, c.lengths, c.refs, c.pages)]
+    c.fork(ints([0, 1]), ints([2, 3]), copy=True)  # four pages, two are free
+    refused(rtams.EPOOL)
+    c.write(0, f.k[:41], f.v[:41], ints([0]), ints([0, 41]), max_new=41)  # more rows than tokens
+    refused(rtams.EINVAL)
+    c.write(0, f.k[:40], f.v[:40], ints([0]), ints([0, 40]), max_new=39)  # more than max_new
+    refused(rtams.EINVAL)
+
+
+def test_writes_are_dropped_after_an_extend_that_was():
+    f = Filled([40], 1, 64, page=32, extra_pages=0, seed=15)
+    before = f.cache.pages.clone()
+    f.cache.extend(starts=ints([0, 30]))
+    f.cache.write(0, f.k[:30] + 1, f.v[:30] + 1, starts=ints([0, 30]), max_new=30)
+    assert torch.equal(before, f.cache.pages) and f.cache.poll_error() == rtams.EINVAL  # (no page beyond max_pages)
+    f.cache.clear_error()
+    f.cache.extend(starts=ints([0, 10]))
+    f.cache.write(0, f.k[:10], f.v[:10], starts=ints([0, 10]), max_new=10)
+    assert not torch.equal(before, f.cache.pages) and f.cache.poll_error() == 0
+
+
+# ------------------------------------------------------------------ streams and graphs
+def test_calls_on_different_streams_follow_one_another():
+    f = Filled([3000, 2500], 2, 128, page=64, seed=16, max_seqs=4, extra_pages=200)
+    q = f.query([1, 1], 8)
+    torch.cuda.synchronize()
+    s, t = torch.cuda.Stream(), torch.cuda.Stream()
+    want = f.cache.attend(0, q)
+    torch.cuda.synchronize()
+    for _ in range(5):
+        f.cache.fork(ints([0, 1]), ints([2, 3]), copy=True, stream=s)
+        with torch.cuda.stream(t):
+            got = f.cache.attend(0, q, ints([2, 3]))
+        f.cache.trim(ints([2, 3]), stream=s)
+        f.cache.compact()
+        t.synchronize()
+        assert torch.equal(got, want)
+    torch.cuda.synchronize()
+    assert f.cache.poll_error() == 0
+
+
+def test_a_recorded_step_is_launched_again_and_again():
+    """extend, write, attend and trim in a graph; every launch against the same calls one by one, with other work between."""
+    lengths = [200, 31, 64]
+    a, b = (Filled(lengths, 2, 64, page=32, seed=17, max_seqs=6, extra_pages=40) for _ in range(2))
+    q, k, v = (torch.empty((3, h, 64), dtype=torch.bfloat16, device=DEV) for h in (8, 2, 2))
+    out = torch.empty_like(q)
+    branch, parent, seqs = ints([3, 4, 5]), ints([0, 1, 2]), ints([0, 1, 2])
+
+    def step(c):
+        c.trim(branch)
+        c.extend(seqs)
+        c.write(0, k, v, seqs)
+        c.fork(parent, branch)
+        c.extend(branch)
+        c.write(0, v, k, branch)
+        c.attend(0, q, branch, out=out)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g, stream=side):
+        step(a.cache)
+    for i in range(40):
+        gen = torch.Generator(device=DEV).manual_seed(i)
+        for x in (q, k, v):
+            x.copy_(torch.randn(x.shape, device=DEV, generator=gen))
+        step(b.cache)
+        want = out.clone()
+        out.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), i
+        assert torch.equal(a.cache.table, b.cache.table) and torch.equal(a.cache.lengths, b.cache.lengths)
+    assert a.cache.poll_error() == 0 and b.cache.poll_error() == 0
+
+
+# ------------------------------------------------------------------ refusals of the host
+def test_arguments_are_refused_on_the_host():
+    f = Filled([40, 20], 2, 64, seed=18, layers=2)
+    c = f.cache
+    q = f.query([1, 1], 4)
+
+    def einval(call):
+        with pytest.raises(rtams.RtamsError) as e:
+            call()
+        assert e.value.code == rtams.EINVAL
+
+    einval(lambda: c.attend(2, q))
+    einval(lambda: c.attend(-1, q))
+    einval(lambda: c.attend(0, f.query([1, 1], 3)))               # heads that are no multiple
+    einval(lambda: c.attend(0, q, window=-1))
+    einval(lambda: c.attend(0, q, window=4, causal=False))
+    einval(lambda: c.attend(0, q, scale=float("inf")))
+    einval(lambda: c.attend(0, q, starts=ints([0, 1, 2]), max_new=0))
+    einval(lambda: c.extend(n=3))
+    einval(lambda: c.write(5, f.k, f.v, starts=ints([0, 40, 60]), max_new=40))
+    einval(lambda: c.read(0, 3, seqs=ints([0, 1])))
+    for call in (lambda: c.attend(0, q.float()), lambda: c.attend(0, q[0]), lambda: c.attend(0, q.cpu()), lambda: c.attend(0, q, seqs=ints([0, 1]).long()),
+                 lambda: c.attend(0, q, starts=ints([0, 1, 2])), lambda: c.attend(0, q, out=q.half()), lambda: c.attend(0, q, lse=torch.empty(2, device=DEV)),
+                 lambda: c.write(0, f.k, f.v[:3]), lambda: c.write(0, f.k[:, :1], f.v[:, :1]), lambda: c.extend(), lambda: c.trim(),
+                 lambda: c.fork(ints([0]), ints([1, 1])), lambda: c.read(0, 2, dtype=torch.float64), lambda: c.attend(0, q.transpose(1, 2).contiguous().transpose(1, 2))):
+        with pytest.raises(ValueError):
+            call()
+    # nothing to do
+    assert c.attend(0, q[:0]).shape == (0, 4, 64)
+    c.extend(n=0), c.trim(n=0), c.write(0, f.k[:0], f.v[:0])
+    torch.cuda.synchronize()
+    assert c.poll_error() == 0
+
+
+def test_items_that_attention_refuses_are_left_out():
+    f = Filled([40, 20], 2, 64, seed=19, max_seqs=3)
+    q = f.query([1, 1], 4)
+    good = f.cache.attend(0, q)
+    for seqs in ([0, 3], [0, -1]):
+        out = f.cache.attend(0, q, ints(seqs), out=torch.zeros_like(q))
+        assert torch.equal(out[0], good[0]) and not out[1].any()
+        assert f.cache.poll_error() == rtams.EINVAL
+        f.cache.clear_error()
+    out = f.cache.attend(0, f.query([5, 3], 4), starts=ints([0, 5, 9]), max_new=5, out=torch.zeros((8, 4, 64), dtype=torch.bfloat16, device=DEV))
+    torch.cuda.synchronize()
+    assert not out[5:].any() and f.cache.poll_error() == rtams.EINVAL
