@@ -82,6 +82,18 @@ __device__ uint32_t number_steps(const CacheDev &d, const CacheQuery &q, int bas
   return all;
 }
 
+// Parts of rows pass between workgroups on different dies: stores that go through to where all dies read, and loads that look
+// there.  (Fences would write back and drop a whole L2 each time: 0.25 ms for 768 workgroups.)
+__device__ inline void put_pair(float *p, float x, float y) {
+  const uint64_t v = (uint64_t)__float_as_uint(y) << 32 | __float_as_uint(x);
+  __hip_atomic_store(reinterpret_cast<uint64_t *>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+__device__ inline float2 get_pair(const float *p) {
+  const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+}
+
 // The worker that step u falls to: worker w has the steps [all * w / workers, all * (w + 1) / workers).
 __device__ inline uint32_t worker_of(uint32_t u, uint32_t all, uint32_t workers) {
   return (uint32_t)((((uint64_t)u + 1) * workers - 1) / all);
@@ -226,12 +238,10 @@ __device__ void attend_piece(const CacheDev &d, const CacheQuery &q, const Span 
         if (whole) {
           store_row(q, sp.row0 + (row_base + row) / q.share, head * q.share + (row_base + row) % q.share, c0 + c, v, top, sum);
         } else {
-          *reinterpret_cast<f32x4 *>(d.part + ((int64_t)slot * (16 * NR) + row) * D + c0 + c) = v;
-          if (c0 + c == 0) {
-            float *ml = d.part_ml + ((int64_t)slot * (16 * NR) + row) * 2;
-            ml[0] = top;
-            ml[1] = sum;
-          }
+          float *part = d.part + ((int64_t)slot * (16 * NR) + row) * D + c0 + c;
+          put_pair(part, v[0], v[1]);
+          put_pair(part + 2, v[2], v[3]);
+          if (c0 + c == 0) put_pair(d.part_ml + ((int64_t)slot * (16 * NR) + row) * 2, top, sum);
         }
       }
       __syncthreads();
@@ -239,28 +249,27 @@ __device__ void attend_piece(const CacheDev &d, const CacheQuery &q, const Span 
   }
   if (whole) return;
   const uint32_t w0 = worker_of(first_unit, all, workers), w1 = worker_of(first_unit + sp.steps - 1, all, workers);
-  __threadfence();
-  __syncthreads();
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wavefront's part is out ...
+  __syncthreads();                                  // ... and that of the others
   if (threadIdx.x == 0) {
     uint32_t *there = d.arrived + (int64_t)item * d.kv_heads + head;
-    const bool last = __hip_atomic_fetch_add(there, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == w1 - w0;
+    const bool last = __hip_atomic_fetch_add(there, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == w1 - w0;
     if (last) __hip_atomic_store(there, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     sh.last = last;
   }
   __syncthreads();
   if (sh.last) {
-    __threadfence();
     for (int u = threadIdx.x; u < rows * (D / 4); u += kLanes) {
       const int row = u / (D / 4), c = u % (D / 4) * 4;
       float top = -INFINITY, sum = 0.0f;
       f32x4 v{0, 0, 0, 0};
-      for (uint32_t w = w0; w <= w1; ++w) top = fmaxf(top, d.part_ml[((int64_t)(w * 2 + (w == w0)) * (16 * NR) + row) * 2]);
+      for (uint32_t w = w0; w <= w1; ++w) top = fmaxf(top, get_pair(d.part_ml + ((int64_t)(w * 2 + (w == w0)) * (16 * NR) + row) * 2).x);
       for (uint32_t w = w0; w <= w1; ++w) {
         const int64_t at = (int64_t)(w * 2 + (w == w0)) * (16 * NR) + row;
-        const float mw = d.part_ml[at * 2];
-        const float by = mw == -INFINITY && top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(mw - top);
-        sum += d.part_ml[at * 2 + 1] * by;
-        v += *reinterpret_cast<const f32x4 *>(d.part + at * D + c) * by;
+        const float2 ml = get_pair(d.part_ml + at * 2), a = get_pair(d.part + at * D + c), b2 = get_pair(d.part + at * D + c + 2);
+        const float by = ml.x == -INFINITY && top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ml.x - top);
+        sum += ml.y * by;
+        v += f32x4{a.x, a.y, b2.x, b2.y} * by;
       }
       store_row(q, sp.row0 + (row_base + row) / q.share, head * q.share + (row_base + row) % q.share, c, v, top, sum);
     }
