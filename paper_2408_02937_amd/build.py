@@ -9,7 +9,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librtams.so")
 SOURCES = ["rtams.hip", "coarse.hip", "coarse_mfma.hip", "insert.hip", "pq.hip", "probe.hip", "group.hip", "scan.hip", "scan_mm.hip", "scan_halves.hip",
            "pq_scan.hip", "small.hip", "select.hip", "rearrange.hip", "maint.hip",
-           "cache.hip", "cache_pages.hip", "cache_write.hip", "cache_attend.hip"]
+           "cache.hip", "cache_pages.hip", "cache_write.hip", "cache_attend.hip", "cache_prompt.hip"]
 HEADERS = ["rtams_dev.h", "rtams_launch.h", "search_common.h", "coarse_exact.h", "bound.h",
            "probe_plan.h", "scan_item.h", "scan_tile.h", "halves.h", "host.h", "cache.h", "cache_mm.h", os.path.join("..", "..", "include", "rtams.h"),
            os.path.join("..", "..", "include", "rtams_cache.h"),

@@ -132,6 +132,11 @@ void launch_cache_write(const CacheDev &d, const CacheRows &r, int layer, const 
                         int64_t head_stride, bool half_type, bool vec, hipStream_t s);
 void launch_cache_read(const CacheDev &d, const CacheRows &r, int layer, void *k, void *v, int type, hipStream_t s);
 void launch_cache_attend(const CacheDev &d, const CacheQuery &q, hipStream_t s);
+void launch_cache_prompt(const CacheDev &d, const CacheQuery &q, hipStream_t s);  // (many rows; launch_cache_attend chooses)
+hipError_t allow_large_lds_cache();
+size_t cache_prompt_part_floats(int head_dim);
+size_t cache_prompt_part_ml_floats();
+size_t cache_prompt_groups();
 size_t cache_part_floats(int head_dim);    // room for parts of rows: values,
 size_t cache_part_ml_floats(int head_dim); // maxima and sums,
 size_t cache_arrived_words(int max_seqs, int kv_heads);

@@ -82,30 +82,18 @@ __device__ uint32_t number_steps(const CacheDev &d, const CacheQuery &q, int bas
   return all;
 }
 
-// Parts of rows pass between workgroups on different dies: stores that go through to where all dies read, and loads that look
-// there.  (Fences would write back and drop a whole L2 each time: 0.25 ms for 768 workgroups.)
-__device__ inline void put_pair(float *p, float x, float y) {
-  const uint64_t v = (uint64_t)__float_as_uint(y) << 32 | __float_as_uint(x);
-  __hip_atomic_store(reinterpret_cast<uint64_t *>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-
-__device__ inline float2 get_pair(const float *p) {
-  const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
-}
-
 // The worker that step u falls to: worker w has the steps [all * w / workers, all * (w + 1) / workers).
 __device__ inline uint32_t worker_of(uint32_t u, uint32_t all, uint32_t workers) {
   return (uint32_t)((((uint64_t)u + 1) * workers - 1) / all);
 }
 
-// Rows row_base .. of item span, steps [sa, sb) of its head.
+// Steps [sa, sb) of an item's head; first_unit: the number of its step 0.
 template <int D, int NR>
-__device__ void attend_piece(const CacheDev &d, const CacheQuery &q, const Span &sp, int item, int head, int row_base, int sa, int sb, uint32_t first_unit,
+__device__ void attend_piece(const CacheDev &d, const CacheQuery &q, const Span &sp, int item, int head, int sa, int sb, uint32_t first_unit,
                              uint32_t all, uint32_t workers, uint32_t worker, Shared<D, NR> &sh) {
   constexpr int NJ = D / 32, NT = D / 16, CH = joined(D);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, b = lane >> 4;
-  const int rows = q.share * sp.count - row_base;  // of the item, from row_base on
+  const int rows = q.share * sp.count;
 
   half8 qf[NR][NJ];
   int see_to[NR], see_from[NR];
@@ -113,7 +101,7 @@ __device__ void attend_piece(const CacheDev &d, const CacheQuery &q, const Span 
   for (int t = 0; t < NR; ++t) {
     const int row = t * 16 + col;
     const bool real = row < rows;
-    const int j = real ? (row_base + row) / q.share : 0, h = real ? (row_base + row) % q.share : 0;
+    const int j = real ? row / q.share : 0, h = real ? row % q.share : 0;
     const int pos = sp.length - sp.count + j;
     see_to[t] = q.causal ? pos + 1 : sp.length;
     see_from[t] = q.window ? pos - q.window + 1 : 0;
@@ -236,7 +224,7 @@ __device__ void attend_piece(const CacheDev &d, const CacheQuery &q, const Span 
           v += *reinterpret_cast<const f32x4 *>(&sh.o[w][r][c]);
         }
         if (whole) {
-          store_row(q, sp.row0 + (row_base + row) / q.share, head * q.share + (row_base + row) % q.share, c0 + c, v, top, sum);
+          store_row(q, sp.row0 + row / q.share, head * q.share + row % q.share, c0 + c, v, top, sum);
         } else {
           float *part = d.part + ((int64_t)slot * (16 * NR) + row) * D + c0 + c;
           put_pair(part, v[0], v[1]);
@@ -259,19 +247,12 @@ __device__ void attend_piece(const CacheDev &d, const CacheQuery &q, const Span 
   }
   __syncthreads();
   if (sh.last) {
+    // (slot 2 w + 1 has what worker w began and did not end, slot 2 w what it found begun)
     for (int u = threadIdx.x; u < rows * (D / 4); u += kLanes) {
       const int row = u / (D / 4), c = u % (D / 4) * 4;
-      float top = -INFINITY, sum = 0.0f;
-      f32x4 v{0, 0, 0, 0};
-      for (uint32_t w = w0; w <= w1; ++w) top = fmaxf(top, get_pair(d.part_ml + ((int64_t)(w * 2 + (w == w0)) * (16 * NR) + row) * 2).x);
-      for (uint32_t w = w0; w <= w1; ++w) {
-        const int64_t at = (int64_t)(w * 2 + (w == w0)) * (16 * NR) + row;
-        const float2 ml = get_pair(d.part_ml + at * 2), a = get_pair(d.part + at * D + c), b2 = get_pair(d.part + at * D + c + 2);
-        const float by = ml.x == -INFINITY && top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ml.x - top);
-        sum += ml.y * by;
-        v += f32x4{a.x, a.y, b2.x, b2.y} * by;
-      }
-      store_row(q, sp.row0 + (row_base + row) / q.share, head * q.share + (row_base + row) % q.share, c, v, top, sum);
+      const int64_t at = (int64_t)(w0 * 2 + 1) * (16 * NR) + row;
+      join_parts(q, sp.row0 + row / q.share, head * q.share + row % q.share, c, (int)(w1 - w0 + 1), d.part + at * D + c, d.part_ml + at * 2,
+                 D, 16 * NR, 32 * NR);
     }
   }
   __syncthreads();
@@ -303,40 +284,36 @@ __global__ __launch_bounds__(kLanes) void k_cache_attend(CacheDev d, CacheQuery 
       const uint32_t within = u - sh.before[lo];
       const int head = (int)(within / (uint32_t)sp.steps), sa = (int)(within % (uint32_t)sp.steps);
       const uint32_t left = end - u, rest = (uint32_t)(sp.steps - sa), take = left < rest ? left : rest;
-      attend_piece<D, NR>(d, q, sp, item, head, 0, sa, sa + (int)take, u - (uint32_t)sa, all, workers, worker, sh);
+      attend_piece<D, NR>(d, q, sp, item, head, sa, sa + (int)take, u - (uint32_t)sa, all, workers, worker, sh);
       u += take;
     }
   }
 }
 
-// Rows that are more than the columns of a piece: a workgroup has 16 NR of them over all the tokens they see.
-template <int D, int NR>
-__global__ __launch_bounds__(kLanes) void k_cache_attend_rows(CacheDev d, CacheQuery q) {
-  __shared__ Shared<D, NR> sh;
-  const int item = blockIdx.x / d.kv_heads, head = blockIdx.x % d.kv_heads;
-  const Span sp = find_span(d, q, item, blockIdx.y == 0 && head == 0 && threadIdx.x == 0);
-  for (int row = blockIdx.y * 16 * NR; row < q.share * sp.count; row += gridDim.y * 16 * NR)
-    attend_piece<D, NR>(d, q, sp, item, head, row, 0, sp.steps, 0, 1, 1, 0, sh);
-}
-
 }  // namespace
 
-size_t cache_part_floats(int head_dim) { return (size_t)kWorkers * 2 * 32 * head_dim; }
-size_t cache_part_ml_floats(int) { return (size_t)kWorkers * 2 * 32 * 2; }
-size_t cache_arrived_words(int max_seqs, int kv_heads) { return (size_t)max_seqs * kv_heads; }
+size_t cache_part_floats(int head_dim) {
+  const size_t few = (size_t)kWorkers * 2 * 32 * head_dim, many = cache_prompt_part_floats(head_dim);
+  return few > many ? few : many;
+}
+size_t cache_part_ml_floats(int) {
+  const size_t few = (size_t)kWorkers * 2 * 32 * 2, many = cache_prompt_part_ml_floats();
+  return few > many ? few : many;
+}
+size_t cache_arrived_words(int max_seqs, int kv_heads) {
+  const size_t few = (size_t)max_seqs * kv_heads, many = cache_prompt_groups();
+  return few > many ? few : many;
+}
 
 void launch_cache_attend(const CacheDev &d, const CacheQuery &q, hipStream_t s) {
   const int64_t rows = (int64_t)q.share * q.r.max_new;
-  auto few = [&](auto one, auto two) {
-    if (rows <= 16) one<<<kWorkers, kLanes, 0, s>>>(d, q);
-    else two<<<kWorkers, kLanes, 0, s>>>(d, q);
-  };
-  auto many = [&](auto kernel) { kernel<<<dim3(q.r.n * d.kv_heads, (uint32_t)((rows + 31) / 32 < 4096 ? (rows + 31) / 32 : 4096)), kLanes, 0, s>>>(d, q); };
+  const auto go = [&](auto kernel) { kernel<<<kWorkers, kLanes, 0, s>>>(d, q); };
+  if (rows > (d.head_dim == 256 ? 16 : 32)) return launch_cache_prompt(d, q, s);
   switch (d.head_dim) {
-    case 64: return rows <= 32 ? few(k_cache_attend<64, 1>, k_cache_attend<64, 2>) : many(k_cache_attend_rows<64, 2>);
-    case 96: return rows <= 32 ? few(k_cache_attend<96, 1>, k_cache_attend<96, 2>) : many(k_cache_attend_rows<96, 2>);
-    case 128: return rows <= 32 ? few(k_cache_attend<128, 1>, k_cache_attend<128, 2>) : many(k_cache_attend_rows<128, 2>);
-    default: return rows <= 16 ? few(k_cache_attend<256, 1>, k_cache_attend<256, 1>) : many(k_cache_attend_rows<256, 1>);
+    case 64: return rows <= 16 ? go(k_cache_attend<64, 1>) : go(k_cache_attend<64, 2>);
+    case 96: return rows <= 16 ? go(k_cache_attend<96, 1>) : go(k_cache_attend<96, 2>);
+    case 128: return rows <= 16 ? go(k_cache_attend<128, 1>) : go(k_cache_attend<128, 2>);
+    default: return go(k_cache_attend<256, 1>);
   }
 }
 

@@ -175,4 +175,32 @@ __device__ inline void store_row(const CacheQuery &q, int64_t row, int head, int
   if (q.lse && c == 0) q.lse[row * q.q_heads + head] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
 }
 
+// Parts of rows pass between workgroups on different dies: stores that go through to where all dies read, and loads that look
+// there.  (Fences would write back and drop a whole L2 each time: 0.25 ms for 768 workgroups.)
+__device__ inline void put_pair(float *p, float x, float y) {
+  const uint64_t v = (uint64_t)__float_as_uint(y) << 32 | __float_as_uint(x);
+  __hip_atomic_store(reinterpret_cast<uint64_t *>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+__device__ inline float2 get_pair(const float *p) {
+  const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+}
+
+// Channels c .. c + 3 of a row of n parts, joined in order.  Part 0 is at part and ml (its maximum and sum); the next is `gap` rows on, every
+// further one `stride` rows.
+__device__ inline void join_parts(const CacheQuery &q, int64_t row, int head, int c, int n, const float *part, const float *ml, int head_dim, int gap, int stride) {
+  const auto at = [&](int i) { return i ? (int64_t)gap + (int64_t)(i - 1) * stride : 0; };
+  float top = -INFINITY, sum = 0.0f;
+  for (int i = 0; i < n; ++i) top = fmaxf(top, get_pair(ml + at(i) * 2).x);
+  f32x4 v{0, 0, 0, 0};
+  for (int i = 0; i < n; ++i) {
+    const float2 x = get_pair(ml + at(i) * 2), a = get_pair(part + at(i) * head_dim), b = get_pair(part + at(i) * head_dim + 2);
+    const float by = x.x == -INFINITY && top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(x.x - top);
+    sum += x.y * by;
+    v += f32x4{a.x, a.y, b.x, b.y} * by;
+  }
+  store_row(q, row, head, c, v, top, sum);
+}
+
 }  // namespace rtams
