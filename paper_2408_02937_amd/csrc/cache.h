@@ -133,7 +133,8 @@ void launch_cache_write(const CacheDev &d, const CacheRows &r, int layer, const 
 void launch_cache_read(const CacheDev &d, const CacheRows &r, int layer, void *k, void *v, int type, hipStream_t s);
 void launch_cache_attend(const CacheDev &d, const CacheQuery &q, hipStream_t s);
 void launch_cache_prompt(const CacheDev &d, const CacheQuery &q, hipStream_t s);  // (many rows; launch_cache_attend chooses)
-hipError_t allow_large_lds_cache();
+hipError_t allow_large_lds_cache_attend();
+hipError_t allow_large_lds_cache_prompt();
 size_t cache_prompt_part_floats(int head_dim);
 size_t cache_prompt_part_ml_floats();
 size_t cache_prompt_groups();

@@ -208,7 +208,7 @@ int rtams_cache_create(const rtams_cache_config *cfg, rtams_cache **out) {
   q += up(cache_part_ml_floats(cfg->head_dim) * 4, kAlign);
   d.part = reinterpret_cast<float *>(q);
   auto bail = [&](int code) { rtams_cache_destroy(c); return code; };
-  if (allow_large_lds_cache() != hipSuccess) return bail(fail(RTAMS_EHIP, "allow_large_lds_cache failed"));
+  if (allow_large_lds_cache_attend() != hipSuccess || allow_large_lds_cache_prompt() != hipSuccess) return bail(fail(RTAMS_EHIP, "hipFuncSetAttribute failed"));
   void *hm = nullptr, *dm = nullptr;
   if (hipHostMalloc(&hm, sizeof(CacheMirror), hipHostMallocMapped) != hipSuccess) return bail(fail(RTAMS_EHIP, "hipHostMalloc failed"));
   c->mirror = static_cast<CacheMirror *>(hm);

@@ -11,6 +11,7 @@
 #include "../../include/rtams_cache.h"
 
 #include "cache_mm.h"
+#include "rtams_dev.h"
 
 namespace rtams {
 
@@ -46,16 +47,19 @@ __device__ inline Span find_span(const CacheDev &d, const CacheQuery &q, int i, 
   return s;
 }
 
-// Channels that the wavefronts join at a time: 32 KiB of LDS.
-constexpr int joined(int head_dim) { return head_dim < 128 ? head_dim : 128; }
+constexpr int kAhead = 2;   // blocks of a wavefront that are in LDS or on their way
+constexpr int kJoin = 32;   // channels that the wavefronts join at a time
+
+__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 template <int D, int NR>
-struct Shared {
+struct alignas(16) Shared {
+  unsigned char ring[kWaves][kAhead][40 * D];
   uint32_t before[kScan + 1];
   uint32_t waves[kWaves];
   int last;
   float ml[kWaves][16 * NR][2];
-  float o[kWaves][16][joined(D) + 4];
+  alignas(16) float o[kWaves][16][kJoin + 4];
 };
 
 // Numbers of the steps of items base .. base + 255 (times kv heads), from `at` on; returns the first number behind them.
@@ -87,13 +91,57 @@ __device__ inline uint32_t worker_of(uint32_t u, uint32_t all, uint32_t workers)
   return (uint32_t)((((uint64_t)u + 1) * workers - 1) / all);
 }
 
-// Steps [sa, sb) of an item's head; first_unit: the number of its step 0.
+struct Run {  // steps [sa, sb) of an item's head
+  Span sp;
+  int item, head, sa, sb;
+  uint32_t first_unit;  // the number of its step 0
+};
+
+typedef const __attribute__((address_space(4))) int32_t *ScalarInts;
+
+// The copies of a wavefront's blocks into its ring: block n of the run goes to slot n % kAhead.
+template <int D>
+struct Copies {
+  static constexpr int kCopies = (40 * D + 1023) / 1024;  // loads of a block
+  ScalarInts table;
+  int head, tok, to;   // next block's first token; end of the run's tokens
+  uint32_t ring, slot;
+  uint32_t page;       // of the next block
+
+  // (pages are looked up by scalar loads, a block ahead: a vector load would wait for all copies under way)
+  __device__ __forceinline__ void look(const CacheDev &d) {
+    if (tok < to) page = (uint32_t)table[cache_page_of(d, (uint32_t)tok / kBlockTokens)];
+  }
+  __device__ __forceinline__ void begin(const CacheDev &d, const Run &r, int wave, uint32_t ring_at) {
+    table = (ScalarInts)(uintptr_t)(d.table + (int64_t)r.sp.seq * d.max_pages);
+    head = r.head;
+    tok = r.sp.low + r.sa * kStep + wave * kBlockTokens;
+    to = min(r.sp.low + r.sb * kStep, r.sp.length);
+    ring = ring_at;
+    slot = 0;
+    look(d);
+  }
+  __device__ __forceinline__ void one(const CacheDev &d, int layer, int lane) {
+    if (tok >= to) return;
+    const uint32_t block = (uint32_t)tok / kBlockTokens;
+    const unsigned char *blk = cache_block(d, layer, (int)page, head, block - cache_page_of(d, block) * d.page_blocks);
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i)
+      if (40 * D - i * 1024 >= 1024 || lane * 16 < 40 * D - i * 1024) copy_to_lds(blk + i * 1024, ring + slot * (40 * D) + i * 1024, lane * 16);
+    slot ^= 1;
+    tok += kStep;
+    look(d);
+  }
+};
+
+// The copies of the run's first blocks are under way; those of `next`, if there is one, are when it returns.
 template <int D, int NR>
-__device__ void attend_piece(const CacheDev &d, const CacheQuery &q, const Span &sp, int item, int head, int sa, int sb, uint32_t first_unit,
-                             uint32_t all, uint32_t workers, uint32_t worker, Shared<D, NR> &sh) {
-  constexpr int NJ = D / 32, NT = D / 16, CH = joined(D);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, b = lane >> 4;
-  const int rows = q.share * sp.count;
+__device__ void attend_run(const CacheDev &d, const CacheQuery &q, const Run &run, bool more, const Run &next, uint32_t all, uint32_t workers, uint32_t worker, Copies<D> &cp,
+                           Shared<D, NR> &sh) {
+  constexpr int NJ = D / 32, NT = D / 16;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, b = lane >> 4;
+  const Span &sp = run.sp;
+  const int rows = q.share * sp.count, head = run.head;
 
   half8 qf[NR][NJ];
   int see_to[NR], see_from[NR];
@@ -121,17 +169,21 @@ __device__ void attend_piece(const CacheDev &d, const CacheQuery &q, const Span 
 #pragma unroll
     for (int n = 0; n < NT; ++n) o[t][n] = f32x4{0, 0, 0, 0};
   }
-  const int32_t *table = d.table + (int64_t)sp.seq * d.max_pages;
-  for (int s = sa; s < sb; ++s) {
-    const int tok0 = __builtin_amdgcn_readfirstlane(sp.low + s * kStep + wave * kBlockTokens);
-    if (tok0 >= sp.length) break;
-    const uint32_t block = (uint32_t)tok0 / kBlockTokens, pg = cache_page_of(d, block);
-    const unsigned char *blk = cache_block(d, q.layer, table[pg], head, block - pg * d.page_blocks);
+  const int to = cp.to;
+  uint32_t slot = 0;
+  for (int tok0 = sp.low + run.sa * kStep + wave * kBlockTokens; tok0 < to; tok0 += kStep) {
+    static_assert(kAhead == 2, "one block behind this one");
+    if (tok0 + kStep < to) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Copies<D>::kCopies) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    const unsigned char *blk = sh.ring[wave][slot];
     KeyTile<D> kt[2];
     kt[0].load(blk, 0, lane);
     kt[1].load(blk, 1, lane);
     ValueBlock<D> vb;
     vb.load(blk, lane);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slot has been read
+    slot ^= 1;
+    cp.one(d, q.layer, lane);
     f32x4 sc[NR][2];
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
@@ -188,6 +240,10 @@ __device__ void attend_piece(const CacheDev &d, const CacheQuery &q, const Span 
       for (int t = 0; t < NR; ++t) o[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pf[t], o[t][n], 0, 0, 0);
     }
   }
+  if (more) {  // (this wavefront has read its ring)
+    cp.begin(d, next, wave, cp.ring);
+    for (int i = 0; i < kAhead; ++i) cp.one(d, q.layer, lane);
+  }
 
   // The wavefronts' parts of each row.
 #pragma unroll
@@ -200,47 +256,48 @@ __device__ void attend_piece(const CacheDev &d, const CacheQuery &q, const Span 
     }
   }
   __syncthreads();
-  const bool whole = sa == 0 && sb == sp.steps;
-  const uint32_t slot = worker * 2 + (sa == 0 ? 1 : 0);
+  const bool whole = run.sa == 0 && run.sb == sp.steps;
+  const uint32_t slot_at = worker * 2 + (run.sa == 0 ? 1 : 0);
 #pragma unroll
   for (int t = 0; t < NR; ++t) {
     float most = -INFINITY;
     for (int w = 0; w < kWaves; ++w) most = fmaxf(most, sh.ml[w][t * 16 + col][0]);
     const float by = m[t] == -INFINITY && most == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[t] - most);
 #pragma unroll
-    for (int c0 = 0; c0 < D; c0 += CH) {
+    for (int c0 = 0; c0 < D; c0 += kJoin) {
 #pragma unroll
-      for (int n = 0; n < CH / 16; ++n) *reinterpret_cast<f32x4 *>(&sh.o[wave][col][n * 16 + b * 4]) = o[t][c0 / 16 + n] * by;
+      for (int n = 0; n < kJoin / 16; ++n) *reinterpret_cast<f32x4 *>(&sh.o[wave][col][n * 16 + b * 4]) = o[t][c0 / 16 + n] * by;
       __syncthreads();
-      for (int u = threadIdx.x; u < 16 * (CH / 4); u += kLanes) {
-        const int r = u / (CH / 4), c = u % (CH / 4) * 4, row = t * 16 + r;
-        if (row >= rows) continue;
-        float top = -INFINITY, sum = 0.0f;
-        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sh.ml[w][row][0]);
-        f32x4 v{0, 0, 0, 0};
-        for (int w = 0; w < kWaves; ++w) {
-          const float mw = sh.ml[w][row][0];
-          sum += sh.ml[w][row][1] * (mw == -INFINITY && top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(mw - top));
-          v += *reinterpret_cast<const f32x4 *>(&sh.o[w][r][c]);
-        }
-        if (whole) {
-          store_row(q, sp.row0 + row / q.share, head * q.share + row % q.share, c0 + c, v, top, sum);
-        } else {
-          float *part = d.part + ((int64_t)slot * (16 * NR) + row) * D + c0 + c;
-          put_pair(part, v[0], v[1]);
-          put_pair(part + 2, v[2], v[3]);
-          if (c0 + c == 0) put_pair(d.part_ml + ((int64_t)slot * (16 * NR) + row) * 2, top, sum);
+      if (threadIdx.x < 16 * (kJoin / 4)) {
+        const int r = threadIdx.x / (kJoin / 4), c = threadIdx.x % (kJoin / 4) * 4, row = t * 16 + r;
+        if (row < rows) {
+          float top = -INFINITY, sum = 0.0f;
+          for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sh.ml[w][row][0]);
+          f32x4 v{0, 0, 0, 0};
+          for (int w = 0; w < kWaves; ++w) {
+            const float mw = sh.ml[w][row][0];
+            sum += sh.ml[w][row][1] * (mw == -INFINITY && top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(mw - top));
+            v += *reinterpret_cast<const f32x4 *>(&sh.o[w][r][c]);
+          }
+          if (whole) {
+            store_row(q, sp.row0 + row / q.share, head * q.share + row % q.share, c0 + c, v, top, sum);
+          } else {
+            float *part = d.part + ((int64_t)slot_at * (16 * NR) + row) * D + c0 + c;
+            put_pair(part, v[0], v[1]);
+            put_pair(part + 2, v[2], v[3]);
+            if (c0 + c == 0) put_pair(d.part_ml + ((int64_t)slot_at * (16 * NR) + row) * 2, top, sum);
+          }
         }
       }
       __syncthreads();
     }
   }
   if (whole) return;
-  const uint32_t w0 = worker_of(first_unit, all, workers), w1 = worker_of(first_unit + sp.steps - 1, all, workers);
+  const uint32_t w0 = worker_of(run.first_unit, all, workers), w1 = worker_of(run.first_unit + sp.steps - 1, all, workers);
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wavefront's part is out ...
   __syncthreads();                                  // ... and that of the others
   if (threadIdx.x == 0) {
-    uint32_t *there = d.arrived + (int64_t)item * d.kv_heads + head;
+    uint32_t *there = d.arrived + (int64_t)run.item * d.kv_heads + head;
     const bool last = __hip_atomic_fetch_add(there, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == w1 - w0;
     if (last) __hip_atomic_store(there, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     sh.last = last;
@@ -259,8 +316,9 @@ __device__ void attend_piece(const CacheDev &d, const CacheQuery &q, const Span 
 }
 
 template <int D, int NR>
-__global__ __launch_bounds__(kLanes) void k_cache_attend(CacheDev d, CacheQuery q) {
-  __shared__ Shared<D, NR> sh;
+__global__ __launch_bounds__(kLanes, NR == 1 && D <= 128 ? 3 : 1) void k_cache_attend(CacheDev d, CacheQuery q) {
+  extern __shared__ uint4 lds[];
+  Shared<D, NR> &sh = *reinterpret_cast<Shared<D, NR> *>(lds);
   const bool tell = blockIdx.x == 0;
   uint32_t all = 0;
   for (int base = 0; base < q.r.n; base += kScan) all = number_steps<D, NR>(d, q, base, all, sh, tell);
@@ -269,24 +327,44 @@ __global__ __launch_bounds__(kLanes) void k_cache_attend(CacheDev d, CacheQuery 
   if (worker >= workers) return;
   uint32_t u = (uint32_t)((uint64_t)all * worker / workers);
   const uint32_t end = (uint32_t)((uint64_t)all * (worker + 1) / workers);
-  uint32_t at = 0;
-  for (int base = 0; base < q.r.n && u < end; base += kScan) {
-    if (q.r.n > kScan) at = number_steps<D, NR>(d, q, base, at, sh, false);
-    while (u < end && u < sh.before[kScan]) {
-      int lo = 0, hi = kScan - 1;  // the last item whose steps begin at u or before
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (sh.before[mid] <= u) lo = mid;
-        else hi = mid - 1;
-      }
-      const int item = base + lo;
-      const Span sp = find_span(d, q, item, false);
-      const uint32_t within = u - sh.before[lo];
-      const int head = (int)(within / (uint32_t)sp.steps), sa = (int)(within % (uint32_t)sp.steps);
-      const uint32_t left = end - u, rest = (uint32_t)(sp.steps - sa), take = left < rest ? left : rest;
-      attend_piece<D, NR>(d, q, sp, item, head, sa, sa + (int)take, u - (uint32_t)sa, all, workers, worker, sh);
-      u += take;
+  int base = 0;
+  if (q.r.n > kScan) {
+    uint32_t at = number_steps<D, NR>(d, q, 0, 0, sh, false);
+    while (at <= u) at = number_steps<D, NR>(d, q, base += kScan, at, sh, false);
+  }
+  // The run that step u begins or goes on with; u moves behind it.
+  const auto find_run = [&]() {
+    while (u >= sh.before[kScan]) number_steps<D, NR>(d, q, base += kScan, sh.before[kScan], sh, false);
+    int lo = 0, hi = kScan - 1;  // the last item whose steps begin at u or before
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) / 2;
+      if (sh.before[mid] <= u) lo = mid;
+      else hi = mid - 1;
     }
+    Run r;
+    r.item = base + lo;
+    r.sp = find_span(d, q, r.item, false);
+    const uint32_t within = u - sh.before[lo], steps = (uint32_t)r.sp.steps, take = min(end - u, steps - within % steps);
+    r.head = (int)(within / steps);
+    r.sa = (int)(within % steps);
+    r.sb = r.sa + (int)take;
+    r.first_unit = u - (uint32_t)r.sa;
+    u += take;
+    r.sp.row0 = (int64_t)uniform((int)((uint64_t)r.sp.row0 >> 32)) << 32 | (uint32_t)uniform((int)r.sp.row0);
+    r.sp = Span{uniform(r.sp.seq), uniform(r.sp.count), uniform(r.sp.length), uniform(r.sp.low), uniform(r.sp.steps), r.sp.row0};
+    return Run{r.sp, uniform(r.item), uniform(r.head), uniform(r.sa), uniform(r.sb), (uint32_t)uniform((int)r.first_unit)};
+  };
+  Run run = find_run();
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  Copies<D> cp;
+  cp.begin(d, run, wave, (uint32_t)uniform((int)lds_address(sh.ring[wave][0])));
+  for (int i = 0; i < kAhead; ++i) cp.one(d, q.layer, lane);
+  for (;;) {
+    const bool more = u < end;
+    const Run next = more ? find_run() : run;
+    attend_run<D, NR>(d, q, run, more, next, all, workers, worker, cp, sh);
+    if (!more) return;
+    run = next;
   }
 }
 
@@ -307,14 +385,18 @@ size_t cache_arrived_words(int max_seqs, int kv_heads) {
 
 void launch_cache_attend(const CacheDev &d, const CacheQuery &q, hipStream_t s) {
   const int64_t rows = (int64_t)q.share * q.r.max_new;
-  const auto go = [&](auto kernel) { kernel<<<kWorkers, kLanes, 0, s>>>(d, q); };
+  const auto go = [&](auto kernel, size_t lds) { kernel<<<kWorkers, kLanes, lds, s>>>(d, q); };
   if (rows > (d.head_dim == 256 ? 16 : 32)) return launch_cache_prompt(d, q, s);
   switch (d.head_dim) {
-    case 64: return rows <= 16 ? go(k_cache_attend<64, 1>) : go(k_cache_attend<64, 2>);
-    case 96: return rows <= 16 ? go(k_cache_attend<96, 1>) : go(k_cache_attend<96, 2>);
-    case 128: return rows <= 16 ? go(k_cache_attend<128, 1>) : go(k_cache_attend<128, 2>);
-    default: return go(k_cache_attend<256, 1>);
+    case 64: return rows <= 16 ? go(k_cache_attend<64, 1>, sizeof(Shared<64, 1>)) : go(k_cache_attend<64, 2>, sizeof(Shared<64, 2>));
+    case 96: return rows <= 16 ? go(k_cache_attend<96, 1>, sizeof(Shared<96, 1>)) : go(k_cache_attend<96, 2>, sizeof(Shared<96, 2>));
+    case 128: return rows <= 16 ? go(k_cache_attend<128, 1>, sizeof(Shared<128, 1>)) : go(k_cache_attend<128, 2>, sizeof(Shared<128, 2>));
+    default: return go(k_cache_attend<256, 1>, sizeof(Shared<256, 1>));
   }
+}
+
+hipError_t allow_large_lds_cache_attend() {
+  return hipFuncSetAttribute(reinterpret_cast<const void *>(k_cache_attend<256, 1>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Shared<256, 1>));
 }
 
 }  // namespace rtams

@@ -308,7 +308,7 @@ void launch_cache_prompt(const CacheDev &d, const CacheQuery &q, hipStream_t s) 
   }
 }
 
-hipError_t allow_large_lds_cache() {
+hipError_t allow_large_lds_cache_prompt() {
   const auto allow = [](const void *f, int bytes) { return hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, bytes); };
   return allow(reinterpret_cast<const void *>(k_cache_prompt<256, 4>), 2 * (int)sizeof(Staging<256>));
 }
