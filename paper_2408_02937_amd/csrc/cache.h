@@ -135,8 +135,7 @@ void launch_cache_attend(const CacheDev &d, const CacheQuery &q, hipStream_t s);
 void launch_cache_prompt(const CacheDev &d, const CacheQuery &q, hipStream_t s);  // (many rows; launch_cache_attend chooses)
 hipError_t allow_large_lds_cache_attend();
 hipError_t allow_large_lds_cache_prompt();
-size_t cache_prompt_part_floats(int head_dim);
-size_t cache_prompt_part_ml_floats();
+size_t cache_prompt_part_rows();
 size_t cache_prompt_groups();
 size_t cache_part_floats(int head_dim);    // room for parts of rows: values,
 size_t cache_part_ml_floats(int head_dim); // maxima and sums,

@@ -3,7 +3,7 @@
 //   s_t = scale * q . K_t,  o = sum_t exp(s_t - m) V_t / sum_t exp(s_t - m),  m the running maximum
 //
 // Bound by the bytes of the cache: 1.25 a channel and token for keys and values together.  A step of a workgroup is 128 tokens of
-// one kv head, 32 to a wavefront; the steps of all sequences and heads lie on one line, which is cut into equal pieces, so
+// one kv head, 32 to a wavefront; a workgroup takes a piece of a head's steps, of a size that lets all pieces run at once, so
 // that ragged lengths fill the chip alike.  The query heads that share a kv head (times an item's rows) are the 16 columns of
 // the matrix instructions.  Codes become halves in registers, straight from the loads: scores come out as S^T = K Q^T,
 // tokens down and rows across, which is the operand that O^T = V^T P^T takes, so nothing is transposed and LDS only joins
@@ -18,8 +18,13 @@ namespace rtams {
 namespace {
 
 constexpr int kLanes = 256, kWaves = 4, kStep = kWaves * kBlockTokens;
-constexpr int kWorkers = 768;    // workgroups of a launch: three to a compute unit
-constexpr int kScan = 256;       // items that are numbered at a time
+constexpr int kUnits = 256;      // compute units
+constexpr int kSizes = 16;       // sizes of pieces that are tried
+
+// Workgroups that a compute unit runs at once: registers decide, and from 128 channels on LDS.
+constexpr int at_once(int head_dim, int tiles) {
+  return tiles == 2 ? (head_dim == 64 ? 3 : 2) : head_dim == 64 ? 5 : head_dim == 96 ? 4 : head_dim == 128 ? 3 : 1;
+}
 
 struct Span {  // what an item asks for
   int seq, count, length, low;  // low: first position that a row of it sees, rounded down to a block
@@ -48,78 +53,89 @@ __device__ inline Span find_span(const CacheDev &d, const CacheQuery &q, int i, 
 }
 
 constexpr int kAhead = 2;   // blocks of a wavefront that are in LDS or on their way
-constexpr int kJoin = 32;   // channels that the wavefronts join at a time
 
-__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+struct Piece {  // steps [sa, sb) of an item's head
+  int item, head, sa, sb;
+  int parts, nth;  // pieces of the head; which one this is
+  int part;        // where the head's parts begin, if there are several
+};
 
 template <int D, int NR>
 struct alignas(16) Shared {
-  unsigned char ring[kWaves][kAhead][40 * D];
-  uint32_t before[kScan + 1];
-  uint32_t waves[kWaves];
-  int last;
+  union {
+    unsigned char ring[kWaves][kAhead][40 * D];
+    float o[kWaves][16][D + 4];  // when the rings are read: the wavefronts' parts of 16 rows
+  };
   float ml[kWaves][16 * NR][2];
-  alignas(16) float o[kWaves][16][kJoin + 4];
+  uint64_t waves[kWaves];
+  uint32_t sizes[kWaves][kSizes];
+  Piece piece;
+  int last;
 };
 
-// Numbers of the steps of items base .. base + 255 (times kv heads), from `at` on; returns the first number behind them.
-template <int D, int NR>
-__device__ uint32_t number_steps(const CacheDev &d, const CacheQuery &q, int base, uint32_t at, Shared<D, NR> &sh, bool tell) {
+__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// The sum over the workgroup and, in *before, over the lanes in front.
+template <class S>
+__device__ uint64_t scan_lanes(uint64_t v, uint64_t *before, S &sh) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint32_t mine = (uint32_t)find_span(d, q, base + threadIdx.x, tell).steps * (uint32_t)d.kv_heads;
-  uint32_t inc = mine;
+  uint64_t inc = v;
+#pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const uint32_t x = __shfl_up(inc, o);
+    const uint64_t x = __shfl_up(inc, o);
     if (lane >= o) inc += x;
   }
   __syncthreads();
   if (lane == 63) sh.waves[wave] = inc;
   __syncthreads();
-  uint32_t lower = at, all = at;
+  uint64_t lower = 0, all = 0;
+#pragma unroll
   for (int w = 0; w < kWaves; ++w) {
     lower += w < wave ? sh.waves[w] : 0;
     all += sh.waves[w];
   }
-  sh.before[threadIdx.x] = lower + inc - mine;
-  if (threadIdx.x == 0) sh.before[kScan] = all;
-  __syncthreads();
+  *before = lower + inc - v;
   return all;
 }
 
-// The worker that step u falls to: worker w has the steps [all * w / workers, all * (w + 1) / workers).
-__device__ inline uint32_t worker_of(uint32_t u, uint32_t all, uint32_t workers) {
-  return (uint32_t)((((uint64_t)u + 1) * workers - 1) / all);
+// Steps of a piece, of `all` steps.  Pieces are to run all at once, so where items are few sixteen sizes from an even share up to twice that
+// are tried and the least is taken with which they do.  Where items are many, pieces are an even share at most, and long items do not keep the others waiting.
+template <class S>
+__device__ uint32_t piece_steps(const CacheDev &d, const CacheQuery &q, uint32_t mine, uint64_t all, uint32_t workers, S &sh) {
+  const uint32_t share = (uint32_t)((all + workers - 1) / workers), more = (share + kSizes - 1) / kSizes;
+  if (share <= 1 || q.r.n > kLanes || q.r.n * d.kv_heads > (int)workers / 2) return share > 1 ? share : 1;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int i = 0; i < kSizes; ++i) {
+    uint32_t x = (uint32_t)ceilf((float)mine * __builtin_amdgcn_rcpf((float)(share + i * more)));
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
+    if (lane == i) sh.sizes[wave][i] = x;
+  }
+  __syncthreads();
+  uint32_t got = share + kSizes * more;
+  for (int i = kSizes - 1; i >= 0; --i) {
+    uint32_t x = 0;
+    for (int w = 0; w < kWaves; ++w) x += sh.sizes[w][i];
+    if (x * (uint32_t)d.kv_heads <= workers) got = share + i * more;
+  }
+  return got;
 }
-
-struct Run {  // steps [sa, sb) of an item's head
-  Span sp;
-  int item, head, sa, sb;
-  uint32_t first_unit;  // the number of its step 0
-};
 
 typedef const __attribute__((address_space(4))) int32_t *ScalarInts;
 
-// The copies of a wavefront's blocks into its ring: block n of the run goes to slot n % kAhead.
+// The copies of a wavefront's blocks into its ring: its n-th block goes to slot n % kAhead.
 template <int D>
 struct Copies {
   static constexpr int kCopies = (40 * D + 1023) / 1024;  // loads of a block
   ScalarInts table;
-  int head, tok, to;   // next block's first token; end of the run's tokens
+  int head, tok, to;   // next block's first token; end of the piece's tokens
   uint32_t ring, slot;
   uint32_t page;       // of the next block
 
   // (pages are looked up by scalar loads, a block ahead: a vector load would wait for all copies under way)
   __device__ __forceinline__ void look(const CacheDev &d) {
     if (tok < to) page = (uint32_t)table[cache_page_of(d, (uint32_t)tok / kBlockTokens)];
-  }
-  __device__ __forceinline__ void begin(const CacheDev &d, const Run &r, int wave, uint32_t ring_at) {
-    table = (ScalarInts)(uintptr_t)(d.table + (int64_t)r.sp.seq * d.max_pages);
-    head = r.head;
-    tok = r.sp.low + r.sa * kStep + wave * kBlockTokens;
-    to = min(r.sp.low + r.sb * kStep, r.sp.length);
-    ring = ring_at;
-    slot = 0;
-    look(d);
   }
   __device__ __forceinline__ void one(const CacheDev &d, int layer, int lane) {
     if (tok >= to) return;
@@ -134,14 +150,59 @@ struct Copies {
   }
 };
 
-// The copies of the run's first blocks are under way; those of `next`, if there is one, are when it returns.
 template <int D, int NR>
-__device__ void attend_run(const CacheDev &d, const CacheQuery &q, const Run &run, bool more, const Run &next, uint32_t all, uint32_t workers, uint32_t worker, Copies<D> &cp,
-                           Shared<D, NR> &sh) {
+__global__ __launch_bounds__(kLanes, at_once(D, NR)) void k_cache_attend(CacheDev d, CacheQuery q) {
   constexpr int NJ = D / 32, NT = D / 16;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, b = lane >> 4;
-  const Span &sp = run.sp;
-  const int rows = q.share * sp.count, head = run.head;
+  extern __shared__ uint4 lds[];
+  Shared<D, NR> &sh = *reinterpret_cast<Shared<D, NR> *>(lds);
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 15, b = lane >> 4;
+
+  // Which piece is this workgroup's: the items' steps, the size of a piece, and the pieces of the items in front.
+  Piece pc;
+  {
+    uint64_t all = 0, before;
+    uint32_t mine = 0;
+    for (int base = 0; base < q.r.n; base += kLanes) {
+      mine = (uint32_t)find_span(d, q, base + threadIdx.x, blockIdx.x == 0).steps;
+      all += scan_lanes(mine, &before, sh);
+    }
+    all *= (uint64_t)d.kv_heads;
+    const uint32_t size = piece_steps(d, q, mine, all, kUnits * at_once(D, NR), sh);
+    uint64_t at = 0;
+    bool found = false;
+    for (int base = 0; base < q.r.n && !found; base += kLanes) {
+      if (q.r.n > kLanes) mine = (uint32_t)find_span(d, q, base + threadIdx.x, false).steps;
+      const uint32_t parts = (mine + size - 1) / size, pieces = parts * (uint32_t)d.kv_heads;
+      // (low half: pieces; high half: those that are parts of a row)
+      const uint64_t sum = scan_lanes(pieces | (uint64_t)(parts > 1 ? pieces : 0) << 32, &before, sh);
+      const uint32_t first = (uint32_t)at + (uint32_t)before;
+      if (blockIdx.x - first < pieces) {
+        const uint32_t x = blockIdx.x - first, head = x / parts, nth = x % parts;
+        sh.piece = Piece{base + (int)threadIdx.x, (int)head, (int)((uint64_t)mine * nth / parts), (int)((uint64_t)mine * (nth + 1) / parts), (int)parts, (int)nth,
+                         (int)((uint32_t)(at >> 32) + (uint32_t)(before >> 32) + head * parts)};
+      }
+      at += sum;
+      found = blockIdx.x < (uint32_t)at;
+    }
+    if (!found) return;
+    __syncthreads();
+    pc = sh.piece;
+    pc = Piece{uniform(pc.item), uniform(pc.head), uniform(pc.sa), uniform(pc.sb), uniform(pc.parts), uniform(pc.nth), uniform(pc.part)};
+  }
+  Span sp = find_span(d, q, pc.item, false);
+  sp = Span{uniform(sp.seq), uniform(sp.count), uniform(sp.length), uniform(sp.low), uniform(sp.steps),
+            (int64_t)uniform((int)((uint64_t)sp.row0 >> 32)) << 32 | (uint32_t)uniform((int)sp.row0)};
+  const int rows = q.share * sp.count, head = pc.head, first_tok = sp.low + pc.sa * kStep + wave * kBlockTokens;
+  Copies<D> cp;
+  cp.table = (ScalarInts)(uintptr_t)(d.table + (int64_t)sp.seq * d.max_pages);
+  cp.head = head;
+  cp.tok = first_tok;
+  cp.to = min(sp.low + pc.sb * kStep, sp.length);
+  cp.ring = (uint32_t)uniform((int)lds_address(sh.ring[wave][0]));
+  cp.slot = 0;
+  cp.look(d);
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) cp.one(d, q.layer, lane);
 
   half8 qf[NR][NJ];
   int see_to[NR], see_from[NR];
@@ -171,7 +232,7 @@ __device__ void attend_run(const CacheDev &d, const CacheQuery &q, const Run &ru
   }
   const int to = cp.to;
   uint32_t slot = 0;
-  for (int tok0 = sp.low + run.sa * kStep + wave * kBlockTokens; tok0 < to; tok0 += kStep) {
+  for (int tok0 = first_tok; tok0 < to; tok0 += kStep) {
     static_assert(kAhead == 2, "one block behind this one");
     if (tok0 + kStep < to) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Copies<D>::kCopies) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -240,10 +301,6 @@ __device__ void attend_run(const CacheDev &d, const CacheQuery &q, const Run &ru
       for (int t = 0; t < NR; ++t) o[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pf[t], o[t][n], 0, 0, 0);
     }
   }
-  if (more) {  // (this wavefront has read its ring)
-    cp.begin(d, next, wave, cp.ring);
-    for (int i = 0; i < kAhead; ++i) cp.one(d, q.layer, lane);
-  }
 
   // The wavefronts' parts of each row.
 #pragma unroll
@@ -255,129 +312,72 @@ __device__ void attend_run(const CacheDev &d, const CacheQuery &q, const Run &ru
       sh.ml[wave][t * 16 + col][1] = l[t];
     }
   }
-  __syncthreads();
-  const bool whole = run.sa == 0 && run.sb == sp.steps;
-  const uint32_t slot_at = worker * 2 + (run.sa == 0 ? 1 : 0);
+  __syncthreads();  // (and the rings are read)
+  float *part = d.part + (int64_t)(pc.part + pc.nth) * (16 * NR) * D, *part_ml = d.part_ml + (int64_t)(pc.part + pc.nth) * (16 * NR) * 2;
 #pragma unroll
   for (int t = 0; t < NR; ++t) {
     float most = -INFINITY;
     for (int w = 0; w < kWaves; ++w) most = fmaxf(most, sh.ml[w][t * 16 + col][0]);
     const float by = m[t] == -INFINITY && most == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[t] - most);
+    if (t * 16 + col < rows)
 #pragma unroll
-    for (int c0 = 0; c0 < D; c0 += kJoin) {
-#pragma unroll
-      for (int n = 0; n < kJoin / 16; ++n) *reinterpret_cast<f32x4 *>(&sh.o[wave][col][n * 16 + b * 4]) = o[t][c0 / 16 + n] * by;
-      __syncthreads();
-      if (threadIdx.x < 16 * (kJoin / 4)) {
-        const int r = threadIdx.x / (kJoin / 4), c = threadIdx.x % (kJoin / 4) * 4, row = t * 16 + r;
-        if (row < rows) {
-          float top = -INFINITY, sum = 0.0f;
-          for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sh.ml[w][row][0]);
-          f32x4 v{0, 0, 0, 0};
-          for (int w = 0; w < kWaves; ++w) {
-            const float mw = sh.ml[w][row][0];
-            sum += sh.ml[w][row][1] * (mw == -INFINITY && top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(mw - top));
-            v += *reinterpret_cast<const f32x4 *>(&sh.o[w][r][c]);
-          }
-          if (whole) {
-            store_row(q, sp.row0 + row / q.share, head * q.share + row % q.share, c0 + c, v, top, sum);
-          } else {
-            float *part = d.part + ((int64_t)slot_at * (16 * NR) + row) * D + c0 + c;
-            put_pair(part, v[0], v[1]);
-            put_pair(part + 2, v[2], v[3]);
-            if (c0 + c == 0) put_pair(d.part_ml + ((int64_t)slot_at * (16 * NR) + row) * 2, top, sum);
-          }
-        }
+      for (int n = 0; n < NT; ++n) *reinterpret_cast<f32x4 *>(&sh.o[wave][col][n * 16 + b * 4]) = o[t][n] * by;
+    __syncthreads();
+    for (int u = threadIdx.x; u < min(16, rows - t * 16) * (D / 4); u += kLanes) {
+      const int r = u / (D / 4), c = u % (D / 4) * 4, row = t * 16 + r;
+      float top = -INFINITY, sum = 0.0f;
+      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sh.ml[w][row][0]);
+      f32x4 v{0, 0, 0, 0};
+      for (int w = 0; w < kWaves; ++w) {
+        const float mw = sh.ml[w][row][0];
+        sum += sh.ml[w][row][1] * (mw == -INFINITY && top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(mw - top));
+        v += *reinterpret_cast<const f32x4 *>(&sh.o[w][r][c]);
       }
-      __syncthreads();
+      if (pc.parts == 1) {
+        store_row(q, sp.row0 + row / q.share, head * q.share + row % q.share, c, v, top, sum);
+      } else {
+        put_pair(part + row * D + c, v[0], v[1]);
+        put_pair(part + row * D + c + 2, v[2], v[3]);
+        if (c == 0) put_pair(part_ml + row * 2, top, sum);
+      }
     }
+    if (t + 1 < NR) __syncthreads();
   }
-  if (whole) return;
-  const uint32_t w0 = worker_of(run.first_unit, all, workers), w1 = worker_of(run.first_unit + sp.steps - 1, all, workers);
+  if (pc.parts == 1) return;
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wavefront's part is out ...
   __syncthreads();                                  // ... and that of the others
   if (threadIdx.x == 0) {
-    uint32_t *there = d.arrived + (int64_t)run.item * d.kv_heads + head;
-    const bool last = __hip_atomic_fetch_add(there, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == w1 - w0;
+    uint32_t *there = d.arrived + (int64_t)pc.item * d.kv_heads + head;
+    const bool last = __hip_atomic_fetch_add(there, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)pc.parts - 1;
     if (last) __hip_atomic_store(there, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     sh.last = last;
   }
   __syncthreads();
-  if (sh.last) {
-    // (slot 2 w + 1 has what worker w began and did not end, slot 2 w what it found begun)
-    for (int u = threadIdx.x; u < rows * (D / 4); u += kLanes) {
-      const int row = u / (D / 4), c = u % (D / 4) * 4;
-      const int64_t at = (int64_t)(w0 * 2 + 1) * (16 * NR) + row;
-      join_parts(q, sp.row0 + row / q.share, head * q.share + row % q.share, c, (int)(w1 - w0 + 1), d.part + at * D + c, d.part_ml + at * 2,
-                 D, 16 * NR, 32 * NR);
-    }
+  if (!sh.last) return;
+  part = d.part + (int64_t)pc.part * (16 * NR) * D;
+  part_ml = d.part_ml + (int64_t)pc.part * (16 * NR) * 2;
+  for (int u = threadIdx.x; u < rows * (D / 4); u += kLanes) {
+    const int row = u / (D / 4), c = u % (D / 4) * 4;
+    join_parts(q, sp.row0 + row / q.share, head * q.share + row % q.share, c, pc.parts, part + row * D + c, part_ml + row * 2, D, 16 * NR);
   }
-  __syncthreads();
 }
 
+// (an even share makes no more pieces than run at once, and one more for each head)
 template <int D, int NR>
-__global__ __launch_bounds__(kLanes, NR == 1 && D <= 128 ? 3 : 1) void k_cache_attend(CacheDev d, CacheQuery q) {
-  extern __shared__ uint4 lds[];
-  Shared<D, NR> &sh = *reinterpret_cast<Shared<D, NR> *>(lds);
-  const bool tell = blockIdx.x == 0;
-  uint32_t all = 0;
-  for (int base = 0; base < q.r.n; base += kScan) all = number_steps<D, NR>(d, q, base, all, sh, tell);
-  if (all == 0) return;
-  const uint32_t workers = all < gridDim.x ? all : gridDim.x, worker = blockIdx.x;
-  if (worker >= workers) return;
-  uint32_t u = (uint32_t)((uint64_t)all * worker / workers);
-  const uint32_t end = (uint32_t)((uint64_t)all * (worker + 1) / workers);
-  int base = 0;
-  if (q.r.n > kScan) {
-    uint32_t at = number_steps<D, NR>(d, q, 0, 0, sh, false);
-    while (at <= u) at = number_steps<D, NR>(d, q, base += kScan, at, sh, false);
-  }
-  // The run that step u begins or goes on with; u moves behind it.
-  const auto find_run = [&]() {
-    while (u >= sh.before[kScan]) number_steps<D, NR>(d, q, base += kScan, sh.before[kScan], sh, false);
-    int lo = 0, hi = kScan - 1;  // the last item whose steps begin at u or before
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) / 2;
-      if (sh.before[mid] <= u) lo = mid;
-      else hi = mid - 1;
-    }
-    Run r;
-    r.item = base + lo;
-    r.sp = find_span(d, q, r.item, false);
-    const uint32_t within = u - sh.before[lo], steps = (uint32_t)r.sp.steps, take = min(end - u, steps - within % steps);
-    r.head = (int)(within / steps);
-    r.sa = (int)(within % steps);
-    r.sb = r.sa + (int)take;
-    r.first_unit = u - (uint32_t)r.sa;
-    u += take;
-    r.sp.row0 = (int64_t)uniform((int)((uint64_t)r.sp.row0 >> 32)) << 32 | (uint32_t)uniform((int)r.sp.row0);
-    r.sp = Span{uniform(r.sp.seq), uniform(r.sp.count), uniform(r.sp.length), uniform(r.sp.low), uniform(r.sp.steps), r.sp.row0};
-    return Run{r.sp, uniform(r.item), uniform(r.head), uniform(r.sa), uniform(r.sb), (uint32_t)uniform((int)r.first_unit)};
-  };
-  Run run = find_run();
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  Copies<D> cp;
-  cp.begin(d, run, wave, (uint32_t)uniform((int)lds_address(sh.ring[wave][0])));
-  for (int i = 0; i < kAhead; ++i) cp.one(d, q.layer, lane);
-  for (;;) {
-    const bool more = u < end;
-    const Run next = more ? find_run() : run;
-    attend_run<D, NR>(d, q, run, more, next, all, workers, worker, cp, sh);
-    if (!more) return;
-    run = next;
-  }
+void launch(const CacheDev &d, const CacheQuery &q, hipStream_t s) {
+  k_cache_attend<D, NR><<<(uint32_t)(kUnits * at_once(D, NR) + q.r.n * d.kv_heads), kLanes, sizeof(Shared<D, NR>), s>>>(d, q);
 }
 
 }  // namespace
 
-size_t cache_part_floats(int head_dim) {
-  const size_t few = (size_t)kWorkers * 2 * 32 * head_dim, many = cache_prompt_part_floats(head_dim);
+// Rows of parts: of the pieces that are parts there are at most two for each that runs at once, a long head's last being short.
+static size_t part_rows(int head_dim) {
+  const size_t few = (size_t)kUnits * 2 * (head_dim == 256 ? 16 * at_once(256, 1) : head_dim == 128 ? 32 * at_once(128, 2) : head_dim == 96 ? 32 * at_once(96, 2) : 32 * at_once(64, 2));
+  const size_t many = cache_prompt_part_rows();
   return few > many ? few : many;
 }
-size_t cache_part_ml_floats(int) {
-  const size_t few = (size_t)kWorkers * 2 * 32 * 2, many = cache_prompt_part_ml_floats();
-  return few > many ? few : many;
-}
+size_t cache_part_floats(int head_dim) { return part_rows(head_dim) * head_dim; }
+size_t cache_part_ml_floats(int head_dim) { return part_rows(head_dim) * 2; }
 size_t cache_arrived_words(int max_seqs, int kv_heads) {
   const size_t few = (size_t)max_seqs * kv_heads, many = cache_prompt_groups();
   return few > many ? few : many;
@@ -385,13 +385,12 @@ size_t cache_arrived_words(int max_seqs, int kv_heads) {
 
 void launch_cache_attend(const CacheDev &d, const CacheQuery &q, hipStream_t s) {
   const int64_t rows = (int64_t)q.share * q.r.max_new;
-  const auto go = [&](auto kernel, size_t lds) { kernel<<<kWorkers, kLanes, lds, s>>>(d, q); };
   if (rows > (d.head_dim == 256 ? 16 : 32)) return launch_cache_prompt(d, q, s);
   switch (d.head_dim) {
-    case 64: return rows <= 16 ? go(k_cache_attend<64, 1>, sizeof(Shared<64, 1>)) : go(k_cache_attend<64, 2>, sizeof(Shared<64, 2>));
-    case 96: return rows <= 16 ? go(k_cache_attend<96, 1>, sizeof(Shared<96, 1>)) : go(k_cache_attend<96, 2>, sizeof(Shared<96, 2>));
-    case 128: return rows <= 16 ? go(k_cache_attend<128, 1>, sizeof(Shared<128, 1>)) : go(k_cache_attend<128, 2>, sizeof(Shared<128, 2>));
-    default: return go(k_cache_attend<256, 1>, sizeof(Shared<256, 1>));
+    case 64: return rows <= 16 ? launch<64, 1>(d, q, s) : launch<64, 2>(d, q, s);
+    case 96: return rows <= 16 ? launch<96, 1>(d, q, s) : launch<96, 2>(d, q, s);
+    case 128: return rows <= 16 ? launch<128, 1>(d, q, s) : launch<128, 2>(d, q, s);
+    default: return launch<256, 1>(d, q, s);
   }
 }
 

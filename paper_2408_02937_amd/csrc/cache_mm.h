@@ -187,15 +187,16 @@ __device__ inline float2 get_pair(const float *p) {
   return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
 }
 
-// Channels c .. c + 3 of a row of n parts, joined in order.  Part 0 is at part and ml (its maximum and sum); the next is `gap` rows on, every
-// further one `stride` rows.
-__device__ inline void join_parts(const CacheQuery &q, int64_t row, int head, int c, int n, const float *part, const float *ml, int head_dim, int gap, int stride) {
-  const auto at = [&](int i) { return i ? (int64_t)gap + (int64_t)(i - 1) * stride : 0; };
+// Channels c .. c + 3 of a row of n parts, `stride` rows apart, joined in order.
+__device__ inline void join_parts(const CacheQuery &q, int64_t row, int head, int c, int n, const float *part, const float *ml, int head_dim, int stride) {
   float top = -INFINITY, sum = 0.0f;
-  for (int i = 0; i < n; ++i) top = fmaxf(top, get_pair(ml + at(i) * 2).x);
+#pragma unroll 4
+  for (int i = 0; i < n; ++i) top = fmaxf(top, get_pair(ml + (int64_t)i * stride * 2).x);
   f32x4 v{0, 0, 0, 0};
+#pragma unroll 4
   for (int i = 0; i < n; ++i) {
-    const float2 x = get_pair(ml + at(i) * 2), a = get_pair(part + at(i) * head_dim), b = get_pair(part + at(i) * head_dim + 2);
+    const float *p = part + (int64_t)i * stride * head_dim;
+    const float2 x = get_pair(ml + (int64_t)i * stride * 2), a = get_pair(p), b = get_pair(p + 2);
     const float by = x.x == -INFINITY && top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(x.x - top);
     sum += x.y * by;
     v += f32x4{a.x, a.y, b.x, b.y} * by;

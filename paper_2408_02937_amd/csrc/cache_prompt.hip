@@ -280,7 +280,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_cache_prompt(CacheDev d, CacheQu
   ml = d.part_ml + group * splits * kRows * 2;
   for (int u = threadIdx.x; u < min(rows, kRows) * (D / 4); u += kLanes) {
     const int r = u / (D / 4), c = u % (D / 4) * 4, i = tile * kRows + r;
-    join_parts(q, row0 + i / q.share, head * q.share + i % q.share, c, parts, part + r * D + c, ml + r * 2, D, kRows, kRows);
+    join_parts(q, row0 + i / q.share, head * q.share + i % q.share, c, parts, part + r * D + c, ml + r * 2, D, kRows);
   }
 }
 
@@ -295,8 +295,7 @@ void launch(const CacheDev &d, const CacheQuery &q, hipStream_t s) {
 
 }  // namespace
 
-size_t cache_prompt_part_floats(int head_dim) { return (size_t)kParts * 256 * head_dim; }
-size_t cache_prompt_part_ml_floats() { return (size_t)kParts * 256 * 2; }
+size_t cache_prompt_part_rows() { return (size_t)kParts * 256; }
 size_t cache_prompt_groups() { return kParts; }
 
 void launch_cache_prompt(const CacheDev &d, const CacheQuery &q, hipStream_t s) {
