@@ -15,13 +15,17 @@ the stream given (the current one unless told), there is no fallback.
 from __future__ import annotations
 
 import ctypes as C
+import struct
 from typing import Optional, Tuple
 
 import torch
 
 from paper_2408_02937_amd import rtams
-from paper_2408_02937_amd.rtams import CacheConfig, CacheQuery, CacheView, _chk, _device_bytes, _stream_ptr, lib
+from paper_2408_02937_amd.rtams import CacheConfig, CacheQuery, CacheView, _chk, _device_bytes, lib
 
+_query = struct.Struct("@iiiiiifPqqPqqP").pack  # CacheQuery, three times as fast as its fields one by one
+assert struct.calcsize("@iiiiiifPqqPqqP") == C.sizeof(CacheQuery)
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 _TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 
 
@@ -35,6 +39,7 @@ class Cache:
         L = lib()
         self.kv_heads, self.head_dim, self.layers, self.page_tokens, self.max_seqs = kv_heads, head_dim, layers, page_tokens, max_seqs
         self.device = torch.device(device)
+        self.device = torch.device(self.device.type, torch.cuda.current_device() if self.device.index is None else self.device.index)
         if pages is None and pool_bytes is None:
             raise ValueError("give pages or pool_bytes")
         if max_pages is None:
@@ -54,7 +59,7 @@ class Cache:
         h = C.c_void_p()
         torch.cuda.synchronize(self.device)
         _chk(L.rtams_cache_create(C.byref(cfg), C.byref(h)), "rtams_cache_create")
-        self._h = h
+        self._h, self._lib = h, L
         v = CacheView()
         _chk(L.rtams_cache_layout(h, C.byref(v)), "rtams_cache_layout")
         base = self.pool.data_ptr()
@@ -84,6 +89,9 @@ class Cache:
             pass
 
     # ---- arguments
+    def _stream(self, stream) -> int:
+        return _current_stream(self.device.index) if stream is None else stream.cuda_stream
+
     def _ints(self, t: Optional[torch.Tensor], what: str, n: Optional[int] = None) -> Optional[int]:
         if t is None:
             return None
@@ -114,7 +122,7 @@ class Cache:
     def extend(self, seqs: Optional[torch.Tensor] = None, starts: Optional[torch.Tensor] = None, n: Optional[int] = None, stream=None) -> None:
         """Room for the items' rows (one each without starts) at the ends of their sequences."""
         n, sp, tp, _ = self._items(seqs, starts, n, 1)
-        _chk(lib().rtams_cache_extend(self._h, n, sp, tp, _stream_ptr(stream)), "rtams_cache_extend")
+        _chk(self._lib.rtams_cache_extend(self._h, n, sp, tp, self._stream(stream)), "rtams_cache_extend")
 
     def write(self, layer: int, k: torch.Tensor, v: torch.Tensor, seqs: Optional[torch.Tensor] = None, starts: Optional[torch.Tensor] = None,
               max_new: Optional[int] = None, stream=None) -> None:
@@ -124,8 +132,8 @@ class Cache:
             raise ValueError("k and v must have the same shape, type and strides")
         rows = k.shape[0]
         n, sp, tp, max_new = self._items(seqs, starts, rows if seqs is None and starts is None else None, max_new)
-        _chk(lib().rtams_cache_write(self._h, layer, n, sp, tp, rows, max_new, k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1),
-                                     _TYPES[k.dtype], _stream_ptr(stream)), "rtams_cache_write")
+        _chk(self._lib.rtams_cache_write(self._h, layer, n, sp, tp, rows, max_new, k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1),
+                                     _TYPES[k.dtype], self._stream(stream)), "rtams_cache_write")
 
     def read(self, layer: int, rows: int, seqs: Optional[torch.Tensor] = None, starts: Optional[torch.Tensor] = None,
              max_new: Optional[int] = None, dtype: torch.dtype = torch.float32, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
@@ -135,7 +143,7 @@ class Cache:
         n, sp, tp, max_new = self._items(seqs, starts, rows if seqs is None and starts is None else None, max_new)
         k = torch.empty((rows, self.kv_heads, self.head_dim), dtype=dtype, device=self.device)
         v = torch.empty_like(k)
-        _chk(lib().rtams_cache_read(self._h, layer, n, sp, tp, rows, max_new, k.data_ptr(), v.data_ptr(), _TYPES[dtype], _stream_ptr(stream)),
+        _chk(self._lib.rtams_cache_read(self._h, layer, n, sp, tp, rows, max_new, k.data_ptr(), v.data_ptr(), _TYPES[dtype], self._stream(stream)),
              "rtams_cache_read")
         return k, v
 
@@ -148,7 +156,7 @@ class Cache:
         rows, heads = q.shape[0], q.shape[1]
         n, sp, tp, max_new = self._items(seqs, starts, rows if seqs is None and starts is None else None, max_new)
         if out is None:
-            out = torch.empty((rows, heads, self.head_dim), dtype=q.dtype, device=q.device)
+            out = q.new_empty((rows, heads, self.head_dim))
         elif self._rows(out, heads, "out").shape != q.shape or out.dtype != q.dtype:
             raise ValueError("out must have the shape and type of q")
         lp = None
@@ -156,16 +164,16 @@ class Cache:
             if not (lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (rows, heads) and lse.device == self.device):
                 raise ValueError("lse must be a contiguous float32 tensor [rows][heads]")
             lp = lse.data_ptr()
-        cq = CacheQuery(layer, heads, _TYPES[q.dtype], int(causal), window, max_new, self.head_dim ** -0.5 if scale is None else scale,
-                        q.data_ptr(), q.stride(0), q.stride(1), out.data_ptr(), out.stride(0), out.stride(1), lp)
-        _chk(lib().rtams_cache_attend(self._h, C.byref(cq), n, sp, tp, rows, _stream_ptr(stream)), "rtams_cache_attend")
+        cq = _query(layer, heads, _TYPES[q.dtype], int(causal), window, max_new, self.head_dim ** -0.5 if scale is None else scale,
+                        q.data_ptr(), q.stride(0), q.stride(1), out.data_ptr(), out.stride(0), out.stride(1), lp or 0)
+        _chk(self._lib.rtams_cache_attend(self._h, cq, n, sp, tp, rows, self._stream(stream)), "rtams_cache_attend")
         return out
 
     # ---- pages
     def fork(self, src: torch.Tensor, dst: torch.Tensor, copy: bool = False, stream=None) -> None:
         """Empty sequences dst become what src are, sharing pages until they grow, or (copy) in pages of their own."""
         n = src.shape[0]
-        _chk(lib().rtams_cache_fork(self._h, n, self._ints(src, "src"), self._ints(dst, "dst", n), int(copy), _stream_ptr(stream)), "rtams_cache_fork")
+        _chk(self._lib.rtams_cache_fork(self._h, n, self._ints(src, "src"), self._ints(dst, "dst", n), int(copy), self._stream(stream)), "rtams_cache_fork")
 
     def trim(self, seqs: Optional[torch.Tensor] = None, lengths: Optional[torch.Tensor] = None, n: Optional[int] = None, stream=None) -> None:
         """Cuts sequences down to `lengths` tokens (without: to none)."""
@@ -173,21 +181,21 @@ class Cache:
             n = seqs.shape[0] if seqs is not None else lengths.shape[0] if lengths is not None else None
         if n is None:
             raise ValueError("give seqs, lengths or n")
-        _chk(lib().rtams_cache_trim(self._h, n, self._ints(seqs, "seqs", n), self._ints(lengths, "lengths", n), _stream_ptr(stream)), "rtams_cache_trim")
+        _chk(self._lib.rtams_cache_trim(self._h, n, self._ints(seqs, "seqs", n), self._ints(lengths, "lengths", n), self._stream(stream)), "rtams_cache_trim")
 
     def compact(self, stream=None) -> None:
         """Moves the pages in use to the front of the pool."""
-        _chk(lib().rtams_cache_compact(self._h, _stream_ptr(stream)), "rtams_cache_compact")
+        _chk(self._lib.rtams_cache_compact(self._h, self._stream(stream)), "rtams_cache_compact")
 
     # ---- introspection
     @property
     def free_pages(self) -> int:
         v = C.c_int64()
-        _chk(lib().rtams_cache_free_pages(self._h, C.byref(v)), "rtams_cache_free_pages")
+        _chk(self._lib.rtams_cache_free_pages(self._h, C.byref(v)), "rtams_cache_free_pages")
         return v.value
 
     def poll_error(self) -> int:
-        return lib().rtams_cache_poll_error(self._h)
+        return self._lib.rtams_cache_poll_error(self._h)
 
     def clear_error(self) -> None:
-        _chk(lib().rtams_cache_clear_error(self._h), "rtams_cache_clear_error")
+        _chk(self._lib.rtams_cache_clear_error(self._h), "rtams_cache_clear_error")

@@ -19,7 +19,6 @@ namespace {
 
 constexpr int kLanes = 256, kWaves = 4, kStep = kWaves * kBlockTokens;
 constexpr int kUnits = 256;      // compute units
-constexpr int kSizes = 16;       // sizes of pieces that are tried
 
 // Workgroups that a compute unit runs at once: registers decide, and from 128 channels on LDS.
 constexpr int at_once(int head_dim, int tiles) {
@@ -55,71 +54,115 @@ __device__ inline Span find_span(const CacheDev &d, const CacheQuery &q, int i, 
 constexpr int kAhead = 2;   // blocks of a wavefront that are in LDS or on their way
 
 struct Piece {  // steps [sa, sb) of an item's head
+  Span sp;
   int item, head, sa, sb;
   int parts, nth;  // pieces of the head; which one this is
   int part;        // where the head's parts begin, if there are several
 };
+
+constexpr int kEach = 4, kRound = 64 * kEach;  // items that a lane of the planning wavefront has, and all of them
 
 template <int D, int NR>
 struct alignas(16) Shared {
   union {
     unsigned char ring[kWaves][kAhead][40 * D];
     float o[kWaves][16][D + 4];  // when the rings are read: the wavefronts' parts of 16 rows
+    float steps[kRound];         // in front of it all
   };
   float ml[kWaves][16 * NR][2];
-  uint64_t waves[kWaves];
-  uint32_t sizes[kWaves][kSizes];
   Piece piece;
   int last;
 };
 
 __device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-// The sum over the workgroup and, in *before, over the lanes in front.
-template <class S>
-__device__ uint64_t scan_lanes(uint64_t v, uint64_t *before, S &sh) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint64_t inc = v;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint64_t x = __shfl_up(inc, o);
-    if (lane >= o) inc += x;
-  }
-  __syncthreads();
-  if (lane == 63) sh.waves[wave] = inc;
-  __syncthreads();
-  uint64_t lower = 0, all = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    lower += w < wave ? sh.waves[w] : 0;
-    all += sh.waves[w];
-  }
-  *before = lower + inc - v;
-  return all;
+// a / b rounded up, a below 2^24
+__device__ inline uint32_t div_up(uint32_t a, uint32_t b, float one_over_b) {
+  uint32_t q = (uint32_t)((float)a * one_over_b), r = a - q * b;  // off by one at most
+  if ((int32_t)r < 0) { --q; r += b; }
+  if (r >= b) { ++q; r -= b; }
+  return q + (r > 0);
 }
 
-// Steps of a piece, of `all` steps.  Pieces are to run all at once, so where items are few sixteen sizes from an even share up to twice that
-// are tried and the least is taken with which they do.  Where items are many, pieces are an even share at most, and long items do not keep the others waiting.
+// Steps of a piece, of `all` steps, for at most kRound items.  Pieces are to run all at once, so sixteen sizes from an even share up to
+// twice that are tried, a quarter of the items to a lane, and the least is taken with which they do.
+__device__ inline uint32_t piece_steps(const float *steps, int n, int kv_heads, uint32_t share, uint32_t workers) {
+  const int lane = threadIdx.x & 63;
+  const uint32_t more = (share + 15) / 16, size = share + (lane & 15) * more;
+  const float one_over = __builtin_amdgcn_rcpf((float)size);
+  float pieces = 0.0f;
+  for (int i = (lane >> 4) * 4; i < n; i += 16) {
+    const f32x4 x = *reinterpret_cast<const f32x4 *>(steps + i) * one_over;  // (no steps behind the last item)
+    pieces += ceilf(x[0]) + ceilf(x[1]) + ceilf(x[2]) + ceilf(x[3]);
+  }
+  pieces += __shfl_xor(pieces, 16);
+  pieces += __shfl_xor(pieces, 32);
+  const uint64_t fits = __ballot(pieces * (float)kv_heads <= (float)workers) & 0xffff;
+  return fits ? share + (uint32_t)(__ffsll((unsigned long long)fits) - 1) * more : 2 * share;
+}
+
+// Which piece is workgroup blockIdx.x's: the items' steps, the size of a piece, and the pieces of the items in front.  One wavefront's work;
+// false where there is none left.
 template <class S>
-__device__ uint32_t piece_steps(const CacheDev &d, const CacheQuery &q, uint32_t mine, uint64_t all, uint32_t workers, S &sh) {
-  const uint32_t share = (uint32_t)((all + workers - 1) / workers), more = (share + kSizes - 1) / kSizes;
-  if (share <= 1 || q.r.n > kLanes || q.r.n * d.kv_heads > (int)workers / 2) return share > 1 ? share : 1;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+__device__ bool find_piece(const CacheDev &d, const CacheQuery &q, uint32_t workers, S &sh) {
+  const int lane = threadIdx.x & 63, n = q.r.n;
+  Span sp[kEach];
+  const auto look = [&](int base, bool tell) {
+    uint32_t sum = 0;
 #pragma unroll
-  for (int i = 0; i < kSizes; ++i) {
-    uint32_t x = (uint32_t)ceilf((float)mine * __builtin_amdgcn_rcpf((float)(share + i * more)));
+    for (int k = 0; k < kEach; ++k) {
+      sp[k] = find_span(d, q, base + lane * kEach + k, tell);
+      sum += (uint32_t)sp[k].steps;
+    }
+    return sum;
+  };
+  uint64_t all = 0;
+  for (int base = 0; base < n; base += kRound) all += last_lane(wave_running_sum((unsigned long long)look(base, blockIdx.x == 0)));
+  all *= (uint64_t)d.kv_heads;
+  // where items are many, pieces are an even share at most, and long items do not keep the others waiting
+  const uint32_t share = (uint32_t)((all + workers - 1) / workers);
+  uint32_t size = share > 1 ? share : 1;
+  if (share > 1 && n <= kRound && n * d.kv_heads <= (int)workers / 2) {
+    *reinterpret_cast<f32x4 *>(sh.steps + lane * kEach) = f32x4{(float)sp[0].steps, (float)sp[1].steps, (float)sp[2].steps, (float)sp[3].steps};
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    size = piece_steps(sh.steps, n, d.kv_heads, share, workers);
+  }
+  const float one_over = 1.0f / (float)size;
+  uint32_t before = 0, parts_before = 0;
+  for (int base = 0; base < n; base += kRound) {
+    if (n > kRound) look(base, false);
+    uint32_t parts[kEach], pieces = 0, shared = 0;
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
-    if (lane == i) sh.sizes[wave][i] = x;
+    for (int k = 0; k < kEach; ++k) {
+      parts[k] = div_up((uint32_t)sp[k].steps, size, one_over);
+      pieces += parts[k] * (uint32_t)d.kv_heads;
+      shared += parts[k] > 1 ? parts[k] * (uint32_t)d.kv_heads : 0;
+    }
+    const uint32_t upto = wave_running_sum(pieces), upto_shared = wave_running_sum(shared);
+    uint32_t first = before + upto - pieces, first_shared = parts_before + upto_shared - shared;
+    // (of this lane's items, the one that the workgroup's piece is of)
+    uint32_t x = ~0u, of = 0, at = 0;
+    Span mine{};
+    int item = 0;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const uint32_t here = parts[k] * (uint32_t)d.kv_heads;
+      if (blockIdx.x - first < here) {
+        x = blockIdx.x - first;
+        of = parts[k];
+        at = first_shared;
+        mine = sp[k];
+        item = base + lane * kEach + k;
+      }
+      first += here;
+      first_shared += parts[k] > 1 ? here : 0;
+    }
+    if (x != ~0u) sh.piece = Piece{mine, item, (int)(x / of), 0, 0, (int)of, (int)(x % of), (int)(at + x - x % of)};
+    if (__any(x != ~0u)) return true;
+    before += last_lane(upto);
+    parts_before += last_lane(upto_shared);
   }
-  __syncthreads();
-  uint32_t got = share + kSizes * more;
-  for (int i = kSizes - 1; i >= 0; --i) {
-    uint32_t x = 0;
-    for (int w = 0; w < kWaves; ++w) x += sh.sizes[w][i];
-    if (x * (uint32_t)d.kv_heads <= workers) got = share + i * more;
-  }
-  return got;
+  return false;
 }
 
 typedef const __attribute__((address_space(4))) int32_t *ScalarInts;
@@ -157,41 +200,21 @@ __global__ __launch_bounds__(kLanes, at_once(D, NR)) void k_cache_attend(CacheDe
   Shared<D, NR> &sh = *reinterpret_cast<Shared<D, NR> *>(lds);
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 15, b = lane >> 4;
 
-  // Which piece is this workgroup's: the items' steps, the size of a piece, and the pieces of the items in front.
-  Piece pc;
-  {
-    uint64_t all = 0, before;
-    uint32_t mine = 0;
-    for (int base = 0; base < q.r.n; base += kLanes) {
-      mine = (uint32_t)find_span(d, q, base + threadIdx.x, blockIdx.x == 0).steps;
-      all += scan_lanes(mine, &before, sh);
-    }
-    all *= (uint64_t)d.kv_heads;
-    const uint32_t size = piece_steps(d, q, mine, all, kUnits * at_once(D, NR), sh);
-    uint64_t at = 0;
-    bool found = false;
-    for (int base = 0; base < q.r.n && !found; base += kLanes) {
-      if (q.r.n > kLanes) mine = (uint32_t)find_span(d, q, base + threadIdx.x, false).steps;
-      const uint32_t parts = (mine + size - 1) / size, pieces = parts * (uint32_t)d.kv_heads;
-      // (low half: pieces; high half: those that are parts of a row)
-      const uint64_t sum = scan_lanes(pieces | (uint64_t)(parts > 1 ? pieces : 0) << 32, &before, sh);
-      const uint32_t first = (uint32_t)at + (uint32_t)before;
-      if (blockIdx.x - first < pieces) {
-        const uint32_t x = blockIdx.x - first, head = x / parts, nth = x % parts;
-        sh.piece = Piece{base + (int)threadIdx.x, (int)head, (int)((uint64_t)mine * nth / parts), (int)((uint64_t)mine * (nth + 1) / parts), (int)parts, (int)nth,
-                         (int)((uint32_t)(at >> 32) + (uint32_t)(before >> 32) + head * parts)};
-      }
-      at += sum;
-      found = blockIdx.x < (uint32_t)at;
-    }
-    if (!found) return;
-    __syncthreads();
-    pc = sh.piece;
-    pc = Piece{uniform(pc.item), uniform(pc.head), uniform(pc.sa), uniform(pc.sb), uniform(pc.parts), uniform(pc.nth), uniform(pc.part)};
+  if (wave == 0) {
+    const bool found = find_piece(d, q, kUnits * at_once(D, NR), sh);
+    if (lane == 0) sh.last = found;
   }
-  Span sp = find_span(d, q, pc.item, false);
-  sp = Span{uniform(sp.seq), uniform(sp.count), uniform(sp.length), uniform(sp.low), uniform(sp.steps),
-            (int64_t)uniform((int)((uint64_t)sp.row0 >> 32)) << 32 | (uint32_t)uniform((int)sp.row0)};
+  __syncthreads();
+  if (!sh.last) return;
+  Piece pc = sh.piece;
+  const Span sp{uniform(pc.sp.seq), uniform(pc.sp.count), uniform(pc.sp.length), uniform(pc.sp.low), uniform(pc.sp.steps),
+                (int64_t)uniform((int)((uint64_t)pc.sp.row0 >> 32)) << 32 | (uint32_t)uniform((int)pc.sp.row0)};
+  pc = Piece{sp, uniform(pc.item), uniform(pc.head), 0, 0, uniform(pc.parts), uniform(pc.nth), uniform(pc.part)};
+  {  // steps in as many equal pieces, the first ones one longer
+    const int each = sp.steps / pc.parts, longer = sp.steps - each * pc.parts;
+    pc.sa = each * pc.nth + min(pc.nth, longer);
+    pc.sb = pc.sa + each + (pc.nth < longer);
+  }
   const int rows = q.share * sp.count, head = pc.head, first_tok = sp.low + pc.sa * kStep + wave * kBlockTokens;
   Copies<D> cp;
   cp.table = (ScalarInts)(uintptr_t)(d.table + (int64_t)sp.seq * d.max_pages);

@@ -19,10 +19,13 @@ union HalfWords {
 __device__ inline HalfWords codes_of(uint32_t w) {
   HalfWords x;
   const uint32_t w8 = w >> 8;
-  x.w[0] = (w & 0x000f000fu) | 0x64006400u;
-  x.w[1] = (w & 0x00f000f0u) | 0x64006400u;
-  x.w[2] = (w8 & 0x000f000fu) | 0x64006400u;
-  x.w[3] = (w8 & 0x00f000f0u) | 0x64006400u;
+  // (in registers, where the compiler does not see them, so that and and or are one instruction, which takes no constants)
+  uint32_t low = 0x000f000fu, high = 0x00f000f0u, base = 0x64006400u;
+  asm("" : "+s"(low), "+s"(high), "+v"(base));
+  x.w[0] = (w & low) | base;
+  x.w[1] = (w & high) | base;
+  x.w[2] = (w8 & low) | base;
+  x.w[3] = (w8 & high) | base;
   const half2v k1024 = {(_Float16)1024.0f, (_Float16)1024.0f}, k16 = {(_Float16)0.0625f, (_Float16)0.0625f}, k64 = {(_Float16)-64.0f, (_Float16)-64.0f};
   x.p[0] = x.p[0] - k1024;
   x.p[1] = __builtin_elementwise_fma(x.p[1], k16, k64);
@@ -189,17 +192,32 @@ __device__ inline float2 get_pair(const float *p) {
 
 // Channels c .. c + 3 of a row of n parts, `stride` rows apart, joined in order.
 __device__ inline void join_parts(const CacheQuery &q, int64_t row, int head, int c, int n, const float *part, const float *ml, int head_dim, int stride) {
+  constexpr int kRun = 8;  // parts that are asked for at a time
   float top = -INFINITY, sum = 0.0f;
-#pragma unroll 4
-  for (int i = 0; i < n; ++i) top = fmaxf(top, get_pair(ml + (int64_t)i * stride * 2).x);
   f32x4 v{0, 0, 0, 0};
-#pragma unroll 4
-  for (int i = 0; i < n; ++i) {
-    const float *p = part + (int64_t)i * stride * head_dim;
-    const float2 x = get_pair(ml + (int64_t)i * stride * 2), a = get_pair(p), b = get_pair(p + 2);
-    const float by = x.x == -INFINITY && top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(x.x - top);
-    sum += x.y * by;
-    v += f32x4{a.x, a.y, b.x, b.y} * by;
+  for (int i0 = 0; i0 < n; i0 += kRun) {
+    float2 x[kRun], a[kRun], b[kRun];
+#pragma unroll
+    for (int k = 0; k < kRun; ++k) {
+      const int64_t i = min(i0 + k, n - 1) * (int64_t)stride;
+      x[k] = get_pair(ml + i * 2);
+      a[k] = get_pair(part + i * head_dim);
+      b[k] = get_pair(part + i * head_dim + 2);
+    }
+    float now = top;
+#pragma unroll
+    for (int k = 0; k < kRun; ++k) now = fmaxf(now, x[k].x);
+    const float shrink = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top - now);
+    sum *= shrink;
+    v *= shrink;
+    top = now;
+#pragma unroll
+    for (int k = 0; k < kRun; ++k)
+      if (i0 + k < n) {
+        const float by = x[k].x == -INFINITY && top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(x[k].x - top);
+        sum += x[k].y * by;
+        v += f32x4{a[k].x, a[k].y, b[k].x, b[k].y} * by;
+      }
   }
   store_row(q, row, head, c, v, top, sum);
 }

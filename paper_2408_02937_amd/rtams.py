@@ -145,7 +145,7 @@ def lib():
         L.rtams_cache_extend.argtypes = [vp, i64, vp, vp, vp]
         L.rtams_cache_write.argtypes = [vp, i32, i64, vp, vp, i64, i32, vp, vp, i64, i64, i32, vp]
         L.rtams_cache_read.argtypes = [vp, i32, i64, vp, vp, i64, i32, vp, vp, i32, vp]
-        L.rtams_cache_attend.argtypes = [vp, C.POINTER(CacheQuery), i64, vp, vp, i64, vp]
+        L.rtams_cache_attend.argtypes = [vp, vp, i64, vp, vp, i64, vp]  # (a packed CacheQuery)
         L.rtams_cache_fork.argtypes = [vp, i64, vp, vp, i32, vp]
         L.rtams_cache_trim.argtypes = [vp, i64, vp, vp, vp]
         L.rtams_cache_compact.argtypes = [vp, vp]
