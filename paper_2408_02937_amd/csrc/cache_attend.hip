@@ -74,33 +74,6 @@ struct alignas(16) Shared {
   int last;
 };
 
-__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-
-// a / b rounded up, a below 2^24
-__device__ inline uint32_t div_up(uint32_t a, uint32_t b, float one_over_b) {
-  uint32_t q = (uint32_t)((float)a * one_over_b), r = a - q * b;  // off by one at most
-  if ((int32_t)r < 0) { --q; r += b; }
-  if (r >= b) { ++q; r -= b; }
-  return q + (r > 0);
-}
-
-// Steps of a piece, of `all` steps, for at most kRound items.  Pieces are to run all at once, so sixteen sizes from an even share up to
-// twice that are tried, a quarter of the items to a lane, and the least is taken with which they do.
-__device__ inline uint32_t piece_steps(const float *steps, int n, int kv_heads, uint32_t share, uint32_t workers) {
-  const int lane = threadIdx.x & 63;
-  const uint32_t more = (share + 15) / 16, size = share + (lane & 15) * more;
-  const float one_over = __builtin_amdgcn_rcpf((float)size);
-  float pieces = 0.0f;
-  for (int i = (lane >> 4) * 4; i < n; i += 16) {
-    const f32x4 x = *reinterpret_cast<const f32x4 *>(steps + i) * one_over;  // (no steps behind the last item)
-    pieces += ceilf(x[0]) + ceilf(x[1]) + ceilf(x[2]) + ceilf(x[3]);
-  }
-  pieces += __shfl_xor(pieces, 16);
-  pieces += __shfl_xor(pieces, 32);
-  const uint64_t fits = __ballot(pieces * (float)kv_heads <= (float)workers) & 0xffff;
-  return fits ? share + (uint32_t)(__ffsll((unsigned long long)fits) - 1) * more : 2 * share;
-}
-
 // Which piece is workgroup blockIdx.x's: the items' steps, the size of a piece, and the pieces of the items in front.  One wavefront's work;
 // false where there is none left.
 template <class S>
@@ -400,7 +373,7 @@ static size_t part_rows(int head_dim) {
   return few > many ? few : many;
 }
 size_t cache_part_floats(int head_dim) { return part_rows(head_dim) * head_dim; }
-size_t cache_part_ml_floats(int head_dim) { return part_rows(head_dim) * 2; }
+size_t cache_part_ml_floats(int head_dim) { return part_rows(head_dim) * 4; }  // (of many rows two lanes have a pair each)
 size_t cache_arrived_words(int max_seqs, int kv_heads) {
   const size_t few = (size_t)max_seqs * kv_heads, many = cache_prompt_groups();
   return few > many ? few : many;
