@@ -124,7 +124,7 @@ struct CacheQuery {
   float *lse;
 };
 
-void launch_cache_extend(const CacheDev &d, const CacheRows &r, hipStream_t s);
+void launch_cache_extend(const CacheDev &d, const CacheRows &r, bool copies, hipStream_t s);  // copies: pages may be shared
 void launch_cache_fork(const CacheDev &d, int32_t n, const int32_t *src, const int32_t *dst, bool copy, hipStream_t s);
 void launch_cache_trim(const CacheDev &d, int32_t n, const int32_t *seqs, const int32_t *lengths, hipStream_t s);
 void launch_cache_compact(const CacheDev &d, hipStream_t s);

@@ -19,6 +19,7 @@ struct rtams_cache {
   hipStream_t stream = nullptr;  // of the last call
   bool have_stream = false;
   hipEvent_t done = nullptr;
+  bool forked = false;  // sequences may share pages
 };
 
 namespace {
@@ -91,9 +92,10 @@ __global__ void k_cache_clear_words(uint32_t *p, uint64_t n) {
 }
 
 // Orders the call behind the cache's work on another stream.  (Not a recorded call, which the graph orders.)
-int cache_enter(rtams_cache *c, hipStream_t s) {
+int cache_enter(rtams_cache *c, hipStream_t s, bool *recorded = nullptr) {
   hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
   if (hipStreamIsCapturing(s, &capture) != hipSuccess) (void)hipGetLastError();
+  if (recorded) *recorded = capture == hipStreamCaptureStatusActive;
   if (capture == hipStreamCaptureStatusActive) return RTAMS_OK;
   if (c->have_stream && c->stream != s) {
     HIP_TRY(hipEventRecord(c->done, c->stream));
@@ -248,9 +250,11 @@ int rtams_cache_extend(rtams_cache *c, int64_t n, const int32_t *d_seqs, const i
   if (rc || n == 0) return rc;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   std::lock_guard<std::mutex> g(c->mutex);
-  if ((rc = cache_enter(c, s))) return rc;
+  bool recorded = false;
+  if ((rc = cache_enter(c, s, &recorded))) return rc;
   CacheRows r = items_of(n, d_seqs, d_starts, 0x7fffffff, 0x7fffffff);
-  launch_cache_extend(c->dev, r, s);
+  // (without a fork before this call no page can be shared; a recorded call may be launched behind a later fork)
+  launch_cache_extend(c->dev, r, c->forked || recorded, s);
   return launched("extend");
 }
 
@@ -260,6 +264,8 @@ int rtams_cache_write(rtams_cache *c, int32_t layer, int64_t n, const int32_t *d
   if (!rc) rc = check_rows(c, layer, n, d_starts, rows, max_new);
   if (rc) return rc;
   if (type != RTAMS_TYPE_BF16 && type != RTAMS_TYPE_F16) return fail(RTAMS_EINVAL, "keys and values are bfloat16 or halves, got type %d", type);
+  if (row_stride < 0 || row_stride >= 1 << 24 || head_stride < 0 || head_stride >= 1 << 24)
+    return fail(RTAMS_EINVAL, "strides must be in 0..2^24 - 1 elements, got %lld and %lld", (long long)row_stride, (long long)head_stride);
   if (n == 0 || rows == 0) return RTAMS_OK;
   if (!d_k || !d_v) return fail(RTAMS_EINVAL, "keys or values are NULL");
   if (((uintptr_t)d_k | (uintptr_t)d_v) % 2) return fail(RTAMS_EINVAL, "keys and values must be 2-byte aligned");
@@ -332,6 +338,7 @@ int rtams_cache_fork(rtams_cache *c, int64_t n, const int32_t *d_src, const int3
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   std::lock_guard<std::mutex> g(c->mutex);
   if ((rc = cache_enter(c, s))) return rc;
+  c->forked |= copy == 0;
   launch_cache_fork(c->dev, (int32_t)n, d_src, d_dst, copy != 0, s);
   return launched("fork");
 }

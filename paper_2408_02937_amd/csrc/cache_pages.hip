@@ -7,6 +7,7 @@
 #include "../../include/rtams_cache.h"
 
 #include "cache.h"
+#include "rtams_dev.h"
 
 namespace rtams {
 
@@ -15,23 +16,30 @@ namespace {
 constexpr int kPlanLanes = 1024;
 constexpr int kCopyBytes = 16384;   // a workgroup's piece
 constexpr int kInlineSlots = 16384; // table entries that the planning workgroup walks by itself
+constexpr int kPicked = 2048;       // new pages that it keeps in LDS
 
 __device__ inline uint32_t lane_id() { return threadIdx.x & 63; }
 
+struct Plan {
+  uint32_t seen[kCacheMaxSeqs / 32];
+  uint32_t waves[kPlanLanes / 64];
+  int32_t picked[kPicked];
+  // of 1024 items: sequence, source of a fork, first page concerned, and how many entries the items in front concern
+  int32_t seq[kPlanLanes], src[kPlanLanes], page0[kPlanLanes];
+  uint32_t before[kPlanLanes + 1];
+  uint32_t pairs, freed;
+};
+
 // Exclusive prefix sum over the workgroup; *total to every lane.
-__device__ inline uint32_t scan_lanes(uint32_t v, uint32_t *total) {
-  __shared__ uint32_t waves[kPlanLanes / 64];
-  uint32_t inc = v;
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint32_t x = __shfl_up(inc, o);
-    if (lane_id() >= (uint32_t)o) inc += x;
-  }
+__device__ inline uint32_t scan_lanes(uint32_t v, uint32_t *total, Plan &sh) {
+  const uint32_t inc = wave_running_sum(v);
   __syncthreads();
-  if (lane_id() == 63) waves[threadIdx.x >> 6] = inc;
+  if (lane_id() == 63) sh.waves[threadIdx.x >> 6] = inc;
   __syncthreads();
   uint32_t before = 0, all = 0;
+#pragma unroll
   for (int w = 0; w < kPlanLanes / 64; ++w) {
-    const uint32_t x = waves[w];
+    const uint32_t x = sh.waves[w];
     before += w < (int)(threadIdx.x >> 6) ? x : 0;
     all += x;
   }
@@ -39,18 +47,19 @@ __device__ inline uint32_t scan_lanes(uint32_t v, uint32_t *total) {
   return before + inc - v;
 }
 
-// Takes the `total` lowest free pages, which there are, in order into picked.
-__device__ void pick_pages(const CacheDev &d, uint32_t total) {
+// Takes the `total` lowest free pages, which there are, in order: the first ones into LDS, the others into memory.
+__device__ void pick_pages(const CacheDev &d, uint32_t total, Plan &sh) {
   const uint32_t words = (d.pages + 31) / 32;
   uint32_t found = 0;
   for (uint32_t base = 0; base < words && found < total; base += kPlanLanes) {
     const uint32_t at = base + threadIdx.x;
     uint32_t w = at < words ? d.free_bits[at] : 0, here;
-    uint32_t rank = found + scan_lanes(__popc(w), &here);
+    uint32_t rank = found + scan_lanes(__popc(w), &here, sh);
     const uint32_t before = w;
     for (uint32_t x = w; x && rank < total; x &= x - 1, ++rank) {
       const int bit = __ffs(x) - 1;
-      d.picked[rank] = (int32_t)(at * 32 + bit);
+      if (rank < kPicked) sh.picked[rank] = (int32_t)(at * 32 + bit);
+      else d.picked[rank] = (int32_t)(at * 32 + bit);
       w &= ~(1u << bit);
     }
     if (w != before) d.free_bits[at] = w;
@@ -59,11 +68,19 @@ __device__ void pick_pages(const CacheDev &d, uint32_t total) {
   __syncthreads();
 }
 
+__device__ inline int32_t picked_page(const CacheDev &d, const Plan &sh, uint32_t rank) { return rank < kPicked ? sh.picked[rank] : d.picked[rank]; }
+
 __device__ inline void put_back(const CacheDev &d, int32_t page) { atomicOr(&d.free_bits[page >> 5], 1u << (page & 31)); }
 
 __device__ inline bool named_before(uint32_t *seen, int32_t seq) { return (atomicOr(&seen[seq >> 5], 1u << (seq & 31)) >> (seq & 31)) & 1; }
 
 __device__ inline int32_t pages_for(const CacheDev &d, int64_t tokens) { return (int32_t)((tokens + d.page_tokens - 1) / d.page_tokens); }
+
+__device__ inline void clear_seen(const CacheDev &d, Plan &sh) {
+  for (int i = threadIdx.x; i < (d.max_seqs + 31) / 32; i += kPlanLanes) sh.seen[i] = 0;
+  if (threadIdx.x == 0) sh.pairs = sh.freed = 0;
+  __syncthreads();
+}
 
 // The call is dropped.
 __device__ inline void drop(const CacheDev &d, int code) {
@@ -74,202 +91,235 @@ __device__ inline void drop(const CacheDev &d, int code) {
   }
 }
 
+// Entry e of the up to 1024 items in LDS: which of them it is.
+__device__ inline int item_of(const Plan &sh, uint32_t e) {
+  int lo = 0, hi = kPlanLanes - 1;
+  while (lo < hi) {  // the last one that begins at e or before
+    const int mid = (lo + hi + 1) / 2;
+    if (sh.before[mid] <= e) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
+
 __global__ __launch_bounds__(kPlanLanes) void k_cache_extend(CacheDev d, CacheRows r) {
-  __shared__ uint32_t seen[kCacheMaxSeqs / 32];
-  __shared__ int32_t big[kPlanLanes];
-  __shared__ uint32_t nbig, npairs, nfreed;
-  for (int i = threadIdx.x; i < (d.max_seqs + 31) / 32; i += kPlanLanes) seen[i] = 0;
-  if (threadIdx.x == 0) npairs = nfreed = 0;
-  __syncthreads();
+  __shared__ Plan sh;
+  clear_seen(d, sh);
   uint32_t total = 0;
   int bad = 0, short_of = 0;
+  CacheItem it{};
   for (int base = 0; base < r.n; base += kPlanLanes) {
     const int i = base + threadIdx.x;
     uint32_t need = 0;
-    CacheItem it{};
+    it = CacheItem{};
     if (i < r.n) {
       int64_t first;
       int count;
       const int s = cache_item_seq(r, i);
-      if (!cache_item_rows(r, i, &first, &count) || (uint32_t)s >= (uint32_t)d.max_seqs || named_before(seen, s) ||
-          (int64_t)d.lengths[s] + count > (int64_t)d.max_pages * d.page_tokens) {
+      const bool rows = cache_item_rows(r, i, &first, &count);
+      if (!rows || (uint32_t)s >= (uint32_t)d.max_seqs || named_before(sh.seen, s)) {
         bad = 1;
       } else {
         const int length = d.lengths[s];
-        it.seq = s;
-        it.src = length + count;
-        it.have = pages_for(d, length);
-        it.want = pages_for(d, (int64_t)length + count);
-        it.copy = count > 0 && length % d.page_tokens && d.refs[d.table[(int64_t)s * d.max_pages + it.have - 1]] > 1;
-        need = (uint32_t)(it.want - it.have + it.copy);
+        if ((int64_t)length + count > (int64_t)d.max_pages * d.page_tokens) {
+          bad = 1;
+        } else {
+          it.seq = s;
+          it.src = length + count;
+          it.have = pages_for(d, length);
+          it.want = pages_for(d, (int64_t)length + count);
+          it.copy = count > 0 && length % d.page_tokens && d.refs[d.table[(int64_t)s * d.max_pages + it.have - 1]] > 1;
+          need = (uint32_t)(it.want - it.have + it.copy);
+        }
       }
     }
     uint32_t here;
-    it.off = total + scan_lanes(need, &here);
-    if (i < r.n) d.items[i] = it;
-    short_of |= here > d.pages - total;  // (sums of a call stay below 2^32)
-    if (__syncthreads_or(bad | short_of)) break;
+    it.off = total + scan_lanes(need, &here, sh);
+    if (r.n > kPlanLanes && i < r.n) d.items[i] = it;
+    short_of = here > d.pages - total;  // (sums of a call stay below 2^32)
+    bad = __syncthreads_or(bad);
+    if (bad || short_of) break;
     total += here;
   }
-  bad = __syncthreads_or(bad);
-  short_of = __syncthreads_or(short_of);
   if (bad || short_of || total > d.ctrl->free) {
     __syncthreads();
     if (threadIdx.x == 0) d.ctrl->stopped = 1;
     return drop(d, bad ? RTAMS_EINVAL : RTAMS_EPOOL);
   }
-  if (total) pick_pages(d, total);
+  if (total) pick_pages(d, total, sh);
   for (int base = 0; base < r.n; base += kPlanLanes) {
-    if (threadIdx.x == 0) nbig = 0;
-    __syncthreads();
     const int i = base + threadIdx.x;
+    if (r.n > kPlanLanes) it = i < r.n ? d.items[i] : CacheItem{};
     if (i < r.n) {
-      const CacheItem it = d.items[i];
-      int32_t *row = d.table + (int64_t)it.seq * d.max_pages;
       if (it.copy) {
-        const int32_t from = row[it.have - 1], to = d.picked[it.off];
-        row[it.have - 1] = to;
+        int32_t *last = d.table + (int64_t)it.seq * d.max_pages + it.have - 1;
+        const int32_t from = *last, to = picked_page(d, sh, it.off);
+        *last = to;
         d.refs[to] = 1;
         if (atomicSub(&d.refs[from], 1) == 1) {  // all that shared it got copies
           put_back(d, from);
-          atomicAdd(&nfreed, 1u);
+          atomicAdd(&sh.freed, 1u);
         }
-        const uint32_t at = atomicAdd(&npairs, 1u);
+        const uint32_t at = atomicAdd(&sh.pairs, 1u);
         d.pair_src[at] = from;
         d.pair_dst[at] = to;
       }
-      if (it.want - it.have <= 4) {
-        for (int p = it.have; p < it.want; ++p) {
-          const int32_t page = d.picked[it.off + it.copy + (p - it.have)];
-          row[p] = page;
-          d.refs[page] = 1;
-        }
-      } else {
-        big[atomicAdd(&nbig, 1u)] = i;
-      }
       d.lengths[it.seq] = it.src;
     }
+    uint32_t fresh;
+    sh.before[threadIdx.x] = scan_lanes(i < r.n ? (uint32_t)(it.want - it.have) : 0, &fresh, sh);
+    if (fresh == 0) continue;
+    sh.seq[threadIdx.x] = it.seq;
+    sh.page0[threadIdx.x] = it.have;
+    sh.src[threadIdx.x] = (int32_t)(it.off + it.copy);
     __syncthreads();
-    for (uint32_t b = 0; b < nbig; ++b) {
-      const CacheItem it = d.items[big[b]];
-      int32_t *row = d.table + (int64_t)it.seq * d.max_pages;
-      for (int p = it.have + (int)threadIdx.x; p < it.want; p += kPlanLanes) {
-        const int32_t page = d.picked[it.off + it.copy + (p - it.have)];
-        row[p] = page;
-        d.refs[page] = 1;
-      }
+    for (uint32_t e = threadIdx.x; e < fresh; e += kPlanLanes) {
+      const int x = item_of(sh, e);
+      const uint32_t nth = e - sh.before[x];
+      const int32_t page = picked_page(d, sh, (uint32_t)sh.src[x] + nth);
+      d.table[(int64_t)sh.seq[x] * d.max_pages + sh.page0[x] + nth] = page;
+      d.refs[page] = 1;
     }
     __syncthreads();
   }
+  __syncthreads();
   if (threadIdx.x == 0) {
-    d.ctrl->free += nfreed - total;
-    d.ctrl->pairs = npairs;
+    d.ctrl->free += sh.freed - total;
+    d.ctrl->pairs = sh.pairs;
     d.ctrl->ok = 1;
     d.ctrl->stopped = 0;
   }
 }
 
-// Table entries of the call's items, 64 at a time, by `waves` wavefronts of which this is number `wave`.
-template <class F>
-__device__ void each_entry(const CacheDev &d, int n, int wave, int waves, F f) {
-  const int per = (d.max_pages + 63) / 64;
-  for (int64_t u = wave; u < (int64_t)n * per; u += waves) {
-    const int i = (int)(u / per);
-    f(i, d.items[i], (int)(u % per) * 64 + (int)lane_id());
+// Table entry p of a sequence that gives it up; true where the page is free now.
+__device__ inline bool give_up(const CacheDev &d, int32_t seq, int p) {
+  int32_t *e = d.table + (int64_t)seq * d.max_pages + p;
+  const int32_t page = *e;
+  *e = -1;
+  const bool gone = atomicSub(&d.refs[page], 1) == 1;
+  if (gone) put_back(d, page);
+  return gone;
+}
+
+// Table entry p of a fork's destination; copy: into `own`, pair `pair` of the call.
+__device__ inline void take_over(const CacheDev &d, int32_t src, int32_t dst, int p, bool copy, int32_t own, uint32_t pair) {
+  const int32_t page = d.table[(int64_t)src * d.max_pages + p];
+  d.table[(int64_t)dst * d.max_pages + p] = copy ? own : page;
+  if (copy) {
+    d.refs[own] = 1;
+    d.pair_src[pair] = page;
+    d.pair_dst[pair] = own;
+  } else {
+    atomicAdd(&d.refs[page], 1);
   }
 }
 
-__device__ void trim_entries(const CacheDev &d, int n, int wave, int waves) {
-  each_entry(d, n, wave, waves, [&](int, const CacheItem &it, int p) {
-    bool gone = false;
-    if (p >= it.want && p < it.have) {
-      int32_t *e = d.table + (int64_t)it.seq * d.max_pages + p;
-      const int32_t page = *e;
-      *e = -1;
-      gone = atomicSub(&d.refs[page], 1) == 1;
-      if (gone) put_back(d, page);
+__global__ __launch_bounds__(kPlanLanes) void k_cache_trim(CacheDev d, int32_t n, const int32_t *seqs, const int32_t *lengths, int inline_too) {
+  __shared__ Plan sh;
+  clear_seen(d, sh);
+  int bad = 0;
+  CacheItem it{};
+  for (int base = 0; base < n; base += kPlanLanes) {
+    const int i = base + threadIdx.x;
+    it = CacheItem{};
+    if (i < n) {
+      const int s = seqs ? seqs[i] : i, to = lengths ? lengths[i] : 0;
+      if ((uint32_t)s >= (uint32_t)d.max_seqs || named_before(sh.seen, s)) {
+        bad = 1;
+      } else {
+        const int length = d.lengths[s];
+        bad |= to < 0 || to > length;
+        it.seq = s;
+        it.src = to;
+        it.have = pages_for(d, length);
+        it.want = pages_for(d, to);
+      }
+      if (n > kPlanLanes || !inline_too) d.items[i] = it;
     }
+  }
+  if (__syncthreads_or(bad)) return drop(d, RTAMS_EINVAL);
+  for (int base = 0; base < n; base += kPlanLanes) {
+    const int i = base + threadIdx.x;
+    if (n > kPlanLanes) it = i < n ? d.items[i] : CacheItem{};
+    if (i < n) d.lengths[it.seq] = it.src;
+    if (!inline_too) continue;
+    uint32_t entries;
+    sh.before[threadIdx.x] = scan_lanes(i < n ? (uint32_t)(it.have - it.want) : 0, &entries, sh);
+    if (entries == 0) continue;
+    sh.seq[threadIdx.x] = it.seq;
+    sh.page0[threadIdx.x] = it.want;
+    __syncthreads();
+    uint32_t gone = 0;
+    for (uint32_t e = threadIdx.x; e < entries; e += kPlanLanes) {
+      const int x = item_of(sh, e);
+      gone += give_up(d, sh.seq[x], sh.page0[x] + (int)(e - sh.before[x]));
+    }
+    if (gone) atomicAdd(&sh.freed, gone);
+    __syncthreads();
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    d.ctrl->ok = 1;
+    d.ctrl->free += sh.freed;
+  }
+}
+
+// Table entries of the call's items, 64 at a time.
+template <class F>
+__device__ void each_entry(const CacheDev &d, int n, F f) {
+  const uint32_t per = (uint32_t)(d.max_pages + 63) / 64;
+  uint32_t i = (blockIdx.x * 4 + (threadIdx.x >> 6)) / per, chunk = (blockIdx.x * 4 + (threadIdx.x >> 6)) % per;
+  const uint32_t step_i = gridDim.x * 4 / per, step_chunk = gridDim.x * 4 % per;
+  while (i < (uint32_t)n) {
+    f(d.items[i], (int)(chunk * 64 + lane_id()));
+    i += step_i;
+    chunk += step_chunk;
+    if (chunk >= per) {
+      chunk -= per;
+      ++i;
+    }
+  }
+}
+
+__global__ __launch_bounds__(256) void k_cache_trim_entries(CacheDev d, int32_t n) {
+  if (!d.ctrl->ok) return;
+  each_entry(d, n, [&](const CacheItem &it, int p) {
+    const bool gone = p >= it.want && p < it.have && give_up(d, it.seq, p);
     const uint64_t all = __ballot(gone);
     if (all && lane_id() == 0) atomicAdd(&d.ctrl->free, (uint32_t)__popcll(all));
   });
 }
 
-__global__ __launch_bounds__(kPlanLanes) void k_cache_trim(CacheDev d, int32_t n, const int32_t *seqs, const int32_t *lengths, int inline_too) {
-  __shared__ uint32_t seen[kCacheMaxSeqs / 32];
-  for (int i = threadIdx.x; i < (d.max_seqs + 31) / 32; i += kPlanLanes) seen[i] = 0;
-  __syncthreads();
-  int bad = 0;
-  for (int i = threadIdx.x; i < n; i += kPlanLanes) {
-    const int s = seqs ? seqs[i] : i, to = lengths ? lengths[i] : 0;
-    if ((uint32_t)s >= (uint32_t)d.max_seqs || named_before(seen, s) || to < 0 || to > d.lengths[s]) {
-      bad = 1;
-    } else {
-      CacheItem it{};
-      it.seq = s;
-      it.src = to;
-      it.have = pages_for(d, d.lengths[s]);
-      it.want = pages_for(d, to);
-      d.items[i] = it;
-    }
-  }
-  if (__syncthreads_or(bad)) return drop(d, RTAMS_EINVAL);
-  for (int i = threadIdx.x; i < n; i += kPlanLanes) d.lengths[d.items[i].seq] = d.items[i].src;
-  if (threadIdx.x == 0) d.ctrl->ok = 1;
-  if (inline_too) trim_entries(d, n, threadIdx.x >> 6, kPlanLanes / 64);
-}
-
-__global__ __launch_bounds__(256) void k_cache_trim_entries(CacheDev d, int32_t n) {
-  if (d.ctrl->ok) trim_entries(d, n, blockIdx.x * 4 + (threadIdx.x >> 6), gridDim.x * 4);
-}
-
-__device__ void fork_entries(const CacheDev &d, int n, int wave, int waves) {
-  each_entry(d, n, wave, waves, [&](int, const CacheItem &it, int p) {
-    if (p == 0) d.lengths[it.seq] = d.lengths[it.src];
-    if (p >= it.have) return;
-    const int32_t page = d.table[(int64_t)it.src * d.max_pages + p];
-    int32_t *to = d.table + (int64_t)it.seq * d.max_pages + p;
-    if (it.copy) {
-      const int32_t own = d.picked[it.off + p];
-      *to = own;
-      d.refs[own] = 1;
-      d.pair_src[it.off + p] = page;
-      d.pair_dst[it.off + p] = own;
-    } else {
-      *to = page;
-      atomicAdd(&d.refs[page], 1);
-    }
-  });
-}
-
 __global__ __launch_bounds__(kPlanLanes) void k_cache_fork(CacheDev d, int32_t n, const int32_t *src, const int32_t *dst, int copy, int inline_too) {
-  __shared__ uint32_t seen[kCacheMaxSeqs / 32];
-  for (int i = threadIdx.x; i < (d.max_seqs + 31) / 32; i += kPlanLanes) seen[i] = 0;
-  __syncthreads();
+  __shared__ Plan sh;
+  clear_seen(d, sh);
   int bad = 0, short_of = 0;
   for (int i = threadIdx.x; i < n; i += kPlanLanes) {
     const int s = dst[i];
-    bad |= (uint32_t)s >= (uint32_t)d.max_seqs || named_before(seen, s) || d.lengths[s] != 0;
+    bad |= (uint32_t)s >= (uint32_t)d.max_seqs || named_before(sh.seen, s) || d.lengths[s] != 0;
   }
   bad = __syncthreads_or(bad);
   uint32_t total = 0;
+  CacheItem it{};
   for (int base = 0; base < n && !bad && !short_of; base += kPlanLanes) {
     const int i = base + threadIdx.x;
     uint32_t need = 0, here;
-    CacheItem it{};
+    it = CacheItem{};
     if (i < n) {
       const int s = src[i];
-      if ((uint32_t)s >= (uint32_t)d.max_seqs || (seen[s >> 5] >> (s & 31)) & 1) {
+      if ((uint32_t)s >= (uint32_t)d.max_seqs || (sh.seen[s >> 5] >> (s & 31)) & 1) {
         bad = 1;
       } else {
         it.seq = dst[i];
         it.src = s;
-        it.have = it.want = pages_for(d, d.lengths[s]);
+        it.want = d.lengths[s];
+        it.have = pages_for(d, it.want);
         it.copy = copy;
         need = copy ? (uint32_t)it.have : 0;
       }
     }
-    it.off = total + scan_lanes(need, &here);
-    if (i < n) d.items[i] = it;
+    it.off = total + scan_lanes(need, &here, sh);
+    if (i < n && (n > kPlanLanes || !inline_too)) d.items[i] = it;
     short_of = here > d.pages - total;
     total += here;
     bad = __syncthreads_or(bad);
@@ -278,22 +328,47 @@ __global__ __launch_bounds__(kPlanLanes) void k_cache_fork(CacheDev d, int32_t n
     __syncthreads();
     return drop(d, bad ? RTAMS_EINVAL : RTAMS_EPOOL);
   }
-  if (total) pick_pages(d, total);
+  if (total) pick_pages(d, total, sh);
   __syncthreads();
   if (threadIdx.x == 0) {
     d.ctrl->free -= total;
     d.ctrl->pairs = total;
     d.ctrl->ok = 1;
   }
-  if (inline_too) fork_entries(d, n, threadIdx.x >> 6, kPlanLanes / 64);
+  if (!inline_too) {  // (the pages in LDS are wanted by others)
+    for (uint32_t x = threadIdx.x; x < total && x < kPicked; x += kPlanLanes) d.picked[x] = sh.picked[x];
+    return;
+  }
+  for (int base = 0; base < n; base += kPlanLanes) {
+    const int i = base + threadIdx.x;
+    if (n > kPlanLanes) it = i < n ? d.items[i] : CacheItem{};
+    if (i < n) d.lengths[it.seq] = it.want;
+    uint32_t entries;
+    sh.before[threadIdx.x] = scan_lanes(i < n ? (uint32_t)it.have : 0, &entries, sh);
+    sh.seq[threadIdx.x] = it.seq;
+    sh.src[threadIdx.x] = it.src;
+    sh.page0[threadIdx.x] = (int32_t)it.off;
+    __syncthreads();
+    for (uint32_t e = threadIdx.x; e < entries; e += kPlanLanes) {
+      const int x = item_of(sh, e), p = (int)(e - sh.before[x]);
+      const uint32_t pair = (uint32_t)sh.page0[x] + (uint32_t)p;
+      take_over(d, sh.src[x], sh.seq[x], p, copy, copy ? picked_page(d, sh, pair) : 0, pair);
+    }
+    __syncthreads();
+  }
 }
 
 __global__ __launch_bounds__(256) void k_cache_fork_entries(CacheDev d, int32_t n) {
-  if (d.ctrl->ok) fork_entries(d, n, blockIdx.x * 4 + (threadIdx.x >> 6), gridDim.x * 4);
+  if (!d.ctrl->ok) return;
+  each_entry(d, n, [&](const CacheItem &it, int p) {
+    if (p == 0) d.lengths[it.seq] = it.want;
+    if (p < it.have) take_over(d, it.src, it.seq, p, it.copy, it.copy ? d.picked[it.off + p] : 0, it.off + p);
+  });
 }
 
 // Which pages go where.  Free pages below the number in use and used ones from there on are equally many.
 __global__ __launch_bounds__(kPlanLanes) void k_cache_compact(CacheDev d) {
+  __shared__ Plan sh;
   const uint32_t used = d.pages - d.ctrl->free, words = (d.pages + 31) / 32;
   uint32_t holes = 0, movers = 0;
   for (uint32_t base = 0; base < words; base += kPlanLanes) {
@@ -308,7 +383,7 @@ __global__ __launch_bounds__(kPlanLanes) void k_cache_compact(CacheDev d) {
       if (low | high) d.free_bits[at] = real & ~below;
     }
     uint32_t all_low, all_high;
-    uint32_t a = holes + scan_lanes(__popc(low), &all_low), b = movers + scan_lanes(__popc(high), &all_high);
+    uint32_t a = holes + scan_lanes(__popc(low), &all_low, sh), b = movers + scan_lanes(__popc(high), &all_high, sh);
     for (uint32_t x = low; x; x &= x - 1) d.pair_dst[a++] = (int32_t)(at * 32 + __ffs(x) - 1);
     for (uint32_t x = high; x; x &= x - 1) d.pair_src[b++] = (int32_t)(at * 32 + __ffs(x) - 1);
     holes += all_low;
@@ -332,14 +407,12 @@ __global__ __launch_bounds__(256) void k_cache_move(CacheDev d, int renames) {
   const uint32_t pairs = d.ctrl->pairs;
   if (pairs == 0) return;
   if ((int)blockIdx.x < renames) {
-    const int per = (d.max_pages + 63) / 64;
     const uint32_t used = d.ctrl->used;
-    for (int64_t u = blockIdx.x * 4 + (threadIdx.x >> 6); u < (int64_t)d.max_seqs * per; u += renames * 4) {
-      const int s = (int)(u / per), p = (int)(u % per) * 64 + (int)lane_id();
-      if (p >= pages_for(d, d.lengths[s])) continue;
-      int32_t *e = d.table + (int64_t)s * d.max_pages + p;
-      if ((uint32_t)*e >= used) *e = d.map[*e];
-    }
+    for (int s = blockIdx.x; s < d.max_seqs; s += renames)
+      for (int p = threadIdx.x, n = pages_for(d, d.lengths[s]); p < n; p += 256) {
+        int32_t *e = d.table + (int64_t)s * d.max_pages + p;
+        if ((uint32_t)*e >= used) *e = d.map[*e];
+      }
     return;
   }
   const uint32_t pieces = (uint32_t)((d.page_bytes + kCopyBytes - 1) / kCopyBytes), per_pair = pieces * (uint32_t)d.layers;
@@ -375,9 +448,9 @@ bool walks_inline(const CacheDev &d, int64_t n) { return n * (int64_t)d.max_page
 
 }  // namespace
 
-void launch_cache_extend(const CacheDev &d, const CacheRows &r, hipStream_t s) {
+void launch_cache_extend(const CacheDev &d, const CacheRows &r, bool copies, hipStream_t s) {
   k_cache_extend<<<1, kPlanLanes, 0, s>>>(d, r);
-  k_cache_move<<<copy_groups(d, r.n), 256, 0, s>>>(d, 0);
+  if (copies) k_cache_move<<<copy_groups(d, r.n), 256, 0, s>>>(d, 0);
 }
 
 void launch_cache_trim(const CacheDev &d, int32_t n, const int32_t *seqs, const int32_t *lengths, hipStream_t s) {
@@ -395,7 +468,7 @@ void launch_cache_fork(const CacheDev &d, int32_t n, const int32_t *src, const i
 
 void launch_cache_compact(const CacheDev &d, hipStream_t s) {
   k_cache_compact<<<1, kPlanLanes, 0, s>>>(d);
-  const int renames = entry_groups(d, d.max_seqs);
+  const int renames = d.max_seqs < 1024 ? d.max_seqs : 1024;
   k_cache_move<<<renames + copy_groups(d, d.pages), 256, 0, s>>>(d, renames);
 }
 

@@ -361,9 +361,14 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(C
       if (t + 1 < t1) put_tile(next, sh.k[now ^ 1], sh.v[now ^ 1]);
       if (t + 2 < t1) load_tile(next, t + 2);
       if (some) {
+        // (matrix instructions first: the other wavefront of the SIMD has its exponentials beside them)
+        __builtin_amdgcn_s_setprio(1);
         scores(sh.k[now]);
+        __builtin_amdgcn_s_setprio(0);
         probabilities(tok0);
+        __builtin_amdgcn_s_setprio(1);
         weigh(sh.v[now]);
+        __builtin_amdgcn_s_setprio(0);
       }
       __syncthreads();
     }

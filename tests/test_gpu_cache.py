@@ -165,6 +165,27 @@ def test_what_is_written_is_what_the_definition_says(dim, dtype):
         assert np.all(np.abs(got - want) <= np.spacing(np.abs(want).astype(np.float32)))  # one rounding to 32 bits
 
 
+def test_every_step_there_is():
+    """Groups whose step is each of the positive halves, and groups in between: the same codes as with divisions."""
+    steps = np.arange(1, 0x7000, dtype=np.uint16).view(np.float16).astype(np.float64)
+    for seed, widths in enumerate((steps * 15, steps * 15 * 1.0003, steps * 14.996)):
+        widths = widths[widths < 60000]
+        rows = -(-len(widths) // 2)
+        rng = np.random.default_rng(seed)
+        x = rng.random((rows * 2, 32))
+        x[:, 0], x[:, 1] = 0.0, 1.0
+        x[: len(widths)] *= widths[:, None]
+        x = torch.from_numpy(x.reshape(rows, 1, 64)).to(DEV).half()
+        c = Cache(1, 64, page_tokens=1024, pages=-(-rows // 1024), max_seqs=1, device=DEV)
+        st = ints([0, rows])
+        c.extend(starts=st)
+        c.write(0, x, -x, starts=st, max_new=rows)
+        k, v = c.read(0, rows, starts=st, max_new=rows)
+        for got, src in ((k, x), (v, -x)):
+            want = held(floats(src))
+            assert np.all(np.abs(got.cpu().numpy() - want) <= np.spacing(np.abs(want).astype(np.float32)))
+
+
 @pytest.mark.parametrize("dim", [64, 96])
 def test_rows_written_one_at_a_time_are_those_written_at_once(dim):
     g = torch.Generator(device=DEV).manual_seed(3)
