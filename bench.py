@@ -432,7 +432,7 @@ def main() -> int:
     ap.add_argument("--pq-m", type=int, default=0,
                     help="with --study pq: only this number of sub-spaces, and only the --batch query batch")
     ap.add_argument("--shape", type=int, default=0, help="with --study shapes: only this configuration (3, 4 or 5)")
-    ap.add_argument("--study", choices=["rearrange", "rearrange5", "blocksize", "pq", "storage", "shapes", "mixed", "growth", "online"],
+    ap.add_argument("--study", choices=["rearrange", "rearrange5", "blocksize", "pq", "storage", "shapes", "mixed", "growth", "online", "answers"],
                     help="run one of the side studies instead of the benchmark (one JSON line each)")
     args = ap.parse_args()
     if args.gpus != 1:
@@ -457,6 +457,10 @@ def main() -> int:
         return 0
     if args.study:
         from paper_2408_02937_amd import studies
+        if args.study == "answers":
+            from paper_2408_02937_amd import answers
+            print(json.dumps(answers.answers_study(scale=args.scale)))
+            return 0
         fn = {"rearrange": studies.rearrangement_study, "blocksize": studies.block_size_sweep,
               "pq": studies.pq_study, "storage": studies.storage_study, "shapes": studies.shape_study,
               "mixed": studies.mixed_load_study, "growth": studies.growth_study,
