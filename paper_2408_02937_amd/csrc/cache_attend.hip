@@ -18,7 +18,6 @@ namespace rtams {
 namespace {
 
 constexpr int kLanes = 256, kWaves = 4, kStep = kWaves * kBlockTokens;
-constexpr int kUnits = 256;      // compute units
 
 // Workgroups that a compute unit runs at once: registers decide, and from 128 channels on LDS.
 constexpr int at_once(int head_dim, int tiles) {
@@ -31,24 +30,38 @@ struct Span {  // what an item asks for
   int64_t row0;
 };
 
-__device__ inline Span find_span(const CacheDev &d, const CacheQuery &q, int i, bool tell) {
-  Span s{};
-  if (i >= q.r.n) return s;
-  const bool ok = cache_item_rows(q.r, i, &s.row0, &s.count);
-  s.seq = cache_item_seq(q.r, i);
-  if (!ok || (uint32_t)s.seq >= (uint32_t)d.max_seqs) {
-    if (tell) cache_raise(d, RTAMS_EINVAL);
-    s.count = 0;
-    return s;
+// Items i + 64 k of the launch, for k of 0 .. N - 1; steps 0 behind the last one.  Loads are asked for together, whatever they find: each is
+// a trip to memory, at the beginning of a launch.
+template <int N>
+__device__ inline void find_spans(const CacheDev &d, const CacheQuery &q, int i, bool tell, Span (&s)[N]) {
+  const int n = q.r.n;
+  int first[N], past[N], seq[N], length[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) first[k] = min(i + 64 * k, n - 1), past[k] = first[k] + 1, seq[k] = first[k];
+  if (q.r.seqs)
+#pragma unroll
+    for (int k = 0; k < N; ++k) seq[k] = q.r.seqs[min(i + 64 * k, n - 1)];
+  if (q.r.starts)
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      first[k] = q.r.starts[min(i + 64 * k, n - 1)];
+      past[k] = q.r.starts[min(i + 64 * k, n - 1) + 1];
+    }
+#pragma unroll
+  for (int k = 0; k < N; ++k) length[k] = d.lengths[(uint32_t)seq[k] < (uint32_t)d.max_seqs ? seq[k] : 0];
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const bool there = i + 64 * k < n, known = (uint32_t)seq[k] < (uint32_t)d.max_seqs;
+    const bool ok = first[k] >= 0 && past[k] >= first[k] && past[k] <= q.r.rows && past[k] - first[k] <= q.r.max_new && known;
+    s[k].row0 = first[k];
+    s[k].seq = seq[k];
+    s[k].count = there && ok ? past[k] - first[k] : 0;
+    s[k].length = length[k];
+    if (tell && there && (!ok || (q.causal && s[k].count > length[k]))) cache_raise(d, RTAMS_EINVAL);
+    const int low = length[k] - s[k].count - q.window + 1;
+    s[k].low = q.window && low > 0 ? low & ~(kBlockTokens - 1) : 0;
+    s[k].steps = s[k].count <= 0 ? 0 : length[k] > s[k].low ? (length[k] - s[k].low + kStep - 1) / kStep : 1;
   }
-  s.length = d.lengths[s.seq];
-  if (tell && q.causal && s.count > s.length) cache_raise(d, RTAMS_EINVAL);
-  if (q.causal && q.window) {
-    const int low = s.length - s.count - q.window + 1;
-    s.low = low > 0 ? low & ~(kBlockTokens - 1) : 0;
-  }
-  if (s.count > 0) s.steps = s.length > s.low ? (s.length - s.low + kStep - 1) / kStep : 1;
-  return s;
 }
 
 constexpr int kAhead = 2;   // blocks of a wavefront that are in LDS or on their way
@@ -60,80 +73,59 @@ struct Piece {  // steps [sa, sb) of an item's head
   int part;        // where the head's parts begin, if there are several
 };
 
-constexpr int kEach = 4, kRound = 64 * kEach;  // items that a lane of the planning wavefront has, and all of them
+constexpr int kRound = 256;  // items that the planning wavefront has at a time, four to a lane at most
 
 template <int D, int NR>
 struct alignas(16) Shared {
   union {
     unsigned char ring[kWaves][kAhead][40 * D];
     float o[kWaves][16][D + 4];  // when the rings are read: the wavefronts' parts of 16 rows
-    float steps[kRound];         // in front of it all
+    float steps[kRound];         // in front of it all: of each item
   };
   float ml[kWaves][16 * NR][2];
   Piece piece;
   int last;
 };
 
-// Which piece is workgroup blockIdx.x's: the items' steps, the size of a piece, and the pieces of the items in front.  One wavefront's work;
-// false where there is none left.
-template <class S>
+// Which piece is workgroup blockIdx.x's: the items' steps, the size of a piece, and the pieces of the items in front.  One wavefront's work, EACH
+// items to a lane (lane, lane + 64, ...); false where there is none left.
+template <int EACH, class S>
 __device__ bool find_piece(const CacheDev &d, const CacheQuery &q, uint32_t workers, S &sh) {
+  constexpr int kItems = 64 * EACH;
   const int lane = threadIdx.x & 63, n = q.r.n;
-  Span sp[kEach];
-  const auto look = [&](int base, bool tell) {
+  Span sp[EACH];
+  uint32_t all = 0;
+  for (int base = 0; base < n; base += kItems) {
+    find_spans<EACH>(d, q, base + lane, blockIdx.x == 0, sp);
     uint32_t sum = 0;
 #pragma unroll
-    for (int k = 0; k < kEach; ++k) {
-      sp[k] = find_span(d, q, base + lane * kEach + k, tell);
-      sum += (uint32_t)sp[k].steps;
-    }
-    return sum;
-  };
-  uint64_t all = 0;
-  for (int base = 0; base < n; base += kRound) all += last_lane(wave_running_sum((unsigned long long)look(base, blockIdx.x == 0)));
-  all *= (uint64_t)d.kv_heads;
+    for (int k = 0; k < EACH; ++k) sum += (uint32_t)sp[k].steps;
+    all += last_lane(wave_running_sum(sum));
+  }
+  all *= (uint32_t)d.kv_heads;
   // where items are many, pieces are an even share at most, and long items do not keep the others waiting
-  const uint32_t share = (uint32_t)((all + workers - 1) / workers);
+  const uint32_t share = (all + workers - 1) / workers;
   uint32_t size = share > 1 ? share : 1;
-  if (share > 1 && n <= kRound && n * d.kv_heads <= (int)workers / 2) {
-    *reinterpret_cast<f32x4 *>(sh.steps + lane * kEach) = f32x4{(float)sp[0].steps, (float)sp[1].steps, (float)sp[2].steps, (float)sp[3].steps};
+  if (share > 1 && n <= kItems && n * d.kv_heads <= (int)workers / 2) {
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) sh.steps[64 * k + lane] = (float)sp[k].steps;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     size = piece_steps(sh.steps, n, d.kv_heads, share, workers);
   }
   const float one_over = 1.0f / (float)size;
   uint32_t before = 0, parts_before = 0;
-  for (int base = 0; base < n; base += kRound) {
-    if (n > kRound) look(base, false);
-    uint32_t parts[kEach], pieces = 0, shared = 0;
+  for (int base = 0; base < n; base += kItems) {
+    if (n > kItems) find_spans<EACH>(d, q, base + lane, false, sp);
 #pragma unroll
-    for (int k = 0; k < kEach; ++k) {
-      parts[k] = div_up((uint32_t)sp[k].steps, size, one_over);
-      pieces += parts[k] * (uint32_t)d.kv_heads;
-      shared += parts[k] > 1 ? parts[k] * (uint32_t)d.kv_heads : 0;
+    for (int k = 0; k < EACH; ++k) {
+      const uint32_t parts = div_up((uint32_t)sp[k].steps, size, one_over), pieces = parts * (uint32_t)d.kv_heads, shared = parts > 1 ? pieces : 0;
+      const uint32_t upto = wave_running_sum(pieces), upto_shared = wave_running_sum(shared), x = blockIdx.x - (before + upto - pieces);
+      if (x < pieces)
+        sh.piece = Piece{sp[k], base + 64 * k + lane, (int)(x / parts), 0, 0, (int)parts, (int)(x % parts), (int)(parts_before + upto_shared - shared + x - x % parts)};
+      if (__any(x < pieces)) return true;
+      before += last_lane(upto);
+      parts_before += last_lane(upto_shared);
     }
-    const uint32_t upto = wave_running_sum(pieces), upto_shared = wave_running_sum(shared);
-    uint32_t first = before + upto - pieces, first_shared = parts_before + upto_shared - shared;
-    // (of this lane's items, the one that the workgroup's piece is of)
-    uint32_t x = ~0u, of = 0, at = 0;
-    Span mine{};
-    int item = 0;
-#pragma unroll
-    for (int k = 0; k < kEach; ++k) {
-      const uint32_t here = parts[k] * (uint32_t)d.kv_heads;
-      if (blockIdx.x - first < here) {
-        x = blockIdx.x - first;
-        of = parts[k];
-        at = first_shared;
-        mine = sp[k];
-        item = base + lane * kEach + k;
-      }
-      first += here;
-      first_shared += parts[k] > 1 ? here : 0;
-    }
-    if (x != ~0u) sh.piece = Piece{mine, item, (int)(x / of), 0, 0, (int)of, (int)(x % of), (int)(at + x - x % of)};
-    if (__any(x != ~0u)) return true;
-    before += last_lane(upto);
-    parts_before += last_lane(upto_shared);
   }
   return false;
 }
@@ -147,11 +139,14 @@ struct Copies {
   ScalarInts table;
   int head, tok, to;   // next block's first token; end of the piece's tokens
   uint32_t ring, slot;
-  uint32_t page;       // of the next block
+  uint32_t page, page2;  // of the next block and the one after
 
-  // (pages are looked up by scalar loads, a block ahead: a vector load would wait for all copies under way)
-  __device__ __forceinline__ void look(const CacheDev &d) {
-    if (tok < to) page = (uint32_t)table[cache_page_of(d, (uint32_t)tok / kBlockTokens)];
+  // (pages are looked up by scalar loads, two blocks ahead: a vector load would wait for all copies under way)
+  __device__ __forceinline__ uint32_t look(const CacheDev &d, int at) { return (uint32_t)table[cache_page_of(d, (uint32_t)min(at, to - 1) / kBlockTokens)]; }
+  __device__ __forceinline__ void begin(const CacheDev &d) {
+    if (tok >= to) return;
+    page = look(d, tok);
+    page2 = look(d, tok + kStep);
   }
   __device__ __forceinline__ void one(const CacheDev &d, int layer, int lane) {
     if (tok >= to) return;
@@ -162,7 +157,8 @@ struct Copies {
       if (40 * D - i * 1024 >= 1024 || lane * 16 < 40 * D - i * 1024) copy_to_lds(blk + i * 1024, ring + slot * (40 * D) + i * 1024, lane * 16);
     slot ^= 1;
     tok += kStep;
-    look(d);
+    page = page2;
+    page2 = look(d, tok + kStep);
   }
 };
 
@@ -174,7 +170,7 @@ __global__ __launch_bounds__(kLanes, at_once(D, NR)) void k_cache_attend(CacheDe
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 15, b = lane >> 4;
 
   if (wave == 0) {
-    const bool found = find_piece(d, q, kUnits * at_once(D, NR), sh);
+    const bool found = q.r.n <= 64 ? find_piece<1>(d, q, kUnits * at_once(D, NR), sh) : find_piece<kRound / 64>(d, q, kUnits * at_once(D, NR), sh);
     if (lane == 0) sh.last = found;
   }
   __syncthreads();
@@ -196,7 +192,7 @@ __global__ __launch_bounds__(kLanes, at_once(D, NR)) void k_cache_attend(CacheDe
   cp.to = min(sp.low + pc.sb * kStep, sp.length);
   cp.ring = (uint32_t)uniform((int)lds_address(sh.ring[wave][0]));
   cp.slot = 0;
-  cp.look(d);
+  cp.begin(d);
 #pragma unroll
   for (int i = 0; i < kAhead; ++i) cp.one(d, q.layer, lane);
 

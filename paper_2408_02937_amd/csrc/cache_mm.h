@@ -200,8 +200,12 @@ __device__ inline uint32_t div_up(uint32_t a, uint32_t b, float one_over_b) {
   return q + (r > 0);
 }
 
-// Steps of a piece, of `all` steps for n items.  Pieces are to run all at once, so sixteen sizes from an even share up to
-// twice that are tried, a quarter of the items to a lane, and the least is taken with which they do.
+constexpr int kUnits = 256;  // compute units
+
+// Steps of a piece, of n items' steps.  Pieces are to run all at once, `workers` of them, and to leave the compute units alike much to do:
+// of sixteen sizes from an even share up to twice that, a quarter of the items to a lane, the one with the least steps for a
+// compute unit, which has pieces / 256 rounded up.  (32 single tokens of 1 to 4 thousand: 680 pieces of 7 steps, three for some and
+// two for others, 28 us; 512 of 9, KPIECE.)
 __device__ inline uint32_t piece_steps(const float *steps, int n, int kv_heads, uint32_t share, uint32_t workers) {
   const int lane = threadIdx.x & 63;
   const uint32_t more = (share + 15) / 16, size = share + (lane & 15) * more;
@@ -213,8 +217,13 @@ __device__ inline uint32_t piece_steps(const float *steps, int n, int kv_heads, 
   }
   pieces += __shfl_xor(pieces, 16);
   pieces += __shfl_xor(pieces, 32);
-  const uint64_t fits = __ballot(pieces * (float)kv_heads <= (float)workers) & 0xffff;
-  return fits ? share + (uint32_t)(__ffsll((unsigned long long)fits) - 1) * more : 2 * share;
+  const uint32_t all = (uint32_t)pieces * (uint32_t)kv_heads;
+  float cost = all <= workers ? (float)((all + kUnits - 1) / kUnits) * (float)size : 3e38f;
+  const float mine = cost;
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) cost = fminf(cost, __shfl_xor(cost, o));
+  const uint64_t best = __ballot(mine == cost && cost < 3e38f) & 0xffff;
+  return best ? share + (uint32_t)(__ffsll((unsigned long long)best) - 1) * more : 2 * share;
 }
 
 // Channels c .. c + 3 of a row of n parts, `stride` rows apart, joined in order.

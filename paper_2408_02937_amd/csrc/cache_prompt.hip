@@ -21,7 +21,6 @@ namespace {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int tile_blocks(int head_dim) { return head_dim == 256 ? 1 : 2; }  // of 32 tokens; registers decide
-constexpr int kUnits = 256;      // compute units
 constexpr int kRows = 256;       // of a workgroup's parts at most
 
 // Workgroups that a compute unit runs at once: registers decide.
