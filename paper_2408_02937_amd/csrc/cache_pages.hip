@@ -15,8 +15,8 @@ namespace {
 
 constexpr int kPlanLanes = 1024;
 constexpr int kCopyBytes = 16384;   // a workgroup's piece
-constexpr int kInlineSlots = 16384; // table entries that the planning workgroup walks by itself
 constexpr int kPicked = 2048;       // new pages that it keeps in LDS
+constexpr int kFewEntries = kPlanLanes;  // table entries that it walks by itself
 
 __device__ inline uint32_t lane_id() { return threadIdx.x & 63; }
 
@@ -24,9 +24,9 @@ struct Plan {
   uint32_t seen[kCacheMaxSeqs / 32];
   uint32_t waves[kPlanLanes / 64];
   int32_t picked[kPicked];
-  // of 1024 items: sequence, source of a fork, first page concerned, and how many entries the items in front concern
-  int32_t seq[kPlanLanes], src[kPlanLanes], page0[kPlanLanes];
-  uint32_t before[kPlanLanes + 1];
+  // of 1024 items: sequence, first new entry and the first page for it, and how many new entries the items in front have
+  int32_t seq[kPlanLanes], page0[kPlanLanes];
+  uint32_t off[kPlanLanes], before[kPlanLanes];
   uint32_t pairs, freed;
 };
 
@@ -147,9 +147,12 @@ __global__ __launch_bounds__(kPlanLanes) void k_cache_extend(CacheDev d, CacheRo
     return drop(d, bad ? RTAMS_EINVAL : RTAMS_EPOOL);
   }
   if (total) pick_pages(d, total, sh);
+  // few new entries, or a row for each item and so a page at most, are this workgroup's work, others the next launch's
+  const bool here_too = total <= kPlanLanes || !r.starts;
   for (int base = 0; base < r.n; base += kPlanLanes) {
     const int i = base + threadIdx.x;
     if (r.n > kPlanLanes) it = i < r.n ? d.items[i] : CacheItem{};
+    else if (!here_too && i < r.n) d.items[i] = it;
     if (i < r.n) {
       if (it.copy) {
         int32_t *last = d.table + (int64_t)it.seq * d.max_pages + it.have - 1;
@@ -166,101 +169,31 @@ __global__ __launch_bounds__(kPlanLanes) void k_cache_extend(CacheDev d, CacheRo
       }
       d.lengths[it.seq] = it.src;
     }
+    if (!here_too) continue;
     uint32_t fresh;
     sh.before[threadIdx.x] = scan_lanes(i < r.n ? (uint32_t)(it.want - it.have) : 0, &fresh, sh);
     if (fresh == 0) continue;
     sh.seq[threadIdx.x] = it.seq;
     sh.page0[threadIdx.x] = it.have;
-    sh.src[threadIdx.x] = (int32_t)(it.off + it.copy);
+    sh.off[threadIdx.x] = it.off + it.copy;
     __syncthreads();
-    for (uint32_t e = threadIdx.x; e < fresh; e += kPlanLanes) {
-      const int x = item_of(sh, e);
-      const uint32_t nth = e - sh.before[x];
-      const int32_t page = picked_page(d, sh, (uint32_t)sh.src[x] + nth);
+    if (threadIdx.x < fresh) {
+      const int x = item_of(sh, threadIdx.x);
+      const uint32_t nth = threadIdx.x - sh.before[x];
+      const int32_t page = picked_page(d, sh, sh.off[x] + nth);
       d.table[(int64_t)sh.seq[x] * d.max_pages + sh.page0[x] + nth] = page;
       d.refs[page] = 1;
     }
     __syncthreads();
   }
+  if (!here_too)
+    for (uint32_t x = threadIdx.x; x < total && x < kPicked; x += kPlanLanes) d.picked[x] = sh.picked[x];
   __syncthreads();
   if (threadIdx.x == 0) {
     d.ctrl->free += sh.freed - total;
     d.ctrl->pairs = sh.pairs;
-    d.ctrl->ok = 1;
+    d.ctrl->ok = here_too ? 0 : 1;  // whether entries are left to the next launch
     d.ctrl->stopped = 0;
-  }
-}
-
-// Table entry p of a sequence that gives it up; true where the page is free now.
-__device__ inline bool give_up(const CacheDev &d, int32_t seq, int p) {
-  int32_t *e = d.table + (int64_t)seq * d.max_pages + p;
-  const int32_t page = *e;
-  *e = -1;
-  const bool gone = atomicSub(&d.refs[page], 1) == 1;
-  if (gone) put_back(d, page);
-  return gone;
-}
-
-// Table entry p of a fork's destination; copy: into `own`, pair `pair` of the call.
-__device__ inline void take_over(const CacheDev &d, int32_t src, int32_t dst, int p, bool copy, int32_t own, uint32_t pair) {
-  const int32_t page = d.table[(int64_t)src * d.max_pages + p];
-  d.table[(int64_t)dst * d.max_pages + p] = copy ? own : page;
-  if (copy) {
-    d.refs[own] = 1;
-    d.pair_src[pair] = page;
-    d.pair_dst[pair] = own;
-  } else {
-    atomicAdd(&d.refs[page], 1);
-  }
-}
-
-__global__ __launch_bounds__(kPlanLanes) void k_cache_trim(CacheDev d, int32_t n, const int32_t *seqs, const int32_t *lengths, int inline_too) {
-  __shared__ Plan sh;
-  clear_seen(d, sh);
-  int bad = 0;
-  CacheItem it{};
-  for (int base = 0; base < n; base += kPlanLanes) {
-    const int i = base + threadIdx.x;
-    it = CacheItem{};
-    if (i < n) {
-      const int s = seqs ? seqs[i] : i, to = lengths ? lengths[i] : 0;
-      if ((uint32_t)s >= (uint32_t)d.max_seqs || named_before(sh.seen, s)) {
-        bad = 1;
-      } else {
-        const int length = d.lengths[s];
-        bad |= to < 0 || to > length;
-        it.seq = s;
-        it.src = to;
-        it.have = pages_for(d, length);
-        it.want = pages_for(d, to);
-      }
-      if (n > kPlanLanes || !inline_too) d.items[i] = it;
-    }
-  }
-  if (__syncthreads_or(bad)) return drop(d, RTAMS_EINVAL);
-  for (int base = 0; base < n; base += kPlanLanes) {
-    const int i = base + threadIdx.x;
-    if (n > kPlanLanes) it = i < n ? d.items[i] : CacheItem{};
-    if (i < n) d.lengths[it.seq] = it.src;
-    if (!inline_too) continue;
-    uint32_t entries;
-    sh.before[threadIdx.x] = scan_lanes(i < n ? (uint32_t)(it.have - it.want) : 0, &entries, sh);
-    if (entries == 0) continue;
-    sh.seq[threadIdx.x] = it.seq;
-    sh.page0[threadIdx.x] = it.want;
-    __syncthreads();
-    uint32_t gone = 0;
-    for (uint32_t e = threadIdx.x; e < entries; e += kPlanLanes) {
-      const int x = item_of(sh, e);
-      gone += give_up(d, sh.seq[x], sh.page0[x] + (int)(e - sh.before[x]));
-    }
-    if (gone) atomicAdd(&sh.freed, gone);
-    __syncthreads();
-  }
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    d.ctrl->ok = 1;
-    d.ctrl->free += sh.freed;
   }
 }
 
@@ -281,16 +214,86 @@ __device__ void each_entry(const CacheDev &d, int n, F f) {
   }
 }
 
+__global__ __launch_bounds__(256) void k_cache_extend_entries(CacheDev d, int32_t n) {
+  if (!d.ctrl->ok) return;
+  each_entry(d, n, [&](const CacheItem &it, int p) {
+    if (p < it.have || p >= it.want) return;
+    const int32_t page = d.picked[it.off + it.copy + (p - it.have)];
+    d.table[(int64_t)it.seq * d.max_pages + p] = page;
+    d.refs[page] = 1;
+  });
+}
+
+// Entry p of a sequence that gives it up; true where the page is free now.
+__device__ inline bool give_up(const CacheDev &d, int32_t seq, int p) {
+  int32_t *e = d.table + (int64_t)seq * d.max_pages + p;
+  const int32_t page = *e;
+  *e = -1;
+  const bool gone = atomicSub(&d.refs[page], 1) == 1;
+  if (gone) put_back(d, page);
+  return gone;
+}
+
+// few: at most 1024 items, and their entries are this workgroup's work.
+__global__ __launch_bounds__(kPlanLanes) void k_cache_trim(CacheDev d, int32_t n, const int32_t *seqs, const int32_t *lengths, int few) {
+  __shared__ Plan sh;
+  clear_seen(d, sh);
+  int bad = 0;
+  CacheItem it{};
+  for (int i = threadIdx.x; i < n; i += kPlanLanes) {
+    const int s = seqs ? seqs[i] : i, to = lengths ? lengths[i] : 0;
+    if ((uint32_t)s >= (uint32_t)d.max_seqs || named_before(sh.seen, s)) {
+      bad = 1;
+    } else {
+      const int length = d.lengths[s];
+      bad |= to < 0 || to > length;
+      it.seq = s;
+      it.src = to;
+      it.have = pages_for(d, length);
+      it.want = pages_for(d, to);
+      if (!few) d.items[i] = it;
+    }
+  }
+  if (__syncthreads_or(bad)) return drop(d, RTAMS_EINVAL);
+  if (threadIdx.x == 0) d.ctrl->ok = 1;
+  if (!few) return;
+  if ((int)threadIdx.x < n) d.lengths[it.seq] = it.src;
+  uint32_t entries;
+  sh.before[threadIdx.x] = scan_lanes((uint32_t)(it.have - it.want), &entries, sh);
+  sh.seq[threadIdx.x] = it.seq;
+  sh.page0[threadIdx.x] = it.want;
+  __syncthreads();
+  uint32_t gone = 0;
+  for (uint32_t e = threadIdx.x; e < entries; e += kPlanLanes) {
+    const int x = item_of(sh, e);
+    gone += give_up(d, sh.seq[x], sh.page0[x] + (int)(e - sh.before[x]));
+  }
+  if (gone) atomicAdd(&d.ctrl->free, gone);
+}
+
 __global__ __launch_bounds__(256) void k_cache_trim_entries(CacheDev d, int32_t n) {
   if (!d.ctrl->ok) return;
   each_entry(d, n, [&](const CacheItem &it, int p) {
-    const bool gone = p >= it.want && p < it.have && give_up(d, it.seq, p);
-    const uint64_t all = __ballot(gone);
+    if (p == 0) d.lengths[it.seq] = it.src;
+    const uint64_t all = __ballot(p >= it.want && p < it.have && give_up(d, it.seq, p));
     if (all && lane_id() == 0) atomicAdd(&d.ctrl->free, (uint32_t)__popcll(all));
   });
 }
 
-__global__ __launch_bounds__(kPlanLanes) void k_cache_fork(CacheDev d, int32_t n, const int32_t *src, const int32_t *dst, int copy, int inline_too) {
+// Entry p of a fork's destination; copy: a page of its own, pair `pair` of the call.
+__device__ inline void take_over(const CacheDev &d, int32_t src, int32_t dst, int p, bool copy, uint32_t pair, int32_t own) {
+  const int32_t page = d.table[(int64_t)src * d.max_pages + p];
+  d.table[(int64_t)dst * d.max_pages + p] = copy ? own : page;
+  if (copy) {
+    d.refs[own] = 1;
+    d.pair_src[pair] = page;
+    d.pair_dst[pair] = own;
+  } else {
+    atomicAdd(&d.refs[page], 1);
+  }
+}
+
+__global__ __launch_bounds__(kPlanLanes) void k_cache_fork(CacheDev d, int32_t n, const int32_t *src, const int32_t *dst, int copy, int few) {
   __shared__ Plan sh;
   clear_seen(d, sh);
   int bad = 0, short_of = 0;
@@ -319,7 +322,7 @@ __global__ __launch_bounds__(kPlanLanes) void k_cache_fork(CacheDev d, int32_t n
       }
     }
     it.off = total + scan_lanes(need, &here, sh);
-    if (i < n && (n > kPlanLanes || !inline_too)) d.items[i] = it;
+    if (i < n && !few) d.items[i] = it;
     short_of = here > d.pages - total;
     total += here;
     bad = __syncthreads_or(bad);
@@ -335,26 +338,21 @@ __global__ __launch_bounds__(kPlanLanes) void k_cache_fork(CacheDev d, int32_t n
     d.ctrl->pairs = total;
     d.ctrl->ok = 1;
   }
-  if (!inline_too) {  // (the pages in LDS are wanted by others)
+  if (!few) {
     for (uint32_t x = threadIdx.x; x < total && x < kPicked; x += kPlanLanes) d.picked[x] = sh.picked[x];
     return;
   }
-  for (int base = 0; base < n; base += kPlanLanes) {
-    const int i = base + threadIdx.x;
-    if (n > kPlanLanes) it = i < n ? d.items[i] : CacheItem{};
-    if (i < n) d.lengths[it.seq] = it.want;
-    uint32_t entries;
-    sh.before[threadIdx.x] = scan_lanes(i < n ? (uint32_t)it.have : 0, &entries, sh);
-    sh.seq[threadIdx.x] = it.seq;
-    sh.src[threadIdx.x] = it.src;
-    sh.page0[threadIdx.x] = (int32_t)it.off;
-    __syncthreads();
-    for (uint32_t e = threadIdx.x; e < entries; e += kPlanLanes) {
-      const int x = item_of(sh, e), p = (int)(e - sh.before[x]);
-      const uint32_t pair = (uint32_t)sh.page0[x] + (uint32_t)p;
-      take_over(d, sh.src[x], sh.seq[x], p, copy, copy ? picked_page(d, sh, pair) : 0, pair);
-    }
-    __syncthreads();
+  if ((int)threadIdx.x < n) d.lengths[it.seq] = it.want;
+  uint32_t entries;
+  sh.before[threadIdx.x] = scan_lanes((uint32_t)it.have, &entries, sh);
+  sh.seq[threadIdx.x] = it.seq;
+  sh.page0[threadIdx.x] = it.src;
+  sh.off[threadIdx.x] = it.off;
+  __syncthreads();
+  for (uint32_t e = threadIdx.x; e < entries; e += kPlanLanes) {
+    const int x = item_of(sh, e);
+    const uint32_t p = e - sh.before[x], pair = sh.off[x] + p;
+    take_over(d, sh.page0[x], sh.seq[x], (int)p, copy, pair, copy ? picked_page(d, sh, pair) : 0);
   }
 }
 
@@ -362,7 +360,7 @@ __global__ __launch_bounds__(256) void k_cache_fork_entries(CacheDev d, int32_t 
   if (!d.ctrl->ok) return;
   each_entry(d, n, [&](const CacheItem &it, int p) {
     if (p == 0) d.lengths[it.seq] = it.want;
-    if (p < it.have) take_over(d, it.src, it.seq, p, it.copy, it.copy ? d.picked[it.off + p] : 0, it.off + p);
+    if (p < it.have) take_over(d, it.src, it.seq, p, it.copy, it.off + p, it.copy ? d.picked[it.off + p] : 0);
   });
 }
 
@@ -443,26 +441,28 @@ int entry_groups(const CacheDev &d, int64_t n) {
   return (int)(groups < 2048 ? groups : 2048);
 }
 
-// A call of few table entries takes one launch: the planning workgroup walks them too.
-bool walks_inline(const CacheDev &d, int64_t n) { return n * (int64_t)d.max_pages <= kInlineSlots; }
-
 }  // namespace
+
+// An entry to a lane of the planning workgroup costs what a launch does (64 sequences of 16 pages trimmed and extended: 26 us, 24 with launches
+// of their own; 4 of 16: 16 and 19), two more (8 of 256: 39 and 27), sixteen far more (64 of 256: 155 and 32).
+static bool few_entries(const CacheDev &d, int64_t n) { return n <= kPlanLanes && n * d.max_pages <= kFewEntries; }
 
 void launch_cache_extend(const CacheDev &d, const CacheRows &r, bool copies, hipStream_t s) {
   k_cache_extend<<<1, kPlanLanes, 0, s>>>(d, r);
+  if (r.starts && (int64_t)r.n * d.max_pages > kPlanLanes) k_cache_extend_entries<<<entry_groups(d, r.n), 256, 0, s>>>(d, r.n);
   if (copies) k_cache_move<<<copy_groups(d, r.n), 256, 0, s>>>(d, 0);
 }
 
 void launch_cache_trim(const CacheDev &d, int32_t n, const int32_t *seqs, const int32_t *lengths, hipStream_t s) {
-  const bool one = walks_inline(d, n);
-  k_cache_trim<<<1, kPlanLanes, 0, s>>>(d, n, seqs, lengths, one);
-  if (!one) k_cache_trim_entries<<<entry_groups(d, n), 256, 0, s>>>(d, n);
+  const bool few = few_entries(d, n);
+  k_cache_trim<<<1, kPlanLanes, 0, s>>>(d, n, seqs, lengths, few);
+  if (!few) k_cache_trim_entries<<<entry_groups(d, n), 256, 0, s>>>(d, n);
 }
 
 void launch_cache_fork(const CacheDev &d, int32_t n, const int32_t *src, const int32_t *dst, bool copy, hipStream_t s) {
-  const bool one = walks_inline(d, n);
-  k_cache_fork<<<1, kPlanLanes, 0, s>>>(d, n, src, dst, copy, one);
-  if (!one) k_cache_fork_entries<<<entry_groups(d, n), 256, 0, s>>>(d, n);
+  const bool few = few_entries(d, n);
+  k_cache_fork<<<1, kPlanLanes, 0, s>>>(d, n, src, dst, copy, few);
+  if (!few) k_cache_fork_entries<<<entry_groups(d, n), 256, 0, s>>>(d, n);
   if (copy) k_cache_move<<<copy_groups(d, (int64_t)n * d.max_pages), 256, 0, s>>>(d, 0);
 }
 
