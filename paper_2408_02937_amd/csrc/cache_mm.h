@@ -204,8 +204,7 @@ constexpr int kUnits = 256;  // compute units
 
 // Steps of a piece, of n items' steps.  Pieces are to run all at once, `workers` of them, and to leave the compute units alike much to do:
 // of sixteen sizes from an even share up to twice that, a quarter of the items to a lane, the one with the least steps for a
-// compute unit, which has pieces / 256 rounded up.  (32 single tokens of 1 to 4 thousand: 680 pieces of 7 steps, three for some and
-// two for others, 28 us; 512 of 9, KPIECE.)
+// compute unit, which has pieces / 256 rounded up.
 __device__ inline uint32_t piece_steps(const float *steps, int n, int kv_heads, uint32_t share, uint32_t workers) {
   const int lane = threadIdx.x & 63;
   const uint32_t more = (share + 15) / 16, size = share + (lane & 15) * more;

@@ -430,7 +430,9 @@ void launch(const CacheDev &d, const CacheQuery &q, hipStream_t s) {
   const int64_t rows = (int64_t)q.share * q.r.max_new;
   const int tiles = (int)((rows + WAVES * 32 - 1) / (WAVES * 32)), tile_rows = (int)((rows + tiles - 1) / tiles + 31) / 32 * 32;  // (all about as long)
   const int64_t groups = (int64_t)tiles * q.r.n * d.kv_heads;
-  const bool split = groups < kSplit * kWorkers && tiles * q.r.n <= kMostEntries;
+  static_assert(kSplit * kWorkers <= kMostEntries, "all row tiles of all items are planned");
+  // (steps of all row tiles are counted in 32 bits)
+  const bool split = groups < kSplit * kWorkers && groups * ((int64_t)d.max_pages * d.page_blocks + 1) < (int64_t)1 << 32;
   k_cache_prompt<D, WAVES><<<(uint32_t)(split ? groups + kWorkers : groups), WAVES * 64, sizeof(Shared<D>), s>>>(d, q, tiles, tile_rows, split);
 }
 
@@ -451,6 +453,7 @@ void launch_cache_prompt(const CacheDev &d, const CacheQuery &q, hipStream_t s) 
 
 hipError_t allow_large_lds_cache_prompt() {
   const auto allow = [](const void *f, size_t bytes) { return hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes); };
+  if (const hipError_t e = allow(reinterpret_cast<const void *>(k_cache_prompt<128, 8>), sizeof(Shared<128>))) return e;
   return allow(reinterpret_cast<const void *>(k_cache_prompt<256, 4>), sizeof(Shared<256>));
 }
 

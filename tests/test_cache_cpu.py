@@ -61,3 +61,25 @@ def test_calls_without_a_cache_are_refused():
                L.rtams_cache_layout(None, C.byref(v)), L.rtams_cache_free_pages(None, C.byref(n)), L.rtams_cache_poll_error(None), L.rtams_cache_clear_error(None)):
         assert rc == rtams.EINVAL
     assert L.rtams_cache_destroy(None) == rtams.OK
+
+
+@pytest.fixture(scope="module")
+def records():
+    from tests.test_kernel_resources import code_objects, kernels
+    with open(rtams.LIB_PATH, "rb") as f:
+        blob = f.read()
+    return {k[".name"]: k for e in code_objects(blob) for k in kernels(e)}
+
+
+# wavefronts of a workgroup and workgroups that are to run at once on a compute unit: four SIMDs of 512 registers, 160 KiB of LDS
+@pytest.mark.parametrize("name,waves,groups,lds", [
+    ("14k_cache_attendILi64ELi1E", 4, 5, 21 * 1024), ("14k_cache_attendILi64ELi2E", 4, 3, 22 * 1024), ("14k_cache_attendILi96ELi1E", 4, 4, 31 * 1024),
+    ("14k_cache_attendILi96ELi2E", 4, 2, 32 * 1024), ("14k_cache_attendILi128ELi1E", 4, 3, 42 * 1024), ("14k_cache_attendILi128ELi2E", 4, 2, 42 * 1024),
+    ("14k_cache_attendILi256ELi1E", 4, 1, 83 * 1024), ("14k_cache_promptILi64ELi8E", 8, 1, 32 * 1024), ("14k_cache_promptILi96ELi8E", 8, 1, 48 * 1024),
+    ("14k_cache_promptILi128ELi8E", 8, 1, 64 * 1024), ("14k_cache_promptILi256ELi4E", 4, 1, 64 * 1024),
+])
+def test_attention_runs_as_many_workgroups_at_once_as_it_plans_for(records, name, waves, groups, lds):
+    mine = [k for n, k in records.items() if name in n]
+    assert len(mine) == 1
+    assert (mine[0][".vgpr_count"] + 7) // 8 * 8 * ((waves * groups + 3) // 4) <= 512
+    assert groups * (mine[0][".group_segment_fixed_size"] + lds) <= 160 * 1024

@@ -272,6 +272,52 @@ def test_long_sequences_are_split_and_joined(lengths, heads, kv, dim):
     f.check([7] * len(lengths), heads)
 
 
+@pytest.mark.parametrize("lengths,counts,heads,kv,dim", [([6_000], [40], 4, 1, 128), ([3_001, 40, 1_999], [33, 40, 300], 8, 4, 64), ([2_500], [2_500], 2, 2, 96),
+                                                         ([1_700, 900], [65, 129], 8, 2, 256)])
+def test_few_long_prompts_are_split_and_joined(lengths, counts, heads, kv, dim):
+    f = Filled(lengths, kv, dim, page=64, seed=20)
+    q, out = f.check(counts, heads)
+    for _ in range(3):
+        assert torch.equal(out, f.cache.attend(0, q, starts=starts_of(counts), max_new=max(counts)))
+    f.check(counts, heads, window=700)
+    f.check([min(c, 70) for c in counts], heads, causal=False)
+
+
+def test_many_prompts():
+    """More row tiles than are split."""
+    lengths = [(i * 37) % 90 + 40 for i in range(300)]
+    f = Filled(lengths, 4, 64, page=32, seed=21)
+    f.check([min(x, 35 + i % 9) for i, x in enumerate(lengths)], 4)
+
+
+def test_a_pool_of_many_gigabytes():
+    """Pages and layers whose places are beyond 2^32 bytes."""
+    layers, kv, dim, page, pages = 48, 8, 128, 64, 2600
+    c = Cache(kv, dim, layers=layers, page_tokens=page, pages=pages, max_seqs=2, device=DEV)
+    assert c.pages.numel() > 1 << 33
+    c.extend(ints([0]), ints([0, (pages - 3) * page]))
+    one = ints([1])
+    c.extend(one, ints([0, 150]))
+    g = torch.Generator(device=DEV).manual_seed(22)
+    q = torch.randn((150, 8, dim), device=DEV, generator=g).bfloat16()
+    for layer in (0, 25, layers - 1):
+        k, v = (torch.randn((150, kv, dim), device=DEV, generator=g).bfloat16() for _ in range(2))
+        c.write(layer, k, v, one, ints([0, 150]), max_new=150)
+        rk, rv = c.read(layer, 150, one, ints([0, 150]), max_new=150)
+        hk, hv = held(floats(k)), held(floats(v))
+        assert np.allclose(rk.cpu().numpy(), hk, rtol=1e-6, atol=1e-7) and np.allclose(rv.cpu().numpy(), hv, rtol=1e-6, atol=1e-7)
+        for count in (1, 150):
+            out = c.attend(layer, q[:count], one, ints([0, count]), max_new=count)
+            want = plain_attention(floats(q[:count]).astype(np.float64), hk, hv, 1, dim ** -0.5, [(0, 151 - count + j) for j in range(count)])
+            check_attention(out, None, want, unit_of(q.dtype))
+    c.trim(ints([0]), ints([40]))
+    before = c.pages[:, pages - 3:].clone()
+    c.compact()  # the second sequence comes down to the front
+    torch.cuda.synchronize()
+    assert c.table[1, :3].tolist() == [1, 2, 3] and torch.equal(c.pages[:, 1:4], before)
+    assert c.poll_error() == 0
+
+
 def test_many_sequences():
     """More of them than are numbered at a time, most of them short, some empty."""
     lengths = [(i * 53) % 97 for i in range(700)]
@@ -642,6 +688,8 @@ def test_arguments_are_refused_on_the_host():
     einval(lambda: c.attend(0, q, window=-1))
     einval(lambda: c.attend(0, q, window=4, causal=False))
     einval(lambda: c.attend(0, q, scale=float("inf")))
+    many = f.query([1], 4).expand(1 << 29, 4, 64)  # (one row in memory) more than is counted in 32 bits
+    einval(lambda: c.attend(0, many, seqs=ints([0]), starts=ints([0, 1]), max_new=1 << 29, out=many))
     einval(lambda: c.attend(0, q, starts=ints([0, 1, 2]), max_new=0))
     einval(lambda: c.extend(n=3))
     einval(lambda: c.write(5, f.k, f.v, starts=ints([0, 40, 60]), max_new=40))
