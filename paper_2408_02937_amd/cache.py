@@ -143,6 +143,8 @@ class Cache:
         n, sp, tp, max_new = self._items(seqs, starts, rows if seqs is None and starts is None else None, max_new)
         k = torch.empty((rows, self.kv_heads, self.head_dim), dtype=dtype, device=self.device)
         v = torch.empty_like(k)
+        if stream is not None:
+            k.record_stream(stream), v.record_stream(stream)
         _chk(self._lib.rtams_cache_read(self._h, layer, n, sp, tp, rows, max_new, k.data_ptr(), v.data_ptr(), _TYPES[dtype], self._stream(stream)),
              "rtams_cache_read")
         return k, v
@@ -157,6 +159,8 @@ class Cache:
         n, sp, tp, max_new = self._items(seqs, starts, rows if seqs is None and starts is None else None, max_new)
         if out is None:
             out = q.new_empty((rows, heads, self.head_dim))
+            if stream is not None:
+                out.record_stream(stream)  # (it comes from the current stream's memory)
         elif self._rows(out, heads, "out").shape != q.shape or out.dtype != q.dtype:
             raise ValueError("out must have the shape and type of q")
         lp = None
