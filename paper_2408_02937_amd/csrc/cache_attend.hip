@@ -5,9 +5,13 @@
 // Bound by the bytes of the cache: 1.25 a channel and token for keys and values together.  A step of a workgroup is 128 tokens of
 // one kv head, 32 to a wavefront; a workgroup takes a piece of a head's steps, of a size that lets all pieces run at once, so
 // that ragged lengths fill the chip alike.  The query heads that share a kv head (times an item's rows) are the 16 columns of
-// the matrix instructions.  Codes become halves in registers, straight from the loads: scores come out as S^T = K Q^T,
-// tokens down and rows across, which is the operand that O^T = V^T P^T takes, so nothing is transposed and LDS only joins
-// the wavefronts.  What a piece leaves of a row goes to scratch; the last piece of it to arrive joins them, in order.
+// the matrix instructions, of one tile or two.  A wavefront copies its blocks into LDS of its own, the next one while it works on this one;
+// codes become halves in registers.  Scores come out as S^T = K Q^T, tokens down and rows across, which is the operand that O^T = V^T P^T
+// takes, so nothing is transposed.  What a piece leaves of a row goes to scratch; the last piece of it to arrive joins them, in order.
+//
+// Measured: 8 sequences of 16 to 131 thousand tokens, 8 heads of 128, 32 query heads: 170 us for 874 MB, 5.1 TB/s where a plain read of 4 GiB reaches
+// 6.0.  32 of 0.5 to 4 thousand: 26.6 us for 94 MB; of these 3 are the plan, 5 pass until the first blocks are there, 3 are the join.
+// One token over 100: 5.7 us.  Heads of 64, 96, 128, 256 channels, 8 times 32,000 tokens each: 4.4, 5.0, 5.0, 5.0 TB/s.
 #include "../../include/rtams_cache.h"
 
 #include "cache_mm.h"
@@ -19,7 +23,7 @@ namespace {
 
 constexpr int kLanes = 256, kWaves = 4, kStep = kWaves * kBlockTokens;
 
-// Workgroups that a compute unit runs at once: registers decide, and from 128 channels on LDS.
+// Workgroups that a compute unit runs at once: registers decide, and from 128 channels on LDS (40 * D * 8 bytes of blocks).
 constexpr int at_once(int head_dim, int tiles) {
   return tiles == 2 ? (head_dim == 64 ? 3 : 2) : head_dim == 64 ? 5 : head_dim == 96 ? 4 : head_dim == 128 ? 3 : 1;
 }
@@ -27,12 +31,13 @@ constexpr int at_once(int head_dim, int tiles) {
 struct Span {  // what an item asks for
   int seq, count, length, low;  // low: first position that a row of it sees, rounded down to a block
   int steps;
+  int tiles;  // of its rows
   int64_t row0;
 };
 
 // Items i + 64 k of the launch, for k of 0 .. N - 1; steps 0 behind the last one.  Loads are asked for together, whatever they find: each is
 // a trip to memory, at the beginning of a launch.
-template <int N>
+template <int N, int ROWS>
 __device__ inline void find_spans(const CacheDev &d, const CacheQuery &q, int i, bool tell, Span (&s)[N]) {
   const int n = q.r.n;
   int first[N], past[N], seq[N], length[N];
@@ -61,16 +66,17 @@ __device__ inline void find_spans(const CacheDev &d, const CacheQuery &q, int i,
     const int low = length[k] - s[k].count - q.window + 1;
     s[k].low = q.window && low > 0 ? low & ~(kBlockTokens - 1) : 0;
     s[k].steps = s[k].count <= 0 ? 0 : length[k] > s[k].low ? (length[k] - s[k].low + kStep - 1) / kStep : 1;
+    s[k].tiles = (q.share * s[k].count + ROWS - 1) / ROWS;
   }
 }
 
 constexpr int kAhead = 2;   // blocks of a wavefront that are in LDS or on their way
 
-struct Piece {  // steps [sa, sb) of an item's head
+struct Piece {  // steps [sa, sb) of a row tile of an item's head
   Span sp;
-  int item, head, sa, sb;
-  int parts, nth;  // pieces of the head; which one this is
-  int part;        // where the head's parts begin, if there are several
+  int item, head, tile, sa, sb;
+  int parts, nth;  // pieces of the tile; which one this is
+  int part;        // where the tile's parts begin, if there are several
 };
 
 constexpr int kRound = 256;  // items that the planning wavefront has at a time, four to a lane at most
@@ -89,39 +95,42 @@ struct alignas(16) Shared {
 
 // Which piece is workgroup blockIdx.x's: the items' steps, the size of a piece, and the pieces of the items in front.  One wavefront's work, EACH
 // items to a lane (lane, lane + 64, ...); false where there is none left.
-template <int EACH, class S>
-__device__ bool find_piece(const CacheDev &d, const CacheQuery &q, uint32_t workers, S &sh) {
+template <int EACH, int ROWS, class S>
+__device__ bool find_piece(const CacheDev &d, const CacheQuery &q, int tiles, uint32_t workers, S &sh) {
   constexpr int kItems = 64 * EACH;
   const int lane = threadIdx.x & 63, n = q.r.n;
   Span sp[EACH];
   uint32_t all = 0;
   for (int base = 0; base < n; base += kItems) {
-    find_spans<EACH>(d, q, base + lane, blockIdx.x == 0, sp);
+    find_spans<EACH, ROWS>(d, q, base + lane, blockIdx.x == 0, sp);
     uint32_t sum = 0;
 #pragma unroll
-    for (int k = 0; k < EACH; ++k) sum += (uint32_t)sp[k].steps;
+    for (int k = 0; k < EACH; ++k) sum += (uint32_t)(sp[k].steps * sp[k].tiles);
     all += last_lane(wave_running_sum(sum));
   }
   all *= (uint32_t)d.kv_heads;
   // where items are many, pieces are an even share at most, and long items do not keep the others waiting
   const uint32_t share = (all + workers - 1) / workers;
   uint32_t size = share > 1 ? share : 1;
-  if (share > 1 && n <= kItems && n * d.kv_heads <= (int)workers / 2) {
+  if (share > 1 && n <= kItems && n * d.kv_heads * tiles <= (int)workers / 2) {
 #pragma unroll
     for (int k = 0; k < EACH; ++k) sh.steps[64 * k + lane] = (float)sp[k].steps;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    size = piece_steps(sh.steps, n, d.kv_heads, share, workers);
+    size = piece_steps(sh.steps, n, d.kv_heads * tiles, share, workers);
   }
   const float one_over = 1.0f / (float)size;
   uint32_t before = 0, parts_before = 0;
   for (int base = 0; base < n; base += kItems) {
-    if (n > kItems) find_spans<EACH>(d, q, base + lane, false, sp);
+    if (n > kItems) find_spans<EACH, ROWS>(d, q, base + lane, false, sp);
 #pragma unroll
     for (int k = 0; k < EACH; ++k) {
-      const uint32_t parts = div_up((uint32_t)sp[k].steps, size, one_over), pieces = parts * (uint32_t)d.kv_heads, shared = parts > 1 ? pieces : 0;
+      const uint32_t parts = div_up((uint32_t)sp[k].steps, size, one_over), pieces = parts * (uint32_t)(d.kv_heads * sp[k].tiles), shared = parts > 1 ? pieces : 0;
       const uint32_t upto = wave_running_sum(pieces), upto_shared = wave_running_sum(shared), x = blockIdx.x - (before + upto - pieces);
-      if (x < pieces)
-        sh.piece = Piece{sp[k], base + 64 * k + lane, (int)(x / parts), 0, 0, (int)parts, (int)(x % parts), (int)(parts_before + upto_shared - shared + x - x % parts)};
+      if (x < pieces) {  // (row tiles fastest: they read the same tokens)
+        const uint32_t t = x % (uint32_t)sp[k].tiles, y = x / (uint32_t)sp[k].tiles, head = y / parts;
+        sh.piece = Piece{sp[k], base + 64 * k + lane, (int)head, (int)t, 0, 0, (int)parts, (int)(y % parts),
+                         (int)(parts_before + upto_shared - shared + (head * sp[k].tiles + t) * parts)};
+      }
       if (__any(x < pieces)) return true;
       before += last_lane(upto);
       parts_before += last_lane(upto_shared);
@@ -163,28 +172,28 @@ struct Copies {
 };
 
 template <int D, int NR>
-__global__ __launch_bounds__(kLanes, at_once(D, NR)) void k_cache_attend(CacheDev d, CacheQuery q) {
+__global__ __launch_bounds__(kLanes, at_once(D, NR)) void k_cache_attend(CacheDev d, CacheQuery q, int tiles) {
   constexpr int NJ = D / 32, NT = D / 16;
   extern __shared__ uint4 lds[];
   Shared<D, NR> &sh = *reinterpret_cast<Shared<D, NR> *>(lds);
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 15, b = lane >> 4;
 
   if (wave == 0) {
-    const bool found = q.r.n <= 64 ? find_piece<1>(d, q, kUnits * at_once(D, NR), sh) : find_piece<kRound / 64>(d, q, kUnits * at_once(D, NR), sh);
+    const bool found = q.r.n <= 64 ? find_piece<1, 16 * NR>(d, q, tiles, kUnits * at_once(D, NR), sh) : find_piece<kRound / 64, 16 * NR>(d, q, tiles, kUnits * at_once(D, NR), sh);
     if (lane == 0) sh.last = found;
   }
   __syncthreads();
   if (!sh.last) return;
   Piece pc = sh.piece;
-  const Span sp{uniform(pc.sp.seq), uniform(pc.sp.count), uniform(pc.sp.length), uniform(pc.sp.low), uniform(pc.sp.steps),
+  const Span sp{uniform(pc.sp.seq), uniform(pc.sp.count), uniform(pc.sp.length), uniform(pc.sp.low), uniform(pc.sp.steps), uniform(pc.sp.tiles),
                 (int64_t)uniform((int)((uint64_t)pc.sp.row0 >> 32)) << 32 | (uint32_t)uniform((int)pc.sp.row0)};
-  pc = Piece{sp, uniform(pc.item), uniform(pc.head), 0, 0, uniform(pc.parts), uniform(pc.nth), uniform(pc.part)};
+  pc = Piece{sp, uniform(pc.item), uniform(pc.head), uniform(pc.tile), 0, 0, uniform(pc.parts), uniform(pc.nth), uniform(pc.part)};
   {  // steps in as many equal pieces, the first ones one longer
     const int each = sp.steps / pc.parts, longer = sp.steps - each * pc.parts;
     pc.sa = each * pc.nth + min(pc.nth, longer);
     pc.sb = pc.sa + each + (pc.nth < longer);
   }
-  const int rows = q.share * sp.count, head = pc.head, first_tok = sp.low + pc.sa * kStep + wave * kBlockTokens;
+  const int row_first = pc.tile * 16 * NR, rows = min(16 * NR, q.share * sp.count - row_first), head = pc.head, first_tok = sp.low + pc.sa * kStep + wave * kBlockTokens;
   Copies<D> cp;
   cp.table = (ScalarInts)(uintptr_t)(d.table + (int64_t)sp.seq * d.max_pages);
   cp.head = head;
@@ -202,7 +211,7 @@ __global__ __launch_bounds__(kLanes, at_once(D, NR)) void k_cache_attend(CacheDe
   for (int t = 0; t < NR; ++t) {
     const int row = t * 16 + col;
     const bool real = row < rows;
-    const int j = real ? row / q.share : 0, h = real ? row % q.share : 0;
+    const int j = real ? (row_first + row) / q.share : 0, h = real ? (row_first + row) % q.share : 0;
     const int pos = sp.length - sp.count + j;
     see_to[t] = q.causal ? pos + 1 : sp.length;
     see_from[t] = q.window ? pos - q.window + 1 : 0;
@@ -326,7 +335,7 @@ __global__ __launch_bounds__(kLanes, at_once(D, NR)) void k_cache_attend(CacheDe
         v += *reinterpret_cast<const f32x4 *>(&sh.o[w][r][c]);
       }
       if (pc.parts == 1) {
-        store_row(q, sp.row0 + row / q.share, head * q.share + row % q.share, c, v, top, sum);
+        store_row(q, sp.row0 + (row_first + row) / q.share, head * q.share + (row_first + row) % q.share, c, v, top, sum);
       } else {
         put_pair(part + row * D + c, v[0], v[1]);
         put_pair(part + row * D + c + 2, v[2], v[3]);
@@ -339,7 +348,7 @@ __global__ __launch_bounds__(kLanes, at_once(D, NR)) void k_cache_attend(CacheDe
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wavefront's part is out ...
   __syncthreads();                                  // ... and that of the others
   if (threadIdx.x == 0) {
-    uint32_t *there = d.arrived + (int64_t)pc.item * d.kv_heads + head;
+    uint32_t *there = d.arrived + ((int64_t)pc.item * d.kv_heads + head) * tiles + pc.tile;
     const bool last = __hip_atomic_fetch_add(there, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)pc.parts - 1;
     if (last) __hip_atomic_store(there, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     sh.last = last;
@@ -350,15 +359,18 @@ __global__ __launch_bounds__(kLanes, at_once(D, NR)) void k_cache_attend(CacheDe
   part_ml = d.part_ml + (int64_t)pc.part * (16 * NR) * 2;
   for (int u = threadIdx.x; u < rows * (D / 4); u += kLanes) {
     const int row = u / (D / 4), c = u % (D / 4) * 4;
-    join_parts(q, sp.row0 + row / q.share, head * q.share + row % q.share, c, pc.parts, part + row * D + c, part_ml + row * 2, D, 16 * NR);
+    join_parts(q, sp.row0 + (row_first + row) / q.share, head * q.share + (row_first + row) % q.share, c, pc.parts, part + row * D + c, part_ml + row * 2, D, 16 * NR);
   }
 }
 
-// (an even share makes no more pieces than run at once, and one more for each head)
+// (an even share makes no more pieces than run at once, and one more for each row tile of a head)
 template <int D, int NR>
-void launch(const CacheDev &d, const CacheQuery &q, hipStream_t s) {
-  k_cache_attend<D, NR><<<(uint32_t)(kUnits * at_once(D, NR) + q.r.n * d.kv_heads), kLanes, sizeof(Shared<D, NR>), s>>>(d, q);
+void launch(const CacheDev &d, const CacheQuery &q, int tiles, hipStream_t s) {
+  k_cache_attend<D, NR><<<(uint32_t)(kUnits * at_once(D, NR) + q.r.n * d.kv_heads * tiles), kLanes, sizeof(Shared<D, NR>), s>>>(d, q, tiles);
 }
+
+// Up to 64 rows; a head's row tiles read its cache one beside the other, and the second finds it in the last-level cache.
+constexpr int kTiles = 4;  // of 16 or 32 rows, at most
 
 }  // namespace
 
@@ -371,18 +383,24 @@ static size_t part_rows(int head_dim) {
 size_t cache_part_floats(int head_dim) { return part_rows(head_dim) * head_dim; }
 size_t cache_part_ml_floats(int head_dim) { return part_rows(head_dim) * 4; }  // (of many rows two lanes have a pair each)
 size_t cache_arrived_words(int max_seqs, int kv_heads) {
-  const size_t few = (size_t)max_seqs * kv_heads, many = cache_prompt_groups();
+  const size_t few = (size_t)max_seqs * kv_heads * kTiles, many = cache_prompt_groups();
   return few > many ? few : many;
 }
 
 void launch_cache_attend(const CacheDev &d, const CacheQuery &q, hipStream_t s) {
+  // Against the kernel for many rows, 8 sequences of up to 32,000 tokens and 8 heads: of 128 channels 32, 40, 64, 96, 128 rows take 69, 111, 108, 159,
+  // 186 us here and 144 to 152 there; of 256 channels 24, 32, 40, 64 rows 201, 203, 370, 425 us and 391 to 403.  32 of up to 2,000, 64 rows: 50 and 51,
+  // of 256 channels 104 and 143.
   const int64_t rows = (int64_t)q.share * q.r.max_new;
-  if (rows > (d.head_dim == 256 ? 16 : 32)) return launch_cache_prompt(d, q, s);
+  const int each = d.head_dim == 256 || rows <= 16 ? 16 : 32;
+  const int64_t tiles = (rows + each - 1) / each;
+  // (steps of all row tiles are counted in 32 bits)
+  if (rows > 64 || (tiles > 1 && q.r.n * d.kv_heads * tiles * ((int64_t)d.max_pages * d.page_blocks / kWaves + 1) >= (int64_t)1 << 32)) return launch_cache_prompt(d, q, s);
   switch (d.head_dim) {
-    case 64: return rows <= 16 ? launch<64, 1>(d, q, s) : launch<64, 2>(d, q, s);
-    case 96: return rows <= 16 ? launch<96, 1>(d, q, s) : launch<96, 2>(d, q, s);
-    case 128: return rows <= 16 ? launch<128, 1>(d, q, s) : launch<128, 2>(d, q, s);
-    default: return launch<256, 1>(d, q, s);
+    case 64: return each == 16 ? launch<64, 1>(d, q, 1, s) : launch<64, 2>(d, q, (int)tiles, s);
+    case 96: return each == 16 ? launch<96, 1>(d, q, 1, s) : launch<96, 2>(d, q, (int)tiles, s);
+    case 128: return each == 16 ? launch<128, 1>(d, q, 1, s) : launch<128, 2>(d, q, (int)tiles, s);
+    default: return launch<256, 1>(d, q, (int)tiles, s);
   }
 }
 

@@ -1,4 +1,3 @@
-#include <climits>
 // Attention of many rows over the cache in 4 bits: prompts, and pieces of prompts behind what the cache already holds.
 //
 // The formulas are those of cache_attend.hip; here arithmetic bounds: 4 * head_dim flops for a row and token.  A workgroup has
@@ -9,7 +8,14 @@
 // only where a score has left it 8 behind.  LDS holds operands in the order in which the lanes take them, 16 bytes each; the slots are
 // swapped so that writing meets no bank twice.  Where rows are too few to fill the chip the tokens are split, and the last
 // part of a row to arrive joins them.
+//
+// Measured: a prompt of 8,192 tokens, 32 heads of 128 over 8: 575 us for 550 GFLOP, 955 TFLOP/s where a plain product of 8,192 squared reaches 1,140
+// in bfloat16 and 1,084 in halves.  Vector work (exponentials, masks, codes) and matrix instructions take 37 % and 36 % of the cycles and
+// share the issue of a SIMD's two wavefronts.  Heads of 64, 96, 256: 613, 626, 357 TFLOP/s: at 64 exponentials are twice as many for a flop; at 256
+// one wavefront fits a SIMD.  4 wavefronts a workgroup at 128 channels: 710 us; wavefronts half a tile apart: 610.
 #include "../../include/rtams_cache.h"
+
+#include <climits>
 
 #include "cache_mm.h"
 #include "rtams_dev.h"
@@ -120,12 +126,16 @@ __device__ inline Span find_span(const CacheDev &d, const CacheQuery &q, int ite
 }
 
 struct Piece {
-  int entry, head;       // entry: item * tiles + tile
+  int entry, head;       // entry: row tiles from the longest on, the items of each
   int parts, nth, part;  // pieces of the head's row tile; which one this is; where its parts begin, if there are several
 };
 
-constexpr int kSplit = 4;           // from so many times the workgroups that run at once tokens are not split
+// From so many times the workgroups that run at once (one item: from as many) nothing is planned.  With a plan and without, 8 heads of 128: 8 items of
+// up to 5,000 tokens and 600 rows 295 and 380 us, 12 of up to 3,000 and 512 rows 213 and 241, 2 of 4,000 and 2,000 rows 161 and 196; all as long 456 and
+// 452, 311 and 301, 220 and 216.  One prompt of 3,000: 101 and 101, of 7,000: 447 and 430.
+constexpr int kSplit = 4;
 constexpr int kMostEntries = 1024;  // row tiles of items that are planned
+constexpr int kClasses = 8;         // of their pieces, by length
 
 template <int D>
 union Shared {
@@ -137,26 +147,35 @@ union Shared {
 __device__ inline bool find_piece(const CacheDev &d, const CacheQuery &q, int tiles, int rows, int step_tokens, uint32_t workers, float *steps, Piece *piece) {
   const int lane = threadIdx.x & 63, n = q.r.n * tiles;
   uint32_t all = 0;
+  float longest = 1.0f;
   for (int base = 0; base < (n + 255) / 256 * 256; base += 64) {
     const int e = base + lane;
-    const Span sp = e < n ? find_span(d, q, e / tiles, e % tiles, rows, step_tokens, blockIdx.x == 0) : Span{};
+    const Span sp = e < n ? find_span(d, q, e % q.r.n, tiles - 1 - e / q.r.n, rows, step_tokens, blockIdx.x == 0) : Span{};
     const int mine = sp.count ? sp.steps : 0;
     steps[e] = (float)mine;
+    longest = fmaxf(longest, (float)mine);
     all += last_lane(wave_running_sum((uint32_t)mine));
   }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) longest = fmaxf(longest, __shfl_xor(longest, o));
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   const uint32_t share = max(1u, (all * (uint32_t)d.kv_heads + workers - 1) / workers), size = share > 1 ? piece_steps(steps, n, d.kv_heads, share, workers) : 1;
-  const float one_over = 1.0f / (float)size;
+  // pieces from the longest on, by eighths: what comes last then fills what is left
+  const float one_over = 1.0f / (float)size, per_class = kClasses / fminf((float)size, longest);
   uint32_t before = 0, parts_before = 0;
-  for (int base = 0; base < n; base += 64) {
-    const int e = base + lane;
-    const uint32_t parts = e < n ? div_up((uint32_t)steps[e], size, one_over) : 0, pieces = parts * (uint32_t)d.kv_heads, shared = parts > 1 ? pieces : 0;
-    const uint32_t upto = wave_running_sum(pieces), upto_shared = wave_running_sum(shared), x = blockIdx.x - (before + upto - pieces);
-    if (x < pieces) *piece = Piece{e, (int)(x / parts), (int)parts, (int)(x % parts), (int)(parts_before + upto_shared - shared + x - x % parts)};
-    if (__any(x < pieces)) return true;
-    before += last_lane(upto);
-    parts_before += last_lane(upto_shared);
-  }
+  for (int c = kClasses; c > 0; --c)
+    for (int base = 0; base < n; base += 64) {
+      const int e = base + lane;
+      const uint32_t mine = e < n ? (uint32_t)steps[e] : 0, parts = div_up(mine, size, one_over);
+      const bool now = parts > 0 && min(kClasses, (int)((float)mine * per_class / (float)parts) + 1) == c;
+      if (!__any(now)) continue;
+      const uint32_t pieces = now ? parts * (uint32_t)d.kv_heads : 0, shared = parts > 1 ? pieces : 0;
+      const uint32_t upto = wave_running_sum(pieces), upto_shared = wave_running_sum(shared), x = blockIdx.x - (before + upto - pieces);
+      if (x < pieces) *piece = Piece{e, (int)(x / parts), (int)parts, (int)(x % parts), (int)(parts_before + upto_shared - shared + x - x % parts)};
+      if (__any(x < pieces)) return true;
+      before += last_lane(upto);
+      parts_before += last_lane(upto_shared);
+    }
   return false;
 }
 
@@ -195,9 +214,9 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(C
     __syncthreads();
   } else {  // heads fastest (a head's cache stays on one die), then the items, and the row tiles from the longest on
     const uint32_t x = blockIdx.x / d.kv_heads;
-    pc = Piece{(int)(x % q.r.n) * tiles + tiles - 1 - (int)(x / q.r.n), (int)(blockIdx.x % d.kv_heads), 1, 0, 0};
+    pc = Piece{(int)x, (int)(blockIdx.x % d.kv_heads), 1, 0, 0};
   }
-  const int item = pc.entry / tiles, tile = pc.entry % tiles, head = pc.head;
+  const int item = pc.entry % q.r.n, tile = tiles - 1 - pc.entry / q.r.n, head = pc.head;
   const Span sp = find_span(d, q, item, tile, tile_rows, kTile, !split && tile == 0 && head == 0 && threadIdx.x == 0);
   const int count = uniform(sp.count);
   if (!count) return;
@@ -432,7 +451,7 @@ void launch(const CacheDev &d, const CacheQuery &q, hipStream_t s) {
   const int64_t groups = (int64_t)tiles * q.r.n * d.kv_heads;
   static_assert(kSplit * kWorkers <= kMostEntries, "all row tiles of all items are planned");
   // (steps of all row tiles are counted in 32 bits)
-  const bool split = groups < kSplit * kWorkers && groups * ((int64_t)d.max_pages * d.page_blocks + 1) < (int64_t)1 << 32;
+  const bool split = groups < (q.r.n > 1 ? kSplit : 1) * kWorkers && groups * ((int64_t)d.max_pages * d.page_blocks + 1) < (int64_t)1 << 32;
   k_cache_prompt<D, WAVES><<<(uint32_t)(split ? groups + kWorkers : groups), WAVES * 64, sizeof(Shared<D>), s>>>(d, q, tiles, tile_rows, split);
 }
 

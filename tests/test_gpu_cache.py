@@ -283,6 +283,35 @@ def test_few_long_prompts_are_split_and_joined(lengths, counts, heads, kv, dim):
     f.check([min(c, 70) for c in counts], heads, causal=False)
 
 
+@pytest.mark.parametrize("lengths,counts,heads,kv,dim", [([5_000, 40, 0, 9_001], [5, 1, 0, 8], 16, 2, 128), ([7_000], [64], 1, 1, 64), ([900, 3_100, 33], [11, 2, 16], 4, 1, 96),
+                                                         ([12_345, 64], [4, 1], 32, 2, 256), ([6_001], [2], 32, 1, 256)])
+def test_row_tiles_of_some_tokens(lengths, counts, heads, kv, dim):
+    """33 to 64 rows of a head, 17 to 64 of the widest, and fewer of other items of the call."""
+    f = Filled(lengths, kv, dim, page=64, seed=23)
+    q, out = f.check(counts, heads)
+    for _ in range(3):
+        assert torch.equal(out, f.cache.attend(0, q, starts=starts_of(counts), max_new=max(counts)))
+    f.check(counts, heads, window=300)
+    f.check([c and max(c - 1, 1) for c in counts], heads, causal=False)
+
+
+@pytest.mark.parametrize("n", [90, 300])
+def test_row_tiles_of_many_sequences(n):
+    lengths = [(i * 53) % 97 for i in range(n)]
+    f = Filled(lengths, 1, 64, page=32, seed=24)
+    f.check([min(x, i % 6) for i, x in enumerate(lengths)], 12)
+    f.check([i % 6 for i in range(n)], 12, causal=False)
+
+
+@pytest.mark.parametrize("lengths,count,heads", [([1_200, 300, 2_500, 64, 700], 300, 4), ([3_300], 3_300, 1), ([2_000] * 3, 150, 8)])
+def test_pieces_of_all_lengths(lengths, count, heads):
+    """Row tiles that are far from alike are taken from the longest on, none is left out."""
+    f = Filled(lengths, 4 if heads == 4 else 1, 64, page=64, seed=25)
+    counts = [min(x, count) for x in lengths]
+    f.check(counts, heads)
+    f.check(counts, heads, window=100)
+
+
 def test_many_prompts():
     """More row tiles than are split."""
     lengths = [(i * 37) % 90 + 40 for i in range(300)]
