@@ -324,6 +324,11 @@ int rtams_cache_attend(rtams_cache *c, const rtams_cache_query *q, int64_t n, co
   k.causal = q->causal != 0;
   k.window = q->window;
   k.scale_log2 = q->scale * 1.4426950408889634f;
+  int twos = 0;
+  const double times = (double)q->scale * 1.4426950408889634;
+  std::frexp(times, &twos);
+  k.scale_two = times == 0.0 ? 0.0f : (float)std::copysign(std::ldexp(1.0, twos - 1 < 127 ? twos - 1 : 127), times);
+  k.scale_rest = k.scale_two == 0.0f ? 1.0f : (float)(times / k.scale_two);
   k.q = static_cast<const uint16_t *>(q->d_q);
   k.q_row = q->q_row_stride;
   k.q_head = q->q_head_stride;

@@ -7,7 +7,8 @@
 // that ragged lengths fill the chip alike.  The query heads that share a kv head (times an item's rows) are the 16 columns of
 // the matrix instructions, of one tile or two.  A wavefront copies its blocks into LDS of its own, the next one while it works on this one;
 // codes become halves in registers.  Scores come out as S^T = K Q^T, tokens down and rows across, which is the operand that O^T = V^T P^T
-// takes, so nothing is transposed.  What a piece leaves of a row goes to scratch; the last piece of it to arrive joins them, in order.
+// takes, so nothing is transposed.  A query is a half as it is, times a power of two; what is left of the scale meets the scores in 32 bits, in the
+// same instruction that takes the maximum off.  What a piece leaves of a row goes to scratch; the last piece of it to arrive joins them, in order.
 //
 // Measured: 8 sequences of 16 to 131 thousand tokens, 8 heads of 128, 32 query heads: 170 us for 874 MB, 5.1 TB/s where a plain read of 4 GiB reaches
 // 6.0.  32 of 0.5 to 4 thousand: 26.6 us for 94 MB; of these 3 are the plan, 5 pass until the first blocks are there, 3 are the join.
@@ -217,7 +218,7 @@ __global__ __launch_bounds__(kLanes, at_once(D, NR)) void k_cache_attend(CacheDe
     see_from[t] = q.window ? pos - q.window + 1 : 0;
     const uint16_t *p = q.q + (sp.row0 + j) * q.q_row + (int64_t)(head * q.share + h) * q.q_head + b * (D / 4);
 #pragma unroll
-    for (int x = 0; x < NJ; ++x) qf[t][x] = real ? load_query(p + 8 * x, q.half_type, q.vec, q.scale_log2) : half8{};
+    for (int x = 0; x < NJ; ++x) qf[t][x] = real ? load_query(p + 8 * x, q.half_type, q.vec, q.scale_two) : half8{};
   }
   const int all_to = q.causal ? sp.length - sp.count + 1 : sp.length;     // every row sees [all_from, all_to)
   const int all_from = q.window ? sp.length - q.window : 0;
@@ -276,7 +277,7 @@ __global__ __launch_bounds__(kLanes, at_once(D, NR)) void k_cache_attend(CacheDe
       float top = fmaxf(fmaxf(fmaxf(sc[t][0][0], sc[t][0][1]), fmaxf(sc[t][0][2], sc[t][0][3])),
                         fmaxf(fmaxf(sc[t][1][0], sc[t][1][1]), fmaxf(sc[t][1][2], sc[t][1][3])));
       top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
+      top = fmaxf(top, __shfl_xor(top, 32)) * q.scale_rest;
       // The maximum follows only where a score has left it 8 behind: probabilities stay below 2^8, far inside a half.
       if (__any(top > m[t] + 8.0f)) {
         const float now = fmaxf(m[t], top), by = m[t] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[t] - now);
@@ -289,7 +290,7 @@ __global__ __launch_bounds__(kLanes, at_once(D, NR)) void k_cache_attend(CacheDe
       float p[8], sum = 0.0f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        p[e] = __builtin_amdgcn_exp2f(sc[t][e / 4][e % 4] - base);
+        p[e] = __builtin_amdgcn_exp2f(fmaf(sc[t][e / 4][e % 4], q.scale_rest, -base));
         sum += p[e];
       }
       l[t] += sum;

@@ -133,7 +133,7 @@ __device__ inline half8 to_half8(const float p[8]) {
   return h;
 }
 
-// Eight channels of a row of q, times the scale of the scores and log2(e) in 32 bits, rounded to halves.
+// Eight channels of a row of q, times the scale in 32 bits, rounded to halves: to a bit or none where the scale is a power of two.
 __device__ inline half8 load_query(const uint16_t *p, bool half_type, bool vec, float scale) {
   uint16_t raw[8];
   if (vec) {
