@@ -116,8 +116,7 @@ struct CacheQuery {
   int32_t half_type;              // 1: halves, 0: bfloat16
   int32_t causal, window;
   int32_t vec;                    // q and out may be read and written 16 and 8 bytes at a time
-  float scale_log2;               // scale * log2(e), which is ...
-  float scale_two, scale_rest;    // ... a power of two, with its sign, times a number from 1 to 2
+  float scale_two, scale_rest;    // scale * log2(e): a power of two, with its sign, times a number from 1 to 2
   const uint16_t *q;
   int64_t q_row, q_head;
   uint16_t *out;

@@ -323,7 +323,6 @@ int rtams_cache_attend(rtams_cache *c, const rtams_cache_query *q, int64_t n, co
   k.half_type = q->type == RTAMS_TYPE_F16;
   k.causal = q->causal != 0;
   k.window = q->window;
-  k.scale_log2 = q->scale * 1.4426950408889634f;
   int twos = 0;
   const double times = (double)q->scale * 1.4426950408889634;
   std::frexp(times, &twos);

@@ -9,9 +9,12 @@
 // swapped so that writing meets no bank twice.  Where rows are too few to fill the chip the tokens are split, and the last
 // part of a row to arrive joins them.
 //
-// Measured: a prompt of 8,192 tokens, 32 heads of 128 over 8: 575 us for 550 GFLOP, 955 TFLOP/s where a plain product of 8,192 squared reaches 1,140
-// in bfloat16 and 1,084 in halves.  Vector work (exponentials, masks, codes) and matrix instructions take 37 % and 36 % of the cycles and
-// share the issue of a SIMD's two wavefronts.  Heads of 64, 96, 256: 613, 626, 357 TFLOP/s: at 64 exponentials are twice as many for a flop; at 256
+// The scale's power of two is in the query, exact as an operand; what is left of it multiplies scores in 32 bits (in the query and rounded there:
+// 576 us instead of 580, and half outputs 1.6 to 1.8 times as far from 64 bits as their own rounding alone, not 1.5 to 1.6).
+//
+// Measured: a prompt of 8,192 tokens, 32 heads of 128 over 8: 580 us for 550 GFLOP, 947 TFLOP/s where a plain product of 8,192 squared reaches 1,140
+// in bfloat16 and 1,084 in halves.  Vector instructions (exponentials, masks, codes) and matrix instructions take 41 % of the cycles each and
+// two wavefronts of a SIMD overlap them in part.  Heads of 64, 96, 256: 613, 626, 357 TFLOP/s: at 64 exponentials are twice as many for a flop; at 256
 // one wavefront fits a SIMD.  4 wavefronts a workgroup at 128 channels: 710 us; wavefronts half a tile apart: 610.
 #include "../../include/rtams_cache.h"
 
@@ -235,7 +238,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(C
   {
     const uint16_t *p = q.q + (row0 + j) * q.q_row + (int64_t)qh * q.q_head + h * 8;
 #pragma unroll
-    for (int s = 0; s < NS; ++s) qf[s] = real ? load_query(p + s * 16, q.half_type, q.vec, q.scale_log2) : half8{};
+    for (int s = 0; s < NS; ++s) qf[s] = real ? load_query(p + s * 16, q.half_type, q.vec, q.scale_two) : half8{};
   }
   // what some of the wavefront's rows see, and what all of them do
   const int w_first = tile * tile_rows + wave * 32, w_last = min(w_first + 31, q.share * count - 1);  // (tile_rows: whole wavefronts)
@@ -251,6 +254,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(C
   for (int c = 0; c < NC; ++c)
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[c][e] = 0.0f;
+  const float rest = q.scale_rest;  // scores and their maximum are what it multiplies
   float m = real ? -INFINITY : 0.0f, l = 0.0f;
   f32x16 start;  // of the scores' sums: less the maximum
 #pragma unroll
@@ -306,7 +310,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(C
         HalfWords w;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          w.p[e] = half2v{(_Float16)__builtin_amdgcn_exp2f(sc[x][8 * y + 2 * e]), (_Float16)__builtin_amdgcn_exp2f(sc[x][8 * y + 2 * e + 1])};
+          w.p[e] = half2v{(_Float16)__builtin_amdgcn_exp2f(sc[x][8 * y + 2 * e] * rest), (_Float16)__builtin_amdgcn_exp2f(sc[x][8 * y + 2 * e + 1] * rest)};
           most = __builtin_elementwise_max(most, w.p[e]);
         }
         pf[x][y] = w.h;
@@ -329,8 +333,8 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(C
 #pragma unroll
         for (int e = 0; e < 16; e += 2) top = fmaxf(top, fmaxf(sc[x][e], sc[x][e + 1]));
       top = fmaxf(top, __shfl_xor(top, 32));
-      const bool move = top > 8.0f || (m == -INFINITY && top > -INFINITY);  // (scores are relative to the maximum)
-      const float by = move ? top : 0.0f, shrink = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(-by);
+      const bool move = top * rest > 8.0f || (m == -INFINITY && top > -INFINITY);  // (scores are relative to the maximum)
+      const float by = move ? top : 0.0f, shrink = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(-by * rest);
       if (move) m = (m == -INFINITY ? 0.0f : m) + by;
       l *= shrink;
 #pragma unroll
@@ -392,6 +396,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(C
     }
   }
   l += __shfl_xor(l, 32);
+  m *= rest;
 
   if (pc.parts > 1) {
     // Parts lie as the lanes hold them, so that stores are whole lines and the last workgroup to arrive joins them in its own registers.
