@@ -108,7 +108,7 @@ typedef struct rtams_cache_query {
 } rtams_cache_query;
 
 /* Attention of the items' rows over one layer.  Scores, their maximum, sum and the weighted values are held in 32 bits; the
- * products take halves (keys and values rounded once to a half, probabilities, scaled queries).  A row that sees nothing
+ * products take halves (keys and values rounded once to a half, probabilities, queries times a power of two).  A row that sees nothing
  * gives 0 and a logarithm of -inf; a row of q that holds a NaN, an infinity or, times the scale, a number beyond the halves
  * spoils its own output only. */
 int rtams_cache_attend(rtams_cache *c, const rtams_cache_query *q, int64_t n, const int32_t *d_seqs,
