@@ -370,6 +370,13 @@ def test_rows_that_see_nothing():
     check_attention(out, lse, f.want(q, counts, 0.125, causal=False), unit_of(q.dtype))
 
 
+@pytest.mark.parametrize("scale", [0.0, -0.2, 0.125, 1.0, 0.3, 1e-3])
+@pytest.mark.parametrize("count", [1, 7, 90])
+def test_scales_of_the_scores(scale, count):
+    f = Filled([300, 129], 2, 64, seed=26, dtype=torch.float16)
+    f.check([count, count], 4, scale=scale)
+
+
 @pytest.mark.parametrize("count", [1, 3, 60])
 def test_scores_far_apart_and_far_from_zero(count):
     """Peaked rows, and scores whose maximum keeps growing: the running maximum follows."""
