@@ -33,13 +33,15 @@ struct Plan {
   uint32_t pairs, freed;
 };
 
-// Exclusive prefix sum over the workgroup; *total to every lane.
-__device__ inline uint32_t scan_lanes(uint32_t v, uint32_t *total, Plan &sh) {
+// Exclusive prefix sum over the workgroup; *total to every lane, in 64 bits: a lane may ask for all pages of a long sequence, 2^25 of
+// them, which 64 lanes do within 32 bits and 1024 do not.  (Where *total is beyond 32 bits the prefix sums are not to be used.)
+__device__ inline uint32_t scan_lanes(uint32_t v, uint64_t *total, Plan &sh) {
   const uint32_t inc = wave_running_sum(v);
   __syncthreads();
   if (lane_id() == 63) sh.waves[threadIdx.x >> 6] = inc;
   __syncthreads();
-  uint32_t before = 0, all = 0;
+  uint32_t before = 0;
+  uint64_t all = 0;
 #pragma unroll
   for (int w = 0; w < kPlanLanes / 64; ++w) {
     const uint32_t x = sh.waves[w];
@@ -56,7 +58,8 @@ __device__ void pick_pages(const CacheDev &d, uint32_t total, Plan &sh) {
   uint32_t found = 0;
   for (uint32_t base = 0; base < words && found < total; base += kPlanLanes) {
     const uint32_t at = base + threadIdx.x;
-    uint32_t w = at < words ? d.free_bits[at] : 0, here;
+    uint32_t w = at < words ? d.free_bits[at] : 0;
+    uint64_t here;
     uint32_t rank = found + scan_lanes(__popc(w), &here, sh);
     const uint32_t before = w;
     for (uint32_t x = w; x && rank < total; x &= x - 1, ++rank) {
@@ -66,7 +69,7 @@ __device__ void pick_pages(const CacheDev &d, uint32_t total, Plan &sh) {
       w &= ~(1u << bit);
     }
     if (w != before) d.free_bits[at] = w;
-    found += here;
+    found += (uint32_t)here;
   }
   __syncthreads();
 }
@@ -136,13 +139,13 @@ __global__ __launch_bounds__(kPlanLanes) void k_cache_extend(CacheDev d, CacheRo
         }
       }
     }
-    uint32_t here;
+    uint64_t here;
     it.off = total + scan_lanes(need, &here, sh);
     if (r.n > kPlanLanes && i < r.n) d.items[i] = it;
-    short_of = here > d.pages - total;  // (sums of a call stay below 2^32)
+    short_of = here > d.pages - total;
     bad = __syncthreads_or(bad);
     if (bad || short_of) break;
-    total += here;
+    total += (uint32_t)here;
   }
   if (bad || short_of || total > d.ctrl->free) {
     __syncthreads();
@@ -173,7 +176,7 @@ __global__ __launch_bounds__(kPlanLanes) void k_cache_extend(CacheDev d, CacheRo
       d.lengths[it.seq] = it.src;
     }
     if (!here_too) continue;
-    uint32_t fresh;
+    uint64_t fresh;
     sh.before[threadIdx.x] = scan_lanes(i < r.n ? (uint32_t)(it.want - it.have) : 0, &fresh, sh);
     if (fresh == 0) continue;
     sh.seq[threadIdx.x] = it.seq;
@@ -261,7 +264,7 @@ __global__ __launch_bounds__(kPlanLanes) void k_cache_trim(CacheDev d, int32_t n
   if (threadIdx.x == 0) d.ctrl->ok = 1;
   if (!few) return;
   if ((int)threadIdx.x < n) d.lengths[it.seq] = it.src;
-  uint32_t entries;
+  uint64_t entries;
   sh.before[threadIdx.x] = scan_lanes((uint32_t)(it.have - it.want), &entries, sh);
   sh.seq[threadIdx.x] = it.seq;
   sh.page0[threadIdx.x] = it.want;
@@ -309,7 +312,8 @@ __global__ __launch_bounds__(kPlanLanes) void k_cache_fork(CacheDev d, int32_t n
   CacheItem it{};
   for (int base = 0; base < n && !bad && !short_of; base += kPlanLanes) {
     const int i = base + threadIdx.x;
-    uint32_t need = 0, here;
+    uint32_t need = 0;
+    uint64_t here;
     it = CacheItem{};
     if (i < n) {
       const int s = src[i];
@@ -326,8 +330,8 @@ __global__ __launch_bounds__(kPlanLanes) void k_cache_fork(CacheDev d, int32_t n
     }
     it.off = total + scan_lanes(need, &here, sh);
     if (i < n && !few) d.items[i] = it;
-    short_of = here > d.pages - total;
-    total += here;
+    short_of = here > d.pages - total;  // (a source may be named by every item: the sum is not bounded by the pages there are)
+    total += (uint32_t)here;
     bad = __syncthreads_or(bad);
   }
   if (bad || short_of || total > d.ctrl->free) {
@@ -346,7 +350,7 @@ __global__ __launch_bounds__(kPlanLanes) void k_cache_fork(CacheDev d, int32_t n
     return;
   }
   if ((int)threadIdx.x < n) d.lengths[it.seq] = it.want;
-  uint32_t entries;
+  uint64_t entries;
   sh.before[threadIdx.x] = scan_lanes((uint32_t)it.have, &entries, sh);
   sh.seq[threadIdx.x] = it.seq;
   sh.page0[threadIdx.x] = it.src;
@@ -383,12 +387,12 @@ __global__ __launch_bounds__(kPlanLanes) void k_cache_compact(CacheDev d) {
       high = ~w & real & ~below;
       if (low | high) d.free_bits[at] = real & ~below;
     }
-    uint32_t all_low, all_high;
+    uint64_t all_low, all_high;
     uint32_t a = holes + scan_lanes(__popc(low), &all_low, sh), b = movers + scan_lanes(__popc(high), &all_high, sh);
     for (uint32_t x = low; x; x &= x - 1) d.pair_dst[a++] = (int32_t)(at * 32 + __ffs(x) - 1);
     for (uint32_t x = high; x; x &= x - 1) d.pair_src[b++] = (int32_t)(at * 32 + __ffs(x) - 1);
-    holes += all_low;
-    movers += all_high;
+    holes += (uint32_t)all_low;
+    movers += (uint32_t)all_high;
   }
   __syncthreads();
   for (uint32_t j = threadIdx.x; j < movers; j += kPlanLanes) {
