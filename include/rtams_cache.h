@@ -24,8 +24,9 @@
  * What only the device can see.  A call whose items are not what it asks for (a sequence outside 0..max_seqs - 1 or named
  * twice, more rows than max_new or than the sequence has, ...) raises EINVAL and a call that finds too few free pages
  * EPOOL, to be asked for with rtams_cache_poll_error; calls that change the table are then dropped as a whole, other
- * calls leave the item's rows as they are.  After an extend that was dropped, writes are dropped too until an extend
- * succeeds or rtams_cache_clear_error is called.
+ * calls leave the item's rows as they are.  (Attention that is not causal asks for no positions: an item may have any
+ * number of rows.)  After an extend that was dropped, writes are dropped too until an extend succeeds or
+ * rtams_cache_clear_error is called.
  *
  * Streams.  The calls of one cache run one after another; a call on another stream than the one before is ordered behind
  * it with an event.  A stream must live until the cache has been used on another one or destroyed.  Recorded calls

@@ -58,12 +58,13 @@ __device__ inline void find_spans(const CacheDev &d, const CacheQuery &q, int i,
 #pragma unroll
   for (int k = 0; k < N; ++k) {
     const bool there = i + 64 * k < n, known = (uint32_t)seq[k] < (uint32_t)d.max_seqs;
-    const bool ok = first[k] >= 0 && past[k] >= first[k] && past[k] <= q.r.rows && past[k] - first[k] <= q.r.max_new && known;
+    const bool rows = first[k] >= 0 && past[k] >= first[k] && past[k] <= q.r.rows && past[k] - first[k] <= q.r.max_new;
+    const bool ok = rows && known && (!q.causal || past[k] - first[k] <= length[k]);
     s[k].row0 = first[k];
     s[k].seq = seq[k];
     s[k].count = there && ok ? past[k] - first[k] : 0;
     s[k].length = length[k];
-    if (tell && there && (!ok || (q.causal && s[k].count > length[k]))) cache_raise(d, RTAMS_EINVAL);
+    if (tell && there && !ok) cache_raise(d, RTAMS_EINVAL);
     const int low = length[k] - s[k].count - q.window + 1;
     s[k].low = q.window && low > 0 ? low & ~(kBlockTokens - 1) : 0;
     s[k].steps = s[k].count <= 0 ? 0 : length[k] > s[k].low ? (length[k] - s[k].low + kStep - 1) / kStep : 1;

@@ -116,7 +116,11 @@ __device__ inline Span find_span(const CacheDev &d, const CacheQuery &q, int ite
     return s;
   }
   s.length = d.lengths[s.seq];
-  if (tell && q.causal && s.count > s.length) cache_raise(d, RTAMS_EINVAL);
+  if (q.causal && s.count > s.length) {
+    if (tell) cache_raise(d, RTAMS_EINVAL);
+    s.count = 0;
+    return s;
+  }
   if (tile * rows >= q.share * s.count) {
     s.count = 0;
     return s;

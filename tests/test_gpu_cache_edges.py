@@ -1,11 +1,12 @@
 """The cache where its calls could go wrong at the edges of what they take: sums beyond 32 bits, items that are not what a call asks for, probabilities
 far below the largest, arguments that another stream reads, strides that say nothing.  Plain implementations and bounds: test_gpu_cache.py."""
+import numpy as np
 import pytest
 import torch
 
 from paper_2408_02937_amd import rtams
 from paper_2408_02937_amd.cache import Cache
-from tests.test_gpu_cache import DEV, ints
+from tests.test_gpu_cache import DEV, Filled, check_attention, ints, starts_of, unit_of
 
 pytestmark = pytest.mark.gpu
 
@@ -30,3 +31,47 @@ def test_copies_of_a_long_sequence_are_counted_beyond_32_bits():
     c.fork(ints([0] * n), ints(range(1, n + 1)), copy=True)
     assert c.poll_error() == 0 and c.free_pages == long + 2000 - 5 * (n + 1)
     assert c.table[1:, :5].flatten().tolist() == list(range(5, 5 * (n + 1)))
+
+
+# ------------------------------------------------------------------ items that attention refuses
+@pytest.mark.parametrize("lengths,counts,heads,kv,dim", [([0, 40, 9], [1, 1, 1], 4, 2, 64), ([3, 40, 0], [5, 5, 2], 4, 2, 128), ([3, 70], [17, 16], 4, 1, 256),
+                                                         ([30, 200, 64], [90, 100, 65], 4, 2, 64), ([69, 300], [70, 70], 2, 2, 256)])
+@pytest.mark.parametrize("window", [0, 20])
+def test_more_causal_rows_than_tokens_are_refused_and_left(lengths, counts, heads, kv, dim, window):
+    """The item's rows and logarithms stay what they were, the other items' are theirs; without a causal mask rows have no places and any number is answered."""
+    f = Filled(lengths, kv, dim, seed=40)
+    q = f.query(counts, heads)
+    out, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 5.0, device=DEV)
+    at = np.concatenate([[0], np.cumsum(counts)])
+    one = all(c == 1 for c in counts)
+    args = (ints(range(len(lengths))), None if one else starts_of(counts), None if one else max(counts))
+    f.cache.attend(0, q, *args, window=window, out=out, lse=lse)
+    torch.cuda.synchronize()
+    assert f.cache.poll_error() == rtams.EINVAL
+    f.cache.clear_error()
+    want = f.want(q, counts, dim ** -0.5, window=window)
+    for i, (n, c) in enumerate(zip(lengths, counts)):
+        rows = slice(at[i], at[i + 1])
+        if c > n:
+            assert (out[rows] == 7.0).all() and (lse[rows] == 5.0).all(), i
+        else:
+            check_attention(out[rows], lse[rows], [x[rows] for x in want], unit_of(q.dtype))
+    if not window:
+        out = f.cache.attend(0, q, *args, causal=False, lse=lse)
+        check_attention(out, lse, f.want(q, counts, dim ** -0.5, causal=False), unit_of(q.dtype))
+        assert f.cache.poll_error() == 0
+
+
+def test_more_causal_rows_than_tokens_among_many_prompts():
+    lengths = [(i * 37) % 90 + 40 for i in range(300)]
+    f = Filled(lengths, 4, 64, page=32, seed=41)
+    counts = [36 + i % 9 for i in range(300)]
+    counts[7], counts[299] = lengths[7] + 1, lengths[299] + 30
+    q = f.query(counts, 8)
+    out = torch.full_like(q, 7.0)
+    f.cache.attend(0, q, starts=starts_of(counts), max_new=max(counts), out=out)
+    torch.cuda.synchronize()
+    assert f.cache.poll_error() == rtams.EINVAL
+    at = np.concatenate([[0], np.cumsum(counts)])
+    for i in range(300):
+        assert bool((out[at[i]:at[i + 1]] == 7.0).all()) == (i in (7, 299)), i
