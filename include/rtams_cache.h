@@ -84,6 +84,7 @@ int rtams_cache_extend(rtams_cache *c, int64_t n, const int32_t *d_seqs, const i
 
 /* One layer's keys and values of the items' rows: d_k and d_v [rows][kv_heads][head_dim] of `type` (BF16 or F16), rows and
  * heads `row_stride` and `head_stride` elements apart (below 2^24), channels next to each other.  max_new: the most rows of one item.
+ * The items of a sequence that is named twice are left out, with EINVAL.
  * Rows whose page another sequence shares are left out, with EINVAL: extend sees to it that new rows' pages are not. */
 int rtams_cache_write(rtams_cache *c, int32_t layer, int64_t n, const int32_t *d_seqs, const int32_t *d_starts,
                       int64_t rows, int32_t max_new, const void *d_k, const void *d_v, int64_t row_stride,

@@ -29,6 +29,7 @@ def test_copies_of_a_long_sequence_are_counted_beyond_32_bits():
     assert c.free_pages == 1999
     c.trim(ints([0]), ints([5 * 32]))  # ... and what there is room for is copied
     c.fork(ints([0] * n), ints(range(1, n + 1)), copy=True)
+    torch.cuda.synchronize()
     assert c.poll_error() == 0 and c.free_pages == long + 2000 - 5 * (n + 1)
     assert c.table[1:, :5].flatten().tolist() == list(range(5, 5 * (n + 1)))
 
@@ -75,3 +76,53 @@ def test_more_causal_rows_than_tokens_among_many_prompts():
     at = np.concatenate([[0], np.cumsum(counts)])
     for i in range(300):
         assert bool((out[at[i]:at[i + 1]] == 7.0).all()) == (i in (7, 299)), i
+
+
+# ------------------------------------------------------------------ sequences named twice
+@pytest.mark.parametrize("n", [2, 5, 257, 300, 1024, 1025, 1500])
+@pytest.mark.parametrize("single", [True, False])
+def test_a_sequence_named_twice_is_not_written(n, single):
+    """Its items are left out, with an error; the others are written."""
+    rng = np.random.default_rng(n)
+    c = Cache(2, 64, page_tokens=32, pages=n, max_seqs=n, max_pages=1, device=DEV)
+    length = 5
+    every = starts_of([length] * n)
+    g = torch.Generator(device=DEV).manual_seed(n)
+    old = [torch.randn((n * length, 2, 64), device=DEV, generator=g).half() for _ in range(2)]
+    c.extend(starts=every)
+    c.write(0, *old, starts=every, max_new=length)
+    was = [x.view(n, length, 2, 64).clone() for x in c.read(0, n * length, starts=every, max_new=length)]
+    seqs = rng.permutation(n)
+    seqs[n - 1] = seqs[0]
+    if n > 4:
+        seqs[n // 2] = seqs[n // 2 - 1]
+    counts = [1] * n if single else [int(x) for x in rng.integers(0, length + 1, n)]
+    counts[0] = counts[n - 1] = 1 if single else 3
+    new = [torch.randn((sum(counts), 2, 64), device=DEV, generator=g).half() for _ in range(2)]
+    args = (ints(seqs), None if single else starts_of(counts), length)
+    c.write(0, *new, *args)
+    got = [x.view(n, length, 2, 64) for x in c.read(0, n * length, starts=every, max_new=length)]
+    torch.cuda.synchronize()
+    assert c.poll_error() == rtams.EINVAL
+    c.clear_error()
+    twice = {s for s in seqs if (seqs == s).sum() > 1}
+    alone = [x.clone() for x in was]
+    at = 0
+    for s, m in zip(seqs, counts):
+        if s not in twice and m:
+            one = Cache(2, 64, page_tokens=32, pages=1, max_seqs=1, device=DEV) if s == seqs[1] else None
+            if one is not None:  # (what a single sequence's write leaves)
+                one.extend(starts=ints([0, m]))
+                one.write(0, *(x[at:at + m] for x in new), starts=ints([0, m]), max_new=m)
+                for x, y in zip(alone, one.read(0, m, starts=ints([0, m]), max_new=m)):
+                    assert torch.equal(got[0 if x is alone[0] else 1][s, length - m:], y)
+            for x, y in zip(alone, got):
+                assert not torch.equal(x[s, length - m:], y[s, length - m:])
+                x[s, length - m:] = y[s, length - m:]
+        at += m
+    for x, y in zip(alone, got):  # nothing else changed
+        assert torch.equal(x, y)
+    some = rng.permutation(n)[:max(1, n - 1)]
+    c.write(0, old[0][:len(some)], old[1][:len(some)], ints(some))
+    torch.cuda.synchronize()
+    assert c.poll_error() == 0
