@@ -279,23 +279,19 @@ __global__ __launch_bounds__(kLanes, at_once(D, NR)) void k_cache_attend(CacheDe
                         fmaxf(fmaxf(sc[t][1][0], sc[t][1][1]), fmaxf(sc[t][1][2], sc[t][1][3])));
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32)) * q.scale_rest;
-      // The maximum follows only where a score has left it 8 behind: probabilities stay below 2^8, far inside a half.
-      if (__any(top > m[t] + 8.0f)) {
-        const float now = fmaxf(m[t], top), by = m[t] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[t] - now);
+      if (__any(top > m[t] + (kTop + kLag))) {
+        const float now = fmaxf(m[t], top - kTop), by = m[t] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[t] - now);
         m[t] = now;
         l[t] *= by;
 #pragma unroll
         for (int n = 0; n < NT; ++n) o[t][n] *= by;
       }
       const float base = m[t] == -INFINITY ? 0.0f : m[t];
-      float p[8], sum = 0.0f;
+      float p[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        p[e] = __builtin_amdgcn_exp2f(fmaf(sc[t][e / 4][e % 4], q.scale_rest, -base));
-        sum += p[e];
-      }
-      l[t] += sum;
+      for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(sc[t][e / 4][e % 4], q.scale_rest, -base));
       pf[t] = to_half8(p);
+      l[t] += add_up(0.0f, pf[t]);
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {

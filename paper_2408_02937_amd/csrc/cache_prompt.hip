@@ -5,7 +5,7 @@
 // 64 at a time (32 where head_dim is 256): all its lanes turn their codes into halves in LDS, once for all rows, while the loads of the next
 // tokens are under way; two buffers, one barrier.  Scores are S^T = K Q^T with Q in registers; a lane has one row's scores and its
 // probabilities are the operand that O^T = V^T P^T takes.  The running maximum enters as the start of the scores' sums and moves
-// only where a score has left it 8 behind.  LDS holds operands in the order in which the lanes take them, 16 bytes each; the slots are
+// only where a score has left it far behind (kLag).  LDS holds operands in the order in which the lanes take them, 16 bytes each; the slots are
 // swapped so that writing meets no bank twice.  Where rows are too few to fill the chip the tokens are split, and the last
 // part of a row to arrive joins them.
 //
@@ -259,7 +259,10 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(C
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[c][e] = 0.0f;
   const float rest = q.scale_rest;  // scores and their maximum are what it multiplies
-  float m = real ? -INFINITY : 0.0f, l = 0.0f;
+  // (a row's sum is that of up to kRun tiles at a time: a long tail's probabilities one by one would be lost in it.  Of each tile: heads of 64, 96, 128, 256
+  // channels, prompts of 4,534, 2 heads of 8: 112, 128, 145, 417 us, of eight 111, 125, 145, 412, without 111, 124, 146, 402)
+  constexpr int kRun = 8;
+  float m = real ? -INFINITY : 0.0f, l = 0.0f, part = 0.0f;
   f32x16 start;  // of the scores' sums: less the maximum
 #pragma unroll
   for (int e = 0; e < 16; ++e) start[e] = 0.0f;
@@ -304,7 +307,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(C
       }
     reads_ahead<NS * TB>();
   };
-  // Probabilities, and whether one has left the maximum 8 behind.
+  // Probabilities, and whether one is beyond what the maximum may be left behind.
   const auto powers = [&]() {
     half2v most = {(_Float16)0.0f, (_Float16)0.0f};
 #pragma unroll
@@ -319,7 +322,8 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(C
         }
         pf[x][y] = w.h;
       }
-    return most[0] > (_Float16)256.0f || most[1] > (_Float16)256.0f;
+    constexpr _Float16 kMost = (_Float16)(1 << (int)(kTop + kLag));
+    return most[0] > kMost || most[1] > kMost;
   };
   const auto probabilities = [&](int tok0) {
     if (tok0 + kTile > all_to || tok0 < all_from) {
@@ -337,10 +341,11 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(C
 #pragma unroll
         for (int e = 0; e < 16; e += 2) top = fmaxf(top, fmaxf(sc[x][e], sc[x][e + 1]));
       top = fmaxf(top, __shfl_xor(top, 32));
-      const bool move = top * rest > 8.0f || (m == -INFINITY && top > -INFINITY);  // (scores are relative to the maximum)
-      const float by = move ? top : 0.0f, shrink = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(-by * rest);
+      const bool move = top * rest > kTop + kLag || (m == -INFINITY && top > -INFINITY);  // (scores are relative to the maximum)
+      const float by = move ? top - kTop * __builtin_amdgcn_rcpf(rest) : 0.0f, shrink = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(-by * rest);
       if (move) m = (m == -INFINITY ? 0.0f : m) + by;
-      l *= shrink;
+      l = (l + part) * shrink;
+      part = 0.0f;
 #pragma unroll
       for (int c = 0; c < NC; ++c) o[c] *= shrink;
 #pragma unroll
@@ -348,16 +353,8 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(C
       start -= by;
       powers();
     }
-    const half2v ones = {(_Float16)1.0f, (_Float16)1.0f};
 #pragma unroll
-    for (int x = 0; x < TB; ++x)
-#pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        HalfWords w;
-        w.h = pf[x][y];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) l = __builtin_amdgcn_fdot2(w.p[e], ones, l, false);
-      }
+    for (int x = 0; x < TB; ++x) part = add_up(add_up(part, pf[x][0]), pf[x][1]);
   };
   const auto weigh = [&](const uint4 *vt) {
 #pragma unroll
@@ -396,9 +393,14 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(C
         weigh(sh.v[now]);
         __builtin_amdgcn_s_setprio(0);
       }
+      if (t % kRun == 0) {
+        l += part;
+        part = 0.0f;
+      }
       __syncthreads();
     }
   }
+  l += part;
   l += __shfl_xor(l, 32);
   m *= rest;
 

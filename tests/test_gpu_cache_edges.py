@@ -6,7 +6,7 @@ import torch
 
 from paper_2408_02937_amd import rtams
 from paper_2408_02937_amd.cache import Cache
-from tests.test_gpu_cache import DEV, Filled, check_attention, ints, starts_of, unit_of
+from tests.test_gpu_cache import DEV, Filled, check_attention, floats, ints, starts_of, unit_of
 
 pytestmark = pytest.mark.gpu
 
@@ -126,3 +126,62 @@ def test_a_sequence_named_twice_is_not_written(n, single):
     c.write(0, old[0][:len(some)], old[1][:len(some)], ints(some))
     torch.cuda.synchronize()
     assert c.poll_error() == 0
+
+
+# ------------------------------------------------------------------ numbers
+UP = 7  # a row's largest probability is at least 2^UP when it is rounded to a half
+
+
+@pytest.mark.parametrize("depth", [12.0, 20.0, 24.5, 25.2, 28.0])
+@pytest.mark.parametrize("dim,count", [(64, 1), (64, 40), (64, 90), (96, 1), (96, 70), (128, 1), (128, 90), (256, 1), (256, 20), (256, 70)])
+@pytest.mark.parametrize("spread", [0.0, 1.0])
+def test_a_long_tail_behind_a_sink(dim, count, depth, spread):
+    """One token with nearly all the weight and a value of 0; what comes out is the tail's, whose probabilities are 2^-depth of it (spread: a factor of two
+    among them).  A half of 2^UP times that is off by 2^-25 at most, and by 2^-11 of itself; scores of up to 25 in 32 bits are off by 2^-20."""
+    tokens = 64
+    g = np.random.default_rng(int(depth * 10) + dim)
+    c = -(depth + spread * (g.random(tokens) - 0.5)) * np.log(2) / dim
+    c[0] = 0.0
+    k = torch.tensor(c, device=DEV).half()[:, None, None].expand(tokens, 1, dim).contiguous()
+    v = torch.full((tokens, 1, dim), 1024.0, dtype=torch.float16, device=DEV)
+    v[0] = 0.0
+    cache = Cache(1, dim, page_tokens=64, pages=1, max_seqs=1, device=DEV)
+    st = ints([0, tokens])
+    cache.extend(starts=st)
+    cache.write(0, k, v, starts=st, max_new=tokens)
+    q = torch.ones((count, 1, dim), dtype=torch.float16, device=DEV)
+    lse = torch.empty((count, 1), device=DEV)
+    out = cache.attend(0, q, starts=ints([0, count]), max_new=count, scale=1.0, causal=False, lse=lse).double().cpu().numpy()
+    p = np.exp(floats(k[:, 0, 0]).astype(np.float64) * dim)
+    want = 1024.0 * p[1:].sum() / p.sum()
+    rel = 2.0 ** -25 / (2.0 ** UP * p[1:].min()) if 2.0 ** UP * p[1:].min() < 2.0 ** -14 else 2.0 ** -11
+    assert rel < 0.2
+    bound = want * (rel + 2.0 ** -11 + 2.0 ** -16) + 2.0 ** -25  # (the last: of an output that is below a half's normal range)
+    assert np.abs(out - want).max() <= bound, (out.flat[0], want)
+    assert abs(lse.cpu().numpy() - np.log(p.sum())).max() <= 2.0 ** -16 + 2.0 ** -10 * p[1:].sum()
+
+
+def test_a_long_tail_adds_up():
+    """Thousands of tokens behind a sink, each of them below a half's normal range at 2^UP times its probability: their sum is in the logarithm.  A
+    half below the normal range is off by 2^-25, as often up as down; what is left of that in a sum of so many is far less than all off alike, the bound."""
+    tokens, heads, dim, depth = 4097, 256, 64, 22.3
+    c = np.full(tokens, -depth * np.log(2) / dim)
+    c[0] = 0.0
+    k = torch.tensor(c, device=DEV).half()[:, None, None].expand(tokens, heads, dim).contiguous()
+    v = torch.full((tokens, heads, dim), 1024.0, dtype=torch.float16, device=DEV)
+    v[0] = 0.0
+    cache = Cache(heads, dim, page_tokens=64, pages=65, max_seqs=1, device=DEV)
+    st = ints([0, tokens])
+    cache.extend(starts=st)
+    cache.write(0, k, v, starts=st, max_new=tokens)
+    p = np.exp(floats(k[:, 0, 0]).astype(np.float64) * dim)
+    tail = p[1:].sum()
+    rel = 2.0 ** -25 / (2.0 ** UP * p[1])
+    assert 2.0 ** UP * p[1] < 2.0 ** -14 and rel < 2.0 ** -9 and tail > 2.0 ** -11
+    for count in (1, 70):
+        q = torch.ones((count, heads, dim), dtype=torch.float16, device=DEV)
+        lse = torch.empty((count, heads), device=DEV)
+        out = cache.attend(0, q, starts=ints([0, count]), max_new=count, scale=1.0, causal=False, lse=lse).double().cpu().numpy()
+        assert np.abs(lse.double().cpu().numpy() - np.log1p(tail)).max() <= rel * tail + 2.0 ** -16
+        want = 1024.0 * tail / (1 + tail)
+        assert np.abs(out - want).max() <= want * (rel + 2.0 ** -11 + 2.0 ** -16)
