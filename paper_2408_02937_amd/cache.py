@@ -2,7 +2,8 @@
 reads it, beside the index of rtams.py.
 
 Like the index, argument marshalling only: every step runs in the HIP kernels behind the C ABI, calls are asynchronous on
-the stream given (the current one unless told), there is no fallback.
+the stream given (the current one unless told), there is no fallback.  Tensors handed to a call on a stream given are kept for that
+stream: they may be dropped when the call has returned.
 
     c = Cache(kv_heads=8, head_dim=128, layers=2, pages=4096, max_seqs=64)
     c.extend(seqs, starts)                              # room for the new rows of these sequences
@@ -92,14 +93,16 @@ class Cache:
     def _stream(self, stream) -> int:
         return _current_stream(self.device.index) if stream is None else stream.cuda_stream
 
-    def _ints(self, t: Optional[torch.Tensor], what: str, n: Optional[int] = None) -> Optional[int]:
+    def _ints(self, t: Optional[torch.Tensor], what: str, n: Optional[int] = None, stream=None) -> Optional[int]:
         if t is None:
             return None
         if not (t.dtype == torch.int32 and t.dim() == 1 and t.is_contiguous() and t.device == self.device and (n is None or t.shape[0] == n)):
             raise ValueError(f"{what} must be a contiguous int32 tensor on {self.device}" + ("" if n is None else f" of {n} entries"))
+        if stream is not None:
+            t.record_stream(stream)
         return t.data_ptr()
 
-    def _items(self, seqs, starts, n, max_new):
+    def _items(self, seqs, starts, n, max_new, stream):
         """(n, pointers of seqs and starts, most rows of an item)."""
         if n is None:
             n = seqs.shape[0] if seqs is not None else starts.shape[0] - 1 if starts is not None else None
@@ -109,29 +112,31 @@ class Cache:
             max_new = 1
         elif max_new is None:
             raise ValueError("with starts, give max_new: the most rows of one item")
-        return n, self._ints(seqs, "seqs", n), self._ints(starts, "starts", n + 1), max_new
+        return n, self._ints(seqs, "seqs", n, stream), self._ints(starts, "starts", n + 1, stream), max_new
 
-    def _rows(self, t: torch.Tensor, heads: Optional[int], what: str) -> torch.Tensor:
+    def _rows(self, t: torch.Tensor, heads: Optional[int], what: str, stream=None) -> torch.Tensor:
         if not (t.dim() == 3 and t.shape[2] == self.head_dim and (heads is None or t.shape[1] == heads) and t.dtype in (torch.bfloat16, torch.float16)
                 and t.device == self.device and (t.stride(2) == 1 or t.numel() == 0)):
             raise ValueError(f"{what} must be a bfloat16 or float16 tensor [rows][{'heads' if heads is None else heads}][{self.head_dim}] on {self.device} "
                              "whose channels lie next to each other")
+        if stream is not None:
+            t.record_stream(stream)
         return t
 
     # ---- the path
     def extend(self, seqs: Optional[torch.Tensor] = None, starts: Optional[torch.Tensor] = None, n: Optional[int] = None, stream=None) -> None:
         """Room for the items' rows (one each without starts) at the ends of their sequences."""
-        n, sp, tp, _ = self._items(seqs, starts, n, 1)
+        n, sp, tp, _ = self._items(seqs, starts, n, 1, stream)
         _chk(self._lib.rtams_cache_extend(self._h, n, sp, tp, self._stream(stream)), "rtams_cache_extend")
 
     def write(self, layer: int, k: torch.Tensor, v: torch.Tensor, seqs: Optional[torch.Tensor] = None, starts: Optional[torch.Tensor] = None,
               max_new: Optional[int] = None, stream=None) -> None:
         """Keys and values of the sequences' last rows, [rows][kv_heads][head_dim]."""
-        k, v = self._rows(k, self.kv_heads, "k"), self._rows(v, self.kv_heads, "v")
+        k, v = self._rows(k, self.kv_heads, "k", stream), self._rows(v, self.kv_heads, "v", stream)
         if k.shape != v.shape or k.dtype != v.dtype or (k.stride() != v.stride() and k.numel()):
             raise ValueError("k and v must have the same shape, type and strides")
         rows = k.shape[0]
-        n, sp, tp, max_new = self._items(seqs, starts, rows if seqs is None and starts is None else None, max_new)
+        n, sp, tp, max_new = self._items(seqs, starts, rows if seqs is None and starts is None else None, max_new, stream)
         _chk(self._lib.rtams_cache_write(self._h, layer, n, sp, tp, rows, max_new, k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1),
                                      _TYPES[k.dtype], self._stream(stream)), "rtams_cache_write")
 
@@ -140,7 +145,7 @@ class Cache:
         """What the cache holds of the sequences' last rows, as values."""
         if dtype not in _TYPES:
             raise ValueError("dtype must be bfloat16, float16 or float32")
-        n, sp, tp, max_new = self._items(seqs, starts, rows if seqs is None and starts is None else None, max_new)
+        n, sp, tp, max_new = self._items(seqs, starts, rows if seqs is None and starts is None else None, max_new, stream)
         k = torch.empty((rows, self.kv_heads, self.head_dim), dtype=dtype, device=self.device)
         v = torch.empty_like(k)
         if stream is not None:
@@ -154,19 +159,21 @@ class Cache:
                out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """Attention of the sequences' last rows, q [rows][heads][head_dim]; lse: float32 [rows][heads] that takes the
         logarithms of the sums of exp(score)."""
-        q = self._rows(q, None, "q")
+        q = self._rows(q, None, "q", stream)
         rows, heads = q.shape[0], q.shape[1]
-        n, sp, tp, max_new = self._items(seqs, starts, rows if seqs is None and starts is None else None, max_new)
+        n, sp, tp, max_new = self._items(seqs, starts, rows if seqs is None and starts is None else None, max_new, stream)
         if out is None:
             out = q.new_empty((rows, heads, self.head_dim))
             if stream is not None:
                 out.record_stream(stream)  # (it comes from the current stream's memory)
-        elif self._rows(out, heads, "out").shape != q.shape or out.dtype != q.dtype:
+        elif self._rows(out, heads, "out", stream).shape != q.shape or out.dtype != q.dtype:
             raise ValueError("out must have the shape and type of q")
         lp = None
         if lse is not None:
             if not (lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (rows, heads) and lse.device == self.device):
                 raise ValueError("lse must be a contiguous float32 tensor [rows][heads]")
+            if stream is not None:
+                lse.record_stream(stream)
             lp = lse.data_ptr()
         cq = _query(layer, heads, _TYPES[q.dtype], int(causal), window, max_new, self.head_dim ** -0.5 if scale is None else scale,
                         q.data_ptr(), q.stride(0), q.stride(1), out.data_ptr(), out.stride(0), out.stride(1), lp or 0)
@@ -177,7 +184,7 @@ class Cache:
     def fork(self, src: torch.Tensor, dst: torch.Tensor, copy: bool = False, stream=None) -> None:
         """Empty sequences dst become what src are, sharing pages until they grow, or (copy) in pages of their own."""
         n = src.shape[0]
-        _chk(self._lib.rtams_cache_fork(self._h, n, self._ints(src, "src"), self._ints(dst, "dst", n), int(copy), self._stream(stream)), "rtams_cache_fork")
+        _chk(self._lib.rtams_cache_fork(self._h, n, self._ints(src, "src", None, stream), self._ints(dst, "dst", n, stream), int(copy), self._stream(stream)), "rtams_cache_fork")
 
     def trim(self, seqs: Optional[torch.Tensor] = None, lengths: Optional[torch.Tensor] = None, n: Optional[int] = None, stream=None) -> None:
         """Cuts sequences down to `lengths` tokens (without: to none)."""
@@ -185,7 +192,7 @@ class Cache:
             n = seqs.shape[0] if seqs is not None else lengths.shape[0] if lengths is not None else None
         if n is None:
             raise ValueError("give seqs, lengths or n")
-        _chk(self._lib.rtams_cache_trim(self._h, n, self._ints(seqs, "seqs", n), self._ints(lengths, "lengths", n), self._stream(stream)), "rtams_cache_trim")
+        _chk(self._lib.rtams_cache_trim(self._h, n, self._ints(seqs, "seqs", n, stream), self._ints(lengths, "lengths", n, stream), self._stream(stream)), "rtams_cache_trim")
 
     def compact(self, stream=None) -> None:
         """Moves the pages in use to the front of the pool."""

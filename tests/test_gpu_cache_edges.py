@@ -185,3 +185,40 @@ def test_a_long_tail_adds_up():
         assert np.abs(lse.double().cpu().numpy() - np.log1p(tail)).max() <= rel * tail + 2.0 ** -16
         want = 1024.0 * tail / (1 + tail)
         assert np.abs(out - want).max() <= want * (rel + 2.0 ** -11 + 2.0 ** -16)
+
+
+# ------------------------------------------------------------------ streams
+@pytest.mark.parametrize("call", ["extend", "write", "read", "attend", "fork", "trim"])
+def test_what_another_stream_reads_is_not_given_out_again(call):
+    """Arguments that die right after a call on a stream that is busy: their memory is not a new tensor's."""
+    f = Filled([300, 200], 2, 64, seed=42, max_seqs=4, extra_pages=20)
+    s = torch.cuda.Stream()
+    a = torch.randn((4096, 4096), device=DEV)
+    b = torch.empty_like(a)
+    q, k, v = f.query([1, 1], 4), f.k[:2].clone(), f.v[:2].clone()
+    x, y, st = ints([0, 1]), ints([2, 3]), ints([0, 1, 2])
+    lens = ints([300, 200])
+    out, lse = torch.empty_like(q), torch.empty((2, 4), device=DEV)
+    with torch.cuda.stream(s):  # everything has run once
+        torch.mm(a, a, out=b)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        for _ in range(1500):
+            torch.mm(a, a, out=b)
+    done = torch.cuda.Event()
+    given = {"extend": lambda: (f.cache.extend(x, st, stream=s), [x, st]),
+             "write": lambda: (f.cache.write(0, k, v, x, st, max_new=1, stream=s), [k, v, x, st]),
+             "read": lambda: (f.cache.read(0, 2, x, st, max_new=1, stream=s), [x, st]),
+             "attend": lambda: (f.cache.attend(0, q, x, st, max_new=1, out=out, lse=lse, stream=s), [q, x, st, out, lse]),
+             "fork": lambda: (f.cache.fork(x, y, stream=s), [x, y]),
+             "trim": lambda: (f.cache.trim(x, lens, stream=s), [x, lens])}[call]
+    result, mine = given()
+    at = [(t.data_ptr(), t.numel() * t.element_size()) for t in mine]
+    del result, mine, given, q, k, v, x, y, st, lens, out, lse
+    done.record(s)
+    fresh = [torch.empty(n, dtype=torch.uint8, device=DEV) for _, n in at for _ in range(500)]
+    again = {t.data_ptr() for t in fresh} & {p for p, _ in at}
+    assert not done.query(), "the stream was to be busy all the while"
+    torch.cuda.synchronize()
+    assert not again
+    assert f.cache.poll_error() == 0
