@@ -123,6 +123,16 @@ class Cache:
             t.record_stream(stream)
         return t
 
+    def _empty(self, shape, dtype: torch.dtype, stream) -> torch.Tensor:
+        """Memory for an output: the given stream's own, since what is free on the current one may still be read there by work under way, and
+        not used again before the current stream, where the caller has it, is done with it."""
+        if stream is None:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(stream):
+            t = torch.empty(shape, dtype=dtype, device=self.device)
+        t.record_stream(torch.cuda.current_stream(self.device))
+        return t
+
     # ---- the path
     def extend(self, seqs: Optional[torch.Tensor] = None, starts: Optional[torch.Tensor] = None, n: Optional[int] = None, stream=None) -> None:
         """Room for the items' rows (one each without starts) at the ends of their sequences."""
@@ -146,10 +156,7 @@ class Cache:
         if dtype not in _TYPES:
             raise ValueError("dtype must be bfloat16, float16 or float32")
         n, sp, tp, max_new = self._items(seqs, starts, rows if seqs is None and starts is None else None, max_new, stream)
-        k = torch.empty((rows, self.kv_heads, self.head_dim), dtype=dtype, device=self.device)
-        v = torch.empty_like(k)
-        if stream is not None:
-            k.record_stream(stream), v.record_stream(stream)
+        k, v = (self._empty((rows, self.kv_heads, self.head_dim), dtype, stream) for _ in range(2))
         _chk(self._lib.rtams_cache_read(self._h, layer, n, sp, tp, rows, max_new, k.data_ptr(), v.data_ptr(), _TYPES[dtype], self._stream(stream)),
              "rtams_cache_read")
         return k, v
@@ -163,9 +170,7 @@ class Cache:
         rows, heads = q.shape[0], q.shape[1]
         n, sp, tp, max_new = self._items(seqs, starts, rows if seqs is None and starts is None else None, max_new, stream)
         if out is None:
-            out = q.new_empty((rows, heads, self.head_dim))
-            if stream is not None:
-                out.record_stream(stream)  # (it comes from the current stream's memory)
+            out = self._empty((rows, heads, self.head_dim), q.dtype, stream)
         elif self._rows(out, heads, "out", stream).shape != q.shape or out.dtype != q.dtype:
             raise ValueError("out must have the shape and type of q")
         lp = None

@@ -222,3 +222,37 @@ def test_what_another_stream_reads_is_not_given_out_again(call):
     torch.cuda.synchronize()
     assert not again
     assert f.cache.poll_error() == 0
+
+
+@pytest.mark.parametrize("call", ["read", "attend"])
+def test_outputs_on_another_stream_take_no_memory_that_is_still_read(call):
+    """A tensor that the current stream has yet to read is dropped: its memory is not the output's that another stream writes at once; and an output that
+    the current stream has yet to read is dropped: the other stream does not get it again."""
+    rows, heads = 4000, 8
+    f = Filled([rows], heads, 64, page=64, seed=47)
+    st = ints([0, rows])
+    s = torch.cuda.Stream()
+    run = {"attend": lambda: f.cache.attend(0, f.k, starts=st, max_new=rows, stream=s), "read": lambda: f.cache.read(0, rows, starts=st, max_new=rows, dtype=torch.bfloat16, stream=s)[0]}[call]
+    want = run()
+    a = torch.randn((4096, 4096), device=DEV)
+    b = torch.mm(a, a)
+    torch.cuda.synchronize()
+    x = torch.full_like(want, 3.0)
+    at = x.data_ptr()
+    for _ in range(200):
+        torch.mm(a, a, out=b)
+    y = x.clone()
+    del x
+    got = run()
+    assert got.data_ptr() != at
+    s.synchronize()
+    del want
+    for _ in range(200):
+        torch.mm(a, a, out=b)
+    z, at = got.clone(), got.data_ptr()
+    del got
+    more = [run() for _ in range(4)]
+    assert not torch.cuda.current_stream().query(), "the stream was to be busy all the while"
+    assert at not in {t.data_ptr() for t in more}
+    torch.cuda.synchronize()
+    assert (y == 3.0).all() and torch.equal(z, more[0]) and f.cache.poll_error() == 0
