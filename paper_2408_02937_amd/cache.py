@@ -3,7 +3,7 @@ reads it, beside the index of rtams.py.
 
 Like the index, argument marshalling only: every step runs in the HIP kernels behind the C ABI, calls are asynchronous on
 the stream given (the current one unless told), there is no fallback.  Tensors handed to a call on a stream given are kept for that
-stream: they may be dropped when the call has returned.
+stream: they may be dropped when the call has returned.  Nothing here has a gradient, and a tensor that asks for one is refused.
 
     c = Cache(kv_heads=8, head_dim=128, layers=2, pages=4096, max_seqs=64)
     c.extend(seqs, starts)                              # room for the new rows of these sequences
@@ -119,6 +119,8 @@ class Cache:
                 and t.device == self.device and (t.stride(2) == 1 or t.numel() == 0)):
             raise ValueError(f"{what} must be a bfloat16 or float16 tensor [rows][{'heads' if heads is None else heads}][{self.head_dim}] on {self.device} "
                              "whose channels lie next to each other")
+        if t.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{what} asks for a gradient, which no call on the cache has: detach it, or call under torch.no_grad()")
         if stream is not None:
             t.record_stream(stream)
         return t

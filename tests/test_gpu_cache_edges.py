@@ -256,3 +256,22 @@ def test_outputs_on_another_stream_take_no_memory_that_is_still_read(call):
     assert at not in {t.data_ptr() for t in more}
     torch.cuda.synchronize()
     assert (y == 3.0).all() and torch.equal(z, more[0]) and f.cache.poll_error() == 0
+
+
+# ------------------------------------------------------------------ gradients
+def test_what_asks_for_a_gradient_is_refused():
+    f = Filled([40, 20], 2, 64, seed=43)
+    q, k, v = f.query([1, 1], 4), f.k[:2].clone(), f.v[:2].clone()
+    want = f.cache.attend(0, q)
+    for t in (q, k, v):
+        t.requires_grad_()
+    for call in (lambda: f.cache.attend(0, q), lambda: f.cache.attend(0, q * 2), lambda: f.cache.write(0, k, v.detach()), lambda: f.cache.write(0, k.detach(), v),
+                 lambda: f.cache.attend(0, q.detach(), out=q)):
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+    assert torch.equal(f.cache.attend(0, q.detach()), want)
+    with torch.no_grad():
+        assert torch.equal(f.cache.attend(0, q), want)
+        f.cache.write(0, k, v)
+    with torch.inference_mode():
+        f.cache.attend(0, q)
