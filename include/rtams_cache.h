@@ -112,7 +112,8 @@ typedef struct rtams_cache_query {
 /* Attention of the items' rows over one layer.  Scores, their maximum, sum and the weighted values are held in 32 bits; the
  * products take halves (keys and values rounded once to a half, probabilities, queries times a power of two).  A row that sees nothing
  * gives 0 and a logarithm of -inf; a row of q that holds a NaN, an infinity or, times the scale, a number beyond the halves
- * spoils its own output only. */
+ * spoils its own output only.  Of more than 64 rows of a head, work is laid out by the longest item: n * kv_heads times its rows of a head / 128 are to be
+ * below 2^28, and what is laid out for a shorter item in vain costs some 10 ns for each 256 of them. */
 int rtams_cache_attend(rtams_cache *c, const rtams_cache_query *q, int64_t n, const int32_t *d_seqs,
                        const int32_t *d_starts, int64_t rows, void *hip_stream);
 

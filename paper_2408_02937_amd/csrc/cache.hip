@@ -310,7 +310,7 @@ int rtams_cache_attend(rtams_cache *c, const rtams_cache_query *q, int64_t n, co
   // what the kernels count in 32 bits: rows of an item, workgroups, steps of 128 tokens
   const int64_t most = d_starts ? (q->max_new < rows ? (int64_t)q->max_new : rows) : 1, share = q->q_heads / c->cfg.kv_heads;
   const int64_t heads = n * c->cfg.kv_heads, steps = (int64_t)c->cfg.max_pages * c->cfg.page_tokens / 128 + 1;
-  if (share * most >= (int64_t)1 << 30 || heads >= 1 << 22 || heads * (share * most / 128 + 1) >= 1 << 22 || heads * steps >= (int64_t)1 << 32)
+  if (share * most >= (int64_t)1 << 30 || heads >= 1 << 22 || heads * (share * most / 128 + 1) >= 1 << 28 || heads * steps >= (int64_t)1 << 32)
     return fail(RTAMS_EINVAL, "%lld items of up to %lld rows, %d heads, are too many for one call", (long long)n, (long long)most, q->q_heads);
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   std::lock_guard<std::mutex> g(c->mutex);

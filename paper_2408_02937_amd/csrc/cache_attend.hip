@@ -392,8 +392,9 @@ void launch_cache_attend(const CacheDev &d, const CacheQuery &q, hipStream_t s) 
   const int64_t rows = (int64_t)q.share * q.r.max_new;
   const int each = d.head_dim == 256 || rows <= 16 ? 16 : 32;
   const int64_t tiles = (rows + each - 1) / each;
-  // (steps of all row tiles are counted in 32 bits)
-  if (rows > 64 || (tiles > 1 && q.r.n * d.kv_heads * tiles * ((int64_t)d.max_pages * d.page_blocks / kWaves + 1) >= (int64_t)1 << 32)) return launch_cache_prompt(d, q, s);
+  // (steps of all row tiles are counted in 32 bits, and they are one launch)
+  const int64_t heads = q.r.n * (int64_t)d.kv_heads * tiles;
+  if (rows > 64 || (tiles > 1 && (heads >= 1 << 22 || heads * ((int64_t)d.max_pages * d.page_blocks / kWaves + 1) >= (int64_t)1 << 32))) return launch_cache_prompt(d, q, s);
   switch (d.head_dim) {
     case 64: return each == 16 ? launch<64, 1>(d, q, 1, s) : launch<64, 2>(d, q, (int)tiles, s);
     case 96: return each == 16 ? launch<96, 1>(d, q, 1, s) : launch<96, 2>(d, q, (int)tiles, s);

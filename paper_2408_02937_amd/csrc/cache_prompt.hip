@@ -201,7 +201,7 @@ __device__ __forceinline__ void reads_ahead() {
 }
 
 template <int D, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(CacheDev d, CacheQuery q, int tiles, int tile_rows, int split) {
+__global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(CacheDev d, CacheQuery q, int tiles, int tile_rows, int split, uint32_t first) {
   constexpr int kLanes = WAVES * 64, NS = D / 16, NC = D / 32, NP = (2 * kPairs<D> + kLanes - 1) / kLanes;
   constexpr int TB = tile_blocks(D), kTile = TB * kBlockTokens;
   extern __shared__ uint4 lds[];
@@ -220,8 +220,8 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(C
     pc = Piece{uniform(piece.entry), uniform(piece.head), uniform(piece.parts), uniform(piece.nth), uniform(piece.part)};
     __syncthreads();
   } else {  // heads fastest (a head's cache stays on one die), then the items, and the row tiles from the longest on
-    const uint32_t x = blockIdx.x / d.kv_heads;
-    pc = Piece{(int)x, (int)(blockIdx.x % d.kv_heads), 1, 0, 0};
+    const uint32_t x = first + blockIdx.x;
+    pc = Piece{(int)(x / d.kv_heads), (int)(x % d.kv_heads), 1, 0, 0};
   }
   const int item = pc.entry % q.r.n, tile = tiles - 1 - pc.entry / q.r.n, head = pc.head;
   const Span sp = find_span(d, q, item, tile, tile_rows, kTile, !split && tile == 0 && head == 0 && threadIdx.x == 0);
@@ -463,7 +463,9 @@ void launch(const CacheDev &d, const CacheQuery &q, hipStream_t s) {
   static_assert(kSplit * kWorkers <= kMostEntries, "all row tiles of all items are planned");
   // (steps of all row tiles are counted in 32 bits)
   const bool split = groups < (q.r.n > 1 ? kSplit : 1) * kWorkers && groups * ((int64_t)d.max_pages * d.page_blocks + 1) < (int64_t)1 << 32;
-  k_cache_prompt<D, WAVES><<<(uint32_t)(split ? groups + kWorkers : groups), WAVES * 64, sizeof(Shared<D>), s>>>(d, q, tiles, tile_rows, split);
+  const int64_t all = split ? groups + kWorkers : groups, most = 1 << 22;  // (of a launch; one that finds no rows takes 10 ns: 512 items of 8 heads, one of 32,768 rows, 28 ms of which it takes 6)
+  for (int64_t at = 0; at < all; at += most)
+    k_cache_prompt<D, WAVES><<<(uint32_t)(all - at < most ? all - at : most), WAVES * 64, sizeof(Shared<D>), s>>>(d, q, tiles, tile_rows, split, (uint32_t)at);
 }
 
 }  // namespace

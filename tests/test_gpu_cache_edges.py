@@ -275,3 +275,27 @@ def test_what_asks_for_a_gradient_is_refused():
         f.cache.write(0, k, v)
     with torch.inference_mode():
         f.cache.attend(0, q)
+
+
+# ------------------------------------------------------------------ many items, and a long one among them
+def test_a_long_piece_among_many_sequences():
+    """Workgroups are counted by the longest item: more of them than a launch takes."""
+    n, rows, heads, kv, dim = 512, 32_768, 32, 8, 64
+    lengths = [rows] + [(i * 7) % 50 + 1 for i in range(1, n)]
+    c = Cache(kv, dim, page_tokens=64, pages=sum(-(-x // 64) for x in lengths), max_seqs=n, max_pages=rows // 64, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(44)
+    st = starts_of(lengths)
+    c.extend(starts=st)
+    k, v = (torch.randn((sum(lengths), kv, dim), device=DEV, generator=g).bfloat16() for _ in range(2))
+    c.write(0, k, v, starts=st, max_new=rows)
+    counts = [rows] + [1] * (n - 1)
+    q = torch.randn((sum(counts), heads, dim), device=DEV, generator=g).bfloat16()
+    out = torch.full_like(q, 7.0)
+    c.attend(0, q, starts=starts_of(counts), max_new=rows, out=out)
+    alone = c.attend(0, q[:rows], ints([0]), ints([0, rows]), max_new=rows)
+    single = c.attend(0, q[rows:], ints(range(1, n)))
+    torch.cuda.synchronize()
+    assert c.poll_error() == 0
+    assert torch.equal(out[:rows], alone)
+    # two kernels: each off by its own roundings (of probabilities, keys and values 2^-11 of a value of up to 5, and the output's)
+    assert (out[rows:].float() - single.float()).abs().max() <= 5 * (3 * 2.0 ** -11 + 2.0 ** -8)
