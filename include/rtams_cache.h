@@ -83,7 +83,7 @@ int rtams_cache_layout(const rtams_cache *c, rtams_cache_view *out);
 int rtams_cache_extend(rtams_cache *c, int64_t n, const int32_t *d_seqs, const int32_t *d_starts, void *hip_stream);
 
 /* One layer's keys and values of the items' rows: d_k and d_v [rows][kv_heads][head_dim] of `type` (BF16 or F16), rows and
- * heads `row_stride` and `head_stride` elements apart (below 2^24), channels next to each other.  max_new: the most rows of one item.
+ * heads `row_stride` and `head_stride` elements apart (below 2^24 and 2^40), channels next to each other.  max_new: the most rows of one item.
  * The items of a sequence that is named twice are left out, with EINVAL.
  * Rows whose page another sequence shares are left out, with EINVAL: extend sees to it that new rows' pages are not. */
 int rtams_cache_write(rtams_cache *c, int32_t layer, int64_t n, const int32_t *d_seqs, const int32_t *d_starts,

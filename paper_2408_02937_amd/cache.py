@@ -125,6 +125,15 @@ class Cache:
             t.record_stream(stream)
         return t
 
+    def _alike(self, k: torch.Tensor, v: torch.Tensor, stream):
+        places = lambda t: [t.stride(d) for d in (0, 1) if t.shape[d] > 1]
+        if k.numel() == 0 or (places(k) == places(v) and (k.shape[0] == 1 or k.stride(0) < 1 << 24)):
+            return k, v
+        if stream is None:
+            return k.contiguous(), v.contiguous()
+        with torch.cuda.stream(stream):
+            return k.contiguous(), v.contiguous()
+
     def _empty(self, shape, dtype: torch.dtype, stream) -> torch.Tensor:
         """Memory for an output: the given stream's own, since what is free on the current one may still be read there by work under way, and
         not used again before the current stream, where the caller has it, is done with it."""
@@ -143,11 +152,14 @@ class Cache:
 
     def write(self, layer: int, k: torch.Tensor, v: torch.Tensor, seqs: Optional[torch.Tensor] = None, starts: Optional[torch.Tensor] = None,
               max_new: Optional[int] = None, stream=None) -> None:
-        """Keys and values of the sequences' last rows, [rows][kv_heads][head_dim]."""
+        """Keys and values of the sequences' last rows, [rows][kv_heads][head_dim].  The kernel takes both at the same strides, rows less than 2^24
+        elements apart; where they are not (keys that were turned, values still in a projection's output), copies are made first."""
         k, v = self._rows(k, self.kv_heads, "k", stream), self._rows(v, self.kv_heads, "v", stream)
-        if k.shape != v.shape or k.dtype != v.dtype or (k.stride() != v.stride() and k.numel()):
-            raise ValueError("k and v must have the same shape, type and strides")
+        if k.shape != v.shape or k.dtype != v.dtype:
+            raise ValueError("k and v must have the same shape and type")
         rows = k.shape[0]
+        if k.stride() != v.stride() or k.stride(0) >= 1 << 24:
+            k, v = self._alike(k, v, stream)
         n, sp, tp, max_new = self._items(seqs, starts, rows if seqs is None and starts is None else None, max_new, stream)
         _chk(self._lib.rtams_cache_write(self._h, layer, n, sp, tp, rows, max_new, k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1),
                                      _TYPES[k.dtype], self._stream(stream)), "rtams_cache_write")

@@ -264,8 +264,11 @@ int rtams_cache_write(rtams_cache *c, int32_t layer, int64_t n, const int32_t *d
   if (!rc) rc = check_rows(c, layer, n, d_starts, rows, max_new);
   if (rc) return rc;
   if (type != RTAMS_TYPE_BF16 && type != RTAMS_TYPE_F16) return fail(RTAMS_EINVAL, "keys and values are bfloat16 or halves, got type %d", type);
-  if (row_stride < 0 || row_stride >= 1 << 24 || head_stride < 0 || head_stride >= 1 << 24)
-    return fail(RTAMS_EINVAL, "strides must be in 0..2^24 - 1 elements, got %lld and %lld", (long long)row_stride, (long long)head_stride);
+  // (of one row, or of one head, the stride says nothing)
+  if (rows == 1) row_stride = 0;
+  if (c->cfg.kv_heads == 1) head_stride = 0;
+  if (row_stride < 0 || row_stride >= 1 << 24 || head_stride < 0 || head_stride >= (int64_t)1 << 40)
+    return fail(RTAMS_EINVAL, "strides must be in 0..2^24 - 1 elements for rows and 0..2^40 - 1 for heads, got %lld and %lld", (long long)row_stride, (long long)head_stride);
   if (n == 0 || rows == 0) return RTAMS_OK;
   if (!d_k || !d_v) return fail(RTAMS_EINVAL, "keys or values are NULL");
   if (((uintptr_t)d_k | (uintptr_t)d_v) % 2) return fail(RTAMS_EINVAL, "keys and values must be 2-byte aligned");

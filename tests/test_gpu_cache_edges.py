@@ -299,3 +299,64 @@ def test_a_long_piece_among_many_sequences():
     assert torch.equal(out[:rows], alone)
     # two kernels: each off by its own roundings (of probabilities, keys and values 2^-11 of a value of up to 5, and the output's)
     assert (out[rows:].float() - single.float()).abs().max() <= 5 * (3 * 2.0 ** -11 + 2.0 ** -8)
+
+
+# ------------------------------------------------------------------ strides
+def test_strides_that_no_place_depends_on():
+    """Of one row, and of one head, the stride says nothing; heads may lie as far apart as they do."""
+    g = torch.Generator(device=DEV).manual_seed(45)
+    base = [torch.randn((2, 1, 64), device=DEV, generator=g).bfloat16() for _ in range(2)]
+    c, want = (Cache(1, 64, page_tokens=32, pages=2, max_seqs=2, device=DEV) for _ in range(2))
+    for x in (c, want):
+        x.extend(n=2)
+    want.write(0, *base)
+    one = [x[1:2].as_strided((1, 1, 64), (1 << 26, 1 << 25, 1)) for x in base]
+    c.write(0, base[0][:1].as_strided((1, 1, 64), (7, 3, 1)), base[1][:1].as_strided((1, 1, 64), (64, 1 << 30, 1)), ints([0]))
+    c.write(0, *one, ints([1]))
+    two = [torch.empty((2, 1, 64), dtype=torch.bfloat16, device=DEV).as_strided((2, 1, 64), (64, s, 1)).copy_(x) for s, x in zip((1 << 28, 5), base)]
+    for _ in range(2):
+        for x, y in zip(c.read(0, 2), want.read(0, 2)):
+            assert torch.equal(x, y)
+        c.write(0, *two)
+    assert c.poll_error() == 0
+    far = torch.empty((2, 131_072, 128), dtype=torch.float16, device=DEV)[:, -40:]  # heads 2^24 elements apart
+    far.copy_(torch.randn((2, 40, 128), device=DEV, generator=g))
+    c, want = (Cache(2, 128, page_tokens=32, pages=2, max_seqs=1, device=DEV) for _ in range(2))
+    st = ints([0, 40])
+    for x, t in ((c, far.transpose(0, 1)), (want, far.transpose(0, 1).contiguous())):
+        x.extend(starts=st)
+        x.write(0, t, t, starts=st, max_new=40)
+    for x, y in zip(c.read(0, 40, starts=st, max_new=40), want.read(0, 40, starts=st, max_new=40)):
+        assert torch.equal(x, y)
+    q = far.transpose(0, 1)
+    assert torch.equal(c.attend(0, q, starts=st, max_new=40), want.attend(0, q.contiguous(), starts=st, max_new=40))
+
+
+def test_keys_and_values_of_different_strides():
+    """Keys that were turned, values still in the fused projection; also on another stream, whose keys are only made there."""
+    g = torch.Generator(device=DEV).manual_seed(46)
+    rows, h, d = 41, 4, 64
+    fused = torch.randn((rows, 3 * h * d), device=DEV, generator=g).half()
+    k, v = fused[:, h * d:2 * h * d].view(rows, h, d), fused[:, 2 * h * d:].view(rows, h, d)
+    st = ints([0, rows])
+    caches = [Cache(h, d, page_tokens=32, pages=3, max_seqs=1, device=DEV) for _ in range(4)]
+    for c in caches:
+        c.extend(starts=st)
+    caches[0].write(0, k.contiguous(), v.contiguous(), starts=st, max_new=rows)
+    caches[1].write(0, k.contiguous(), v, starts=st, max_new=rows)
+    caches[2].write(0, k, v.permute(1, 0, 2).contiguous().permute(1, 0, 2), starts=st, max_new=rows)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    a = torch.randn((4096, 4096), device=DEV)
+    with torch.cuda.stream(s):
+        for _ in range(20):
+            a @ a
+        late = torch.zeros_like(v.contiguous())
+        late.copy_(v)
+    caches[3].write(0, k, late, starts=st, max_new=rows, stream=s)
+    torch.cuda.synchronize()
+    want = caches[0].read(0, rows, starts=st, max_new=rows)
+    for c in caches[1:]:
+        assert c.poll_error() == 0
+        for x, y in zip(c.read(0, rows, starts=st, max_new=rows), want):
+            assert torch.equal(x, y)
