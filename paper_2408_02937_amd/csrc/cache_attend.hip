@@ -111,7 +111,9 @@ __device__ bool find_piece(const CacheDev &d, const CacheQuery &q, int tiles, ui
     all += last_lane(wave_running_sum(sum));
   }
   all *= (uint32_t)d.kv_heads;
-  // where items are many, pieces are an even share at most, and long items do not keep the others waiting
+  // Where items are many, pieces are an even share, and long items do not keep the others waiting.  (Never less than an even share: scratch has room
+  // for twice as many parts as there are workers.  A head of s steps that is split, s > size, has fewer than 2 s / size parts, all of them fewer than
+  // 2 all / size.)
   const uint32_t share = (all + workers - 1) / workers;
   uint32_t size = share > 1 ? share : 1;
   if (share > 1 && n <= kItems && n * d.kv_heads * tiles <= (int)workers / 2) {

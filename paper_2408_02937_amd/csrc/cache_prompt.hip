@@ -166,6 +166,7 @@ __device__ inline bool find_piece(const CacheDev &d, const CacheQuery &q, int ti
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) longest = fmaxf(longest, __shfl_xor(longest, o));
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  // (never less than an even share: scratch has room for twice as many parts as there are workers, as in cache_attend.hip)
   const uint32_t share = max(1u, (all * (uint32_t)d.kv_heads + workers - 1) / workers), size = share > 1 ? piece_steps(steps, n, d.kv_heads, share, workers) : 1;
   // pieces from the longest on, by eighths: what comes last then fills what is left
   const float one_over = 1.0f / (float)size, per_class = kClasses / fminf((float)size, longest);

@@ -360,3 +360,63 @@ def test_keys_and_values_of_different_strides():
         assert c.poll_error() == 0
         for x, y in zip(c.read(0, rows, starts=st, max_new=rows), want):
             assert torch.equal(x, y)
+
+
+# ------------------------------------------------------------------ what no test looked at
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("dim", [64, 96, 128, 256])
+def test_values_read_back_in_fewer_bits(dim, dtype):
+    """The values in 32 bits, rounded once to the nearest."""
+    f = Filled([70, 1, 33], 3, dim, page=64, dtype=dtype, seed=dim)
+    f.cache.write(0, f.k * 50, f.v * 1e-6, starts=starts_of(f.lengths), max_new=70)
+    args = dict(starts=starts_of([69, 1, 20]), max_new=69)
+    for x, y in zip(f.cache.read(0, 90, dtype=dtype, **args), f.cache.read(0, 90, **args)):
+        assert x.dtype == dtype and torch.equal(x, y.to(dtype))
+    assert f.cache.poll_error() == 0
+
+
+def test_a_token_past_a_sequences_last_page():
+    """Among others that have room, without starts: nothing changes, and the error says which it was."""
+    c = Cache(1, 64, page_tokens=32, pages=9, max_seqs=4, max_pages=2, device=DEV)
+    c.extend(starts=ints([0, 64, 94, 126, 126]))
+    state = [x.clone() for x in (c.table, c.lengths, c.refs)]
+    for call in (lambda: c.extend(n=4), lambda: c.extend(ints([1, 0])), lambda: c.extend(ints([0]), ints([0, 1]))):
+        call()
+        torch.cuda.synchronize()
+        assert c.poll_error() == rtams.EINVAL
+        assert all(torch.equal(x, y) for x, y in zip(state, (c.table, c.lengths, c.refs)))
+        c.clear_error()
+    c.extend(ints([1, 2, 3]))
+    assert c.lengths.tolist() == [64, 31, 33, 1] and c.poll_error() == 0
+
+
+# ------------------------------------------------------------------ scratch
+@pytest.mark.parametrize("dim,kv,n,share,count,tokens", [(64, 100, 12, 1, 1, 17 * 128), (64, 100, 7, 4, 8, 9 * 128), (96, 50, 20, 2, 1, 12 * 128), (96, 50, 10, 4, 8, 8 * 128),
+                                                         (128, 50, 14, 4, 1, 12 * 128), (128, 50, 10, 8, 8, 7 * 128), (256, 50, 5, 2, 1, 12 * 128), (256, 31, 2, 8, 8, 9 * 128),
+                                                         (64, 50, 5, 1, 100, 9 * 128), (96, 50, 5, 1, 256, 9 * 128), (128, 31, 8, 4, 64, 1100), (256, 31, 8, 2, 64, 1000)])
+def test_parts_of_rows_stay_in_their_scratch(dim, kv, n, share, count, tokens, monkeypatch):
+    """Pieces a little shorter than what they are cut from, so that parts are as many as they can be: what lies behind the scratch is not touched, and a call
+    gives what its items give one by one, but for the order of sums."""
+    from paper_2408_02937_amd import cache as module
+    kept = []
+
+    def more(nbytes, device):
+        kept.append(torch.full((nbytes + (64 << 20),), 0x5A, dtype=torch.uint8, device=device))
+        return kept[-1][:nbytes]
+
+    monkeypatch.setattr(module, "_device_bytes", more)
+    c = Cache(kv, dim, page_tokens=128, pages=n * -(-tokens // 128), max_seqs=n, max_pages=-(-tokens // 128), device=DEV)
+    scratch = c.scratch.numel()
+    st = starts_of([tokens] * n)
+    c.extend(starts=st)
+    g = torch.Generator(device=DEV).manual_seed(48)
+    k, v = (torch.randn((n * tokens, kv, dim), device=DEV, generator=g).half() for _ in range(2))
+    c.write(0, k, v, starts=st, max_new=tokens)
+    q = torch.randn((n * count, kv * share, dim), device=DEV, generator=g).half()
+    out = c.attend(0, q, starts=starts_of([count] * n), max_new=count, causal=False)
+    apart = torch.cat([c.attend(0, q[i * count:(i + 1) * count], ints([i]), ints([0, count]), max_new=count, causal=False) for i in range(n)])
+    torch.cuda.synchronize()
+    assert c.poll_error() == 0 and kept[1].numel() == scratch + (64 << 20)
+    assert (kept[1][scratch:] == 0x5A).all()
+    # (probabilities of one part or another relative to another maximum: each rounded to 2^-11 of itself, times values of up to 5; and the outputs')
+    assert (out.float() - apart.float()).abs().max() <= 5 * (2 * 2.0 ** -11) + 2.0 ** -9
