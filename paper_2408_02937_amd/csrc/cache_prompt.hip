@@ -260,10 +260,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(C
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[c][e] = 0.0f;
   const float rest = q.scale_rest;  // scores and their maximum are what it multiplies
-  // (a row's sum is that of up to kRun tiles at a time: a long tail's probabilities one by one would be lost in it.  Of each tile: heads of 64, 96, 128, 256
-  // channels, prompts of 4,534, 2 heads of 8: 112, 128, 145, 417 us, of eight 111, 125, 145, 412, without 111, 124, 146, 402)
-  constexpr int kRun = 8;
-  float m = real ? -INFINITY : 0.0f, l = 0.0f, part = 0.0f;
+  float m = real ? -INFINITY : 0.0f, l = 0.0f;
   f32x16 start;  // of the scores' sums: less the maximum
 #pragma unroll
   for (int e = 0; e < 16; ++e) start[e] = 0.0f;
@@ -345,8 +342,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(C
       const bool move = top * rest > kTop + kLag || (m == -INFINITY && top > -INFINITY);  // (scores are relative to the maximum)
       const float by = move ? top - kTop * __builtin_amdgcn_rcpf(rest) : 0.0f, shrink = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(-by * rest);
       if (move) m = (m == -INFINITY ? 0.0f : m) + by;
-      l = (l + part) * shrink;
-      part = 0.0f;
+      l *= shrink;
 #pragma unroll
       for (int c = 0; c < NC; ++c) o[c] *= shrink;
 #pragma unroll
@@ -354,8 +350,10 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(C
       start -= by;
       powers();
     }
+    // (32 tokens first: a long tail's probabilities one by one would be lost in the row's sum.  The row's sum itself, 64 tokens, 32: heads of 64, 96, 128, 256
+    // channels, prompts of 4,534, 2 heads of 8: 111, 124, 144, 417 us; 113, 127, 142, 407; 112, 125, 142, 408)
 #pragma unroll
-    for (int x = 0; x < TB; ++x) part = add_up(add_up(part, pf[x][0]), pf[x][1]);
+    for (int x = 0; x < TB; ++x) l += add_up(add_up(0.0f, pf[x][0]), pf[x][1]);
   };
   const auto weigh = [&](const uint4 *vt) {
 #pragma unroll
@@ -394,14 +392,9 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(C
         weigh(sh.v[now]);
         __builtin_amdgcn_s_setprio(0);
       }
-      if (t % kRun == 0) {
-        l += part;
-        part = 0.0f;
-      }
       __syncthreads();
     }
   }
-  l += part;
   l += __shfl_xor(l, 32);
   m *= rest;
 
