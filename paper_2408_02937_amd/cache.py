@@ -135,10 +135,8 @@ class Cache:
             return k.contiguous(), v.contiguous()
 
     def _empty(self, shape, dtype: torch.dtype, stream) -> torch.Tensor:
-        """Memory for an output: the given stream's own, since what is free on the current one may still be read there by work under way, and
-        not used again before the current stream, where the caller has it, is done with it."""
-        if stream is None:
-            return torch.empty(shape, dtype=dtype, device=self.device)
+        """Memory for an output on a stream given: that stream's own, since what is free on the current one may still be read there by work under
+        way, and not used again before the current stream, where the caller has it, is done with it."""
         with torch.cuda.stream(stream):
             t = torch.empty(shape, dtype=dtype, device=self.device)
         t.record_stream(torch.cuda.current_stream(self.device))
@@ -158,10 +156,12 @@ class Cache:
         if k.shape != v.shape or k.dtype != v.dtype:
             raise ValueError("k and v must have the same shape and type")
         rows = k.shape[0]
-        if k.stride() != v.stride() or k.stride(0) >= 1 << 24:
+        strides = k.stride()
+        if strides != v.stride() or strides[0] >= 1 << 24:
             k, v = self._alike(k, v, stream)
+            strides = k.stride()
         n, sp, tp, max_new = self._items(seqs, starts, rows if seqs is None and starts is None else None, max_new, stream)
-        _chk(self._lib.rtams_cache_write(self._h, layer, n, sp, tp, rows, max_new, k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1),
+        _chk(self._lib.rtams_cache_write(self._h, layer, n, sp, tp, rows, max_new, k.data_ptr(), v.data_ptr(), strides[0], strides[1],
                                      _TYPES[k.dtype], self._stream(stream)), "rtams_cache_write")
 
     def read(self, layer: int, rows: int, seqs: Optional[torch.Tensor] = None, starts: Optional[torch.Tensor] = None,
@@ -170,7 +170,12 @@ class Cache:
         if dtype not in _TYPES:
             raise ValueError("dtype must be bfloat16, float16 or float32")
         n, sp, tp, max_new = self._items(seqs, starts, rows if seqs is None and starts is None else None, max_new, stream)
-        k, v = (self._empty((rows, self.kv_heads, self.head_dim), dtype, stream) for _ in range(2))
+        shape = (rows, self.kv_heads, self.head_dim)
+        if stream is None:
+            k = torch.empty(shape, dtype=dtype, device=self.device)
+            v = torch.empty_like(k)
+        else:
+            k, v = self._empty(shape, dtype, stream), self._empty(shape, dtype, stream)
         _chk(self._lib.rtams_cache_read(self._h, layer, n, sp, tp, rows, max_new, k.data_ptr(), v.data_ptr(), _TYPES[dtype], self._stream(stream)),
              "rtams_cache_read")
         return k, v
@@ -184,7 +189,8 @@ class Cache:
         rows, heads = q.shape[0], q.shape[1]
         n, sp, tp, max_new = self._items(seqs, starts, rows if seqs is None and starts is None else None, max_new, stream)
         if out is None:
-            out = self._empty((rows, heads, self.head_dim), q.dtype, stream)
+            shape = (rows, heads, self.head_dim)
+            out = q.new_empty(shape) if stream is None else self._empty(shape, q.dtype, stream)
         elif self._rows(out, heads, "out", stream).shape != q.shape or out.dtype != q.dtype:
             raise ValueError("out must have the shape and type of q")
         lp = None
