@@ -83,8 +83,8 @@ int rtams_cache_layout(const rtams_cache *c, rtams_cache_view *out);
 int rtams_cache_extend(rtams_cache *c, int64_t n, const int32_t *d_seqs, const int32_t *d_starts, void *hip_stream);
 
 /* One layer's keys and values of the items' rows: d_k and d_v [rows][kv_heads][head_dim] of `type` (BF16 or F16), rows and
- * heads `row_stride` and `head_stride` elements apart (below 2^24 and 2^40), channels next to each other.  max_new: the most rows of one item.
- * The items of a sequence that is named twice are left out, with EINVAL.
+ * heads `row_stride` and `head_stride` elements apart (below 2^24 and 2^40; of a single row or head it says nothing), channels
+ * next to each other.  max_new: the most rows of one item.  The items of a sequence that is named twice are left out, with EINVAL.
  * Rows whose page another sequence shares are left out, with EINVAL: extend sees to it that new rows' pages are not. */
 int rtams_cache_write(rtams_cache *c, int32_t layer, int64_t n, const int32_t *d_seqs, const int32_t *d_starts,
                       int64_t rows, int32_t max_new, const void *d_k, const void *d_v, int64_t row_stride,
@@ -110,10 +110,11 @@ typedef struct rtams_cache_query {
 } rtams_cache_query;
 
 /* Attention of the items' rows over one layer.  Scores, their maximum, sum and the weighted values are held in 32 bits; the
- * products take halves (keys and values rounded once to a half, probabilities, queries times a power of two).  A row that sees nothing
- * gives 0 and a logarithm of -inf; a row of q that holds a NaN, an infinity or, times the scale, a number beyond the halves
- * spoils its own output only.  Of more than 64 rows of a head, work is laid out by the longest item: n * kv_heads times its rows of a head / 128 are to be
- * below 2^28, and what is laid out for a shorter item in vain costs some 10 ns for each 256 of them. */
+ * products take halves: keys and values rounded once, queries times a power of two, and probabilities, of which a row's largest
+ * stands at 2^7 to 2^15, so that one 2^-32 of it may be lost.  A row that sees nothing gives 0 and a logarithm of -inf; a row of
+ * q that holds a NaN, an infinity or, times the scale, a number beyond the halves spoils its own output only.
+ * Of more than 64 rows of a head, work is laid out by the longest item: n * kv_heads * (its rows of a head / 128 + 1) has to be
+ * below 2^28, and what is laid out for shorter items in vain takes some 10 ns for each 256 rows. */
 int rtams_cache_attend(rtams_cache *c, const rtams_cache_query *q, int64_t n, const int32_t *d_seqs,
                        const int32_t *d_starts, int64_t rows, void *hip_stream);
 

@@ -11,8 +11,8 @@
 // same instruction that takes the maximum off.  What a piece leaves of a row goes to scratch; the last piece of it to arrive joins them, in order.
 //
 // Measured: 8 sequences of 16 to 131 thousand tokens, 8 heads of 128, 32 query heads: 170 us for 874 MB, 5.1 TB/s where a plain read of 4 GiB reaches
-// 6.0.  32 of 0.5 to 4 thousand: 26.6 us for 94 MB; of these 3 are the plan, 5 pass until the first blocks are there, 3 are the join.
-// One token over 100: 5.7 us.  Heads of 64, 96, 128, 256 channels, 8 times 32,000 tokens each: 4.4, 5.0, 5.0, 5.0 TB/s.
+// 6.0.  32 of 0.5 to 4 thousand: 26.9 us for 94 MB; of these 3 are the plan, 5 pass until the first blocks are there, 3 are the join.
+// One token over 100: 4.8 us.  Heads of 64, 96, 128, 256 channels, 8 times 32,000 tokens each: 4.2, 4.7, 4.7, 5.0 TB/s.
 #include "../../include/rtams_cache.h"
 
 #include "cache_mm.h"
@@ -389,8 +389,9 @@ size_t cache_arrived_words(int max_seqs, int kv_heads) {
 
 void launch_cache_attend(const CacheDev &d, const CacheQuery &q, hipStream_t s) {
   // Against the kernel for many rows, 8 sequences of up to 32,000 tokens and 8 heads: of 128 channels 32, 40, 64, 96, 128 rows take 69, 111, 108, 159,
-  // 186 us here and 144 to 152 there; of 256 channels 24, 32, 40, 64 rows 201, 203, 370, 425 us and 391 to 403.  32 of up to 2,000, 64 rows: 50 and 51,
-  // of 256 channels 104 and 143.
+  // 186 us here and 144 to 152 there; of 256 channels 24, 32, 40, 48, 64 rows 200, 201, 368, 369, 421 us and 420 to 433.  64 rows of 64, 96, 256 channels:
+  // one sequence of 32,000 34, 42, 71 us and 66, 86, 160; 8 of up to 8,000 28, 36, 122 and 41, 49, 129; 32 of up to 2,000 29, 34, 105 and 44, 51, 153,
+  // of 128 channels 50 and 51.
   const int64_t rows = (int64_t)q.share * q.r.max_new;
   const int each = d.head_dim == 256 || rows <= 16 ? 16 : 32;
   const int64_t tiles = (rows + each - 1) / each;

@@ -76,7 +76,9 @@ struct KeyTile {
       }
     }
   }
-  // Eight channels, rounded once to a half.
+  // Eight channels, rounded once to a half, as the matrix instructions take them: by 2^-11 of a value at most, half a unit in the last place of a half and
+  // less of a bfloat16 that was written, but more than a step of the codes where a group's zero is above 2^11 steps; reading back has the values in 32
+  // bits.  (Exact, zeros would be products of their own beside those of the codes.)
   __device__ half8 values(int j) const {
     HalfWords x = codes_of(code[j]);
     const uint32_t mt = meta[D == 96 ? j : j / 4];

@@ -5,7 +5,7 @@
 // a function of the table: counts are added with atomics, whose order shows nowhere.  Tables are small (four bytes a page); what
 // moves bytes, a copy of whole pages, runs on the whole chip in pieces of 16 KiB.
 //
-// Planning is a chain of loads and barriers on one compute unit: 4.6 us for a token each of 48 sequences, 2.4 for a trim, 5.7 for a fork of 32, 6.2
+// Planning is a chain of loads and barriers on one compute unit: 4.8 us for a token each of 48 sequences, 2 to 4 for a trim, 5.8 for a fork of 32, 6.1
 // for the plan of a compaction.  Copies are bound by memory: 3.3 GB read and written in 655 us, 5.1 TB/s; 354 MB in 76 us, 4.6.
 #include "../../include/rtams_cache.h"
 

@@ -12,10 +12,11 @@
 // The scale's power of two is in the query, exact as an operand; what is left of it multiplies scores in 32 bits (in the query and rounded there:
 // 576 us instead of 580, and half outputs 1.6 to 1.8 times as far from 64 bits as their own rounding alone, not 1.5 to 1.6).
 //
-// Measured: a prompt of 8,192 tokens, 32 heads of 128 over 8: 580 us for 550 GFLOP, 947 TFLOP/s where a plain product of 8,192 squared reaches 1,140
-// in bfloat16 and 1,084 in halves.  Vector instructions (exponentials, masks, codes) and matrix instructions take 41 % of the cycles each and
-// two wavefronts of a SIMD overlap them in part.  Heads of 64, 96, 256: 613, 626, 357 TFLOP/s: at 64 exponentials are twice as many for a flop; at 256
-// one wavefront fits a SIMD.  4 wavefronts a workgroup at 128 channels: 710 us; wavefronts half a tile apart: 610.
+// Measured: a prompt of 8,192 tokens, 32 heads of 128 over 8: 575 to 640 us from card to card for 550 GFLOP, 860 to 957 TFLOP/s where a plain product
+// of 8,192 squared reaches 1,140 in bfloat16 and 1,084 in halves.  Vector instructions (exponentials, masks, codes) take 48 % of the cycles, matrix
+// instructions 41 %, and two wavefronts of a SIMD overlap them in part.  Heads of 64, 96, 128, 256 on one card: 455, 551, 640, 2,314 us; 604, 749, 859,
+// 475 TFLOP/s: the fewer the channels, the more exponentials for a flop; at 256 one wavefront fits a SIMD.  At 128 channels, on a card of 580 us:
+// 4 wavefronts a workgroup 710, wavefronts half a tile apart 610.
 #include "../../include/rtams_cache.h"
 
 #include <climits>
@@ -137,9 +138,13 @@ struct Piece {
   int parts, nth, part;  // pieces of the head's row tile; which one this is; where its parts begin, if there are several
 };
 
-// From so many times the workgroups that run at once (one item: from as many) nothing is planned.  With a plan and without, 8 heads of 128: 8 items of
-// up to 5,000 tokens and 600 rows 295 and 380 us, 12 of up to 3,000 and 512 rows 213 and 241, 2 of 4,000 and 2,000 rows 161 and 196; all as long 456 and
-// 452, 311 and 301, 220 and 216.  One prompt of 3,000: 101 and 101, of 7,000: 447 and 430.
+// From so many times the workgroups that run at once (one item: from as many) nothing is planned.  With a plan and without, 8 heads: 8 items of up to
+// 5,000 tokens and 600 rows, 12 of up to 3,000 and 512 rows, 2 of up to 4,000 and 2,000 rows, ragged and then all as long:
+//    64 channels  232, 161, 122 us and 298, 184, 150   341, 224, 161 us and 333, 213, 152
+//    96           252, 187, 141        340, 211, 174   397, 269, 191        390, 256, 186
+//   128           304, 222, 170        401, 253, 214   482, 331, 237        477, 321, 234
+//   256           1535, 960, 634       1540, 960, 876  1673, 1221, 901      1674, 1221, 881
+// One prompt of 3,000, 128 channels: 101 and 101, of 7,000: 447 and 430.
 constexpr int kSplit = 4;
 constexpr int kMostEntries = 1024;  // row tiles of items that are planned
 constexpr int kClasses = 8;         // of their pieces, by length

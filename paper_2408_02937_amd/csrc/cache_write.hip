@@ -6,8 +6,8 @@
 // channel on the side of the rows, 1.25 on that of the cache.  Of single tokens they are a chain of loads (length, page, count), so the
 // rows are asked for before the page is known.
 //
-// Measured: 34,439 rows of 8 heads of 128 channels, keys and values: read back in 31 us for 185 MB, 5.9 TB/s; written in 57 us, 3.2 TB/s: vector
-// instructions take 60 % of the cycles, wavefronts wait for 56 % of their time.
+// Measured: 34,439 rows of 8 heads of 128 channels, keys and values: read back in 31 us for 185 MB, 5.9 TB/s; written in 56 us, 3.3 TB/s: vector
+// instructions take 62 % of the cycles.
 // 64 single rows: 5 us written, 4 read.  Four heads a workgroup took 72 us (half as many run at once), 8 workgroups a unit forced 92 (registers spill).
 #include "../../include/rtams_cache.h"
 
