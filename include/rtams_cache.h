@@ -118,6 +118,41 @@ typedef struct rtams_cache_query {
 int rtams_cache_attend(rtams_cache *c, const rtams_cache_query *q, int64_t n, const int32_t *d_seqs,
                        const int32_t *d_starts, int64_t rows, void *hip_stream);
 
+/* What rows see besides what a query says.  All zero: nothing else. */
+typedef struct rtams_cache_sight {
+  int32_t sinks;          /* with a window: the sequence's first `sinks` positions stay visible (up to a row's own) */
+  int32_t tree_words;     /* words of a row of d_tree: a bit for each of max_new rows, at most 32 words */
+  const uint32_t *d_tree; /* [rows][tree_words]: bit i of row j's words: it sees row i of its item.  NULL: the rows up to itself */
+} rtams_cache_sight;
+
+/* rtams_cache_attend with a sight (NULL: none).  With a tree, which is causal, the items' rows stand side by side in the cache, but each sees of
+ * them those that its bits name, whatever their order, and what lies before the item's first row.  Its own position, from which a window
+ * counts, is the one behind as many rows as its bits name: base + bits - 1, base being that of the item's first row; rows that it names it sees whatever the window.
+ * (A tree that is a chain is what no tree is, while the window has room for the chain.)  Bits beyond the item's rows say nothing. */
+int rtams_cache_attend_sight(rtams_cache *c, const rtams_cache_query *q, const rtams_cache_sight *sight, int64_t n,
+                             const int32_t *d_seqs, const int32_t *d_starts, int64_t rows, void *hip_stream);
+
+/* Trees of drafted tokens.  An item's rows are the nodes of a tree, at most 1024 of them: d_parents[row] is the number, within the item, of the row
+ * that a row follows, which is lower than its own, or -1.  An item of which that does not hold raises EINVAL.
+ *
+ * What each row sees: d_tree as rtams_cache_sight takes it, its ancestors and itself, and d_positions (NULL: not asked for) the position in the
+ * sequence that it would have if its path were all there is: rows of the same depth stand at the same one. */
+int rtams_cache_tree(rtams_cache *c, int64_t n, const int32_t *d_seqs, const int32_t *d_starts, int64_t rows, int32_t max_new,
+                     const int32_t *d_parents, uint32_t *d_tree, int32_t tree_words, int32_t *d_positions, void *hip_stream);
+
+/* The path that a model's choices follow.  d_tokens[row] is the token of a row, d_chosen[row] the one that was chosen behind it.  The path begins at the
+ * item's row 0 and goes on to the first row whose parent is the path's last and whose token, not negative, was chosen there.  d_path [rows]: the rows'
+ * numbers within the item, then -1; d_kept [n]: how many; d_next [n]: the token chosen behind the last.  Items without rows have 0 and -1,
+ * items that raise EINVAL -1 and -1.  (The cache's own state is not read.) */
+int rtams_cache_walk(rtams_cache *c, int64_t n, const int32_t *d_starts, int64_t rows, int32_t max_new, const int32_t *d_parents,
+                     const int32_t *d_tokens, const int32_t *d_chosen, int32_t *d_path, int32_t *d_kept, int32_t *d_next, void *hip_stream);
+
+/* Of each item's rows the d_kept[i] that the first entries of its d_path name, in ascending order, move to the front, in all layers, and the sequence is cut
+ * behind them; pages that nothing lies in any more are free.  A call that changes the table: dropped as a whole where an item is not what it asks for or would write into a
+ * page that another sequence shares (EINVAL), and after an extend that was dropped. */
+int rtams_cache_keep(rtams_cache *c, int64_t n, const int32_t *d_seqs, const int32_t *d_starts, int64_t rows, int32_t max_new,
+                     const int32_t *d_path, const int32_t *d_kept, void *hip_stream);
+
 /* Sequence d_dst[i], which is empty, becomes what d_src[i] is: naming the same pages, or (copy != 0) pages of its own with
  * the same contents.  A source may be named several times, a destination once and not as a source. */
 int rtams_cache_fork(rtams_cache *c, int64_t n, const int32_t *d_src, const int32_t *d_dst, int32_t copy,

@@ -10,6 +10,9 @@ stream: they may be dropped when the call has returned.  Nothing here has a grad
     for layer in range(2):
         c.write(layer, k, v, seqs, starts, max_new)     # k, v [rows][8][128] bfloat16 or float16
         out = c.attend(layer, q, seqs, starts, max_new) # q [rows][heads][128], a multiple of 8 heads
+    tree, positions = c.tree(parents, seqs, starts, max_new)       # rows that are trees of drafted tokens: attend(..., tree=tree),
+    path, kept, following = c.walk(parents, tokens, chosen, starts, max_new)  # the path that the model's choices follow,
+    c.keep(path, kept, seqs, starts, max_new)           # and its rows, which stay
     c.fork(src, dst)                                    # branches share pages until they grow
     c.trim(seqs)                                        # ... and are freed
 """
@@ -22,10 +25,12 @@ from typing import Optional, Tuple
 import torch
 
 from paper_2408_02937_amd import rtams
-from paper_2408_02937_amd.rtams import CacheConfig, CacheQuery, CacheView, _chk, _device_bytes, lib
+from paper_2408_02937_amd.rtams import CacheConfig, CacheQuery, CacheSight, CacheView, _chk, _device_bytes, lib
 
 _query = struct.Struct("@iiiiiifPqqPqqP").pack  # CacheQuery, three times as fast as its fields one by one
 assert struct.calcsize("@iiiiiifPqqPqqP") == C.sizeof(CacheQuery)
+_sight = struct.Struct("@iiP").pack  # CacheSight
+assert struct.calcsize("@iiP") == C.sizeof(CacheSight)
 _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 _TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 
@@ -182,9 +187,11 @@ class Cache:
 
     def attend(self, layer: int, q: torch.Tensor, seqs: Optional[torch.Tensor] = None, starts: Optional[torch.Tensor] = None,
                max_new: Optional[int] = None, scale: Optional[float] = None, causal: bool = True, window: int = 0,
-               out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+               out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, stream=None, sinks: int = 0,
+               tree: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Attention of the sequences' last rows, q [rows][heads][head_dim]; lse: float32 [rows][heads] that takes the
-        logarithms of the sums of exp(score)."""
+        logarithms of the sums of exp(score).  sinks: with a window, the first so many positions stay visible.  tree: int32 [rows][words], bit i of
+        a row's words: of its item's rows it sees row i (what `tree` makes of parents), and all before them."""
         q = self._rows(q, None, "q", stream)
         rows, heads = q.shape[0], q.shape[1]
         n, sp, tp, max_new = self._items(seqs, starts, rows if seqs is None and starts is None else None, max_new, stream)
@@ -202,8 +209,54 @@ class Cache:
             lp = lse.data_ptr()
         cq = _query(layer, heads, _TYPES[q.dtype], int(causal), window, max_new, self.head_dim ** -0.5 if scale is None else scale,
                         q.data_ptr(), q.stride(0), q.stride(1), out.data_ptr(), out.stride(0), out.stride(1), lp or 0)
-        _chk(self._lib.rtams_cache_attend(self._h, cq, n, sp, tp, rows, self._stream(stream)), "rtams_cache_attend")
+        if not sinks and tree is None:
+            _chk(self._lib.rtams_cache_attend(self._h, cq, n, sp, tp, rows, self._stream(stream)), "rtams_cache_attend")
+            return out
+        words = trp = 0
+        if tree is not None:
+            if not (tree.dtype == torch.int32 and tree.dim() == 2 and tree.shape[0] == rows and tree.shape[1] > 0 and tree.is_contiguous() and tree.device == self.device):
+                raise ValueError(f"tree must be a contiguous int32 tensor [rows][words] on {self.device}")
+            if stream is not None:
+                tree.record_stream(stream)
+            words, trp = tree.shape[1], tree.data_ptr()
+            if rows == 0:
+                return out
+        _chk(self._lib.rtams_cache_attend_sight(self._h, cq, _sight(sinks, words, trp), n, sp, tp, rows, self._stream(stream)), "rtams_cache_attend_sight")
         return out
+
+    # ---- trees of drafted tokens
+    def _new(self, like: torch.Tensor, shape, stream) -> torch.Tensor:
+        return like.new_empty(shape) if stream is None else self._empty(shape, torch.int32, stream)
+
+    def tree(self, parents: torch.Tensor, seqs: Optional[torch.Tensor] = None, starts: Optional[torch.Tensor] = None, max_new: Optional[int] = None,
+             stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """(tree, positions) of the sequences' last rows, which follow `parents` [rows]: each the number, within its item, of an earlier row, or -1.
+        tree is what attend takes; rows of one depth stand at one position."""
+        pp, rows = self._ints(parents, "parents", None, stream), parents.shape[0]
+        n, sp, tp, max_new = self._items(seqs, starts, rows if seqs is None and starts is None else None, max_new, stream)
+        words = (min(max_new, rows) + 31) // 32
+        tree, positions = self._new(parents, (rows, words), stream), self._new(parents, (rows,), stream)
+        _chk(self._lib.rtams_cache_tree(self._h, n, sp, tp, rows, max_new, pp, tree.data_ptr(), words, positions.data_ptr(), self._stream(stream)), "rtams_cache_tree")
+        return tree, positions
+
+    def walk(self, parents: torch.Tensor, tokens: torch.Tensor, chosen: torch.Tensor, starts: Optional[torch.Tensor] = None, max_new: Optional[int] = None,
+             stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+        """(path, kept, following): from each item's first row on, the rows whose token is what was chosen behind their parent: their numbers
+        within the item, then -1 [rows]; how many [n]; the token chosen behind the last [n]."""
+        pp, rows = self._ints(parents, "parents", None, stream), parents.shape[0]
+        n, _, tp, max_new = self._items(None, starts, rows if starts is None else None, max_new, stream)
+        kp, cp = self._ints(tokens, "tokens", rows, stream), self._ints(chosen, "chosen", rows, stream)
+        path, kept, following = self._new(parents, (rows,), stream), self._new(parents, (n,), stream), self._new(parents, (n,), stream)
+        _chk(self._lib.rtams_cache_walk(self._h, n, tp, rows, max_new, pp, kp, cp, path.data_ptr(), kept.data_ptr(), following.data_ptr(), self._stream(stream)),
+             "rtams_cache_walk")
+        return path, kept, following
+
+    def keep(self, path: torch.Tensor, kept: torch.Tensor, seqs: Optional[torch.Tensor] = None, starts: Optional[torch.Tensor] = None, max_new: Optional[int] = None,
+             stream=None) -> None:
+        """Of each item's rows the first kept[i] that its path names, in ascending order, move to the front in all layers; its sequence ends behind them."""
+        pp, rows = self._ints(path, "path", None, stream), path.shape[0]
+        n, sp, tp, max_new = self._items(seqs, starts, rows if seqs is None and starts is None else None, max_new, stream)
+        _chk(self._lib.rtams_cache_keep(self._h, n, sp, tp, rows, max_new, pp, self._ints(kept, "kept", n, stream), self._stream(stream)), "rtams_cache_keep")
 
     # ---- pages
     def fork(self, src: torch.Tensor, dst: torch.Tensor, copy: bool = False, stream=None) -> None:

@@ -124,6 +124,12 @@ struct CacheQuery {
   float *lse;
 };
 
+struct CacheSight {  // what rows see besides the last positions of a window and, of each other, the ones before
+  int32_t sinks;         // with a window: the first so many positions
+  int32_t words;         // of a row of tree
+  const uint32_t *tree;  // bit i of row j's words: it sees row i of its item; NULL: the rows up to itself
+};
+
 void launch_cache_extend(const CacheDev &d, const CacheRows &r, bool copies, hipStream_t s);  // copies: pages may be shared
 void launch_cache_fork(const CacheDev &d, int32_t n, const int32_t *src, const int32_t *dst, bool copy, hipStream_t s);
 void launch_cache_trim(const CacheDev &d, int32_t n, const int32_t *seqs, const int32_t *lengths, hipStream_t s);
@@ -131,8 +137,15 @@ void launch_cache_compact(const CacheDev &d, hipStream_t s);
 void launch_cache_write(const CacheDev &d, const CacheRows &r, int layer, const void *k, const void *v, int64_t row_stride,
                         int64_t head_stride, bool half_type, bool vec, hipStream_t s);
 void launch_cache_read(const CacheDev &d, const CacheRows &r, int layer, void *k, void *v, int type, hipStream_t s);
-void launch_cache_attend(const CacheDev &d, const CacheQuery &q, hipStream_t s);
-void launch_cache_prompt(const CacheDev &d, const CacheQuery &q, hipStream_t s);  // (many rows; launch_cache_attend chooses)
+void launch_cache_attend(const CacheDev &d, const CacheQuery &q, const CacheSight *sight, hipStream_t s);  // (sight: NULL where it says nothing)
+void launch_cache_prompt(const CacheDev &d, const CacheQuery &q, const CacheSight *sight, hipStream_t s);  // (many rows; launch_cache_attend chooses)
+void launch_cache_tree(const CacheDev &d, const CacheRows &r, const int32_t *parents, uint32_t *tree, int words, int32_t *positions, hipStream_t s);
+void launch_cache_walk(const CacheDev &d, const CacheRows &r, const int32_t *parents, const int32_t *tokens, const int32_t *chosen, int32_t *path, int32_t *kept,
+                       int32_t *next, hipStream_t s);
+void launch_cache_keep(const CacheDev &d, const CacheRows &r, const int32_t *path, const int32_t *kept, hipStream_t s);
+void launch_cache_keep_plan(const CacheDev &d, const CacheRows &r, const int32_t *path, const int32_t *kept, hipStream_t s);  // checks, and d.items
+void launch_cache_keep_cut(const CacheDev &d, int32_t n, hipStream_t s);                                                     // lengths, and pages given up
+hipError_t allow_large_lds_cache_tree();
 hipError_t allow_large_lds_cache_attend();
 hipError_t allow_large_lds_cache_prompt();
 size_t cache_prompt_part_rows();

@@ -129,6 +129,16 @@ int check_rows(const rtams_cache *c, int32_t layer, int64_t n, const int32_t *d_
   return RTAMS_OK;
 }
 
+constexpr int32_t kMostTree = 1024;  // rows of a tree
+
+int check_tree(const int32_t *d_starts, int64_t rows, int32_t max_new, int32_t words) {
+  const int64_t most = d_starts ? (max_new < rows ? (int64_t)max_new : rows) : 1;
+  if (most > kMostTree) return fail(RTAMS_EINVAL, "a tree has at most %d rows, got %lld", kMostTree, (long long)most);
+  if (words >= 0 && (words < (most + 31) / 32 || words > kMostTree / 32))
+    return fail(RTAMS_EINVAL, "tree_words must hold a bit for each of an item's %lld rows, and be at most %d, got %d", (long long)most, kMostTree / 32, words);
+  return RTAMS_OK;
+}
+
 CacheRows items_of(int64_t n, const int32_t *d_seqs, const int32_t *d_starts, int64_t rows, int32_t max_new) {
   CacheRows r{};
   r.n = (int32_t)n;
@@ -210,7 +220,7 @@ int rtams_cache_create(const rtams_cache_config *cfg, rtams_cache **out) {
   q += up(cache_part_ml_floats(cfg->head_dim) * 4, kAlign);
   d.part = reinterpret_cast<float *>(q);
   auto bail = [&](int code) { rtams_cache_destroy(c); return code; };
-  if (allow_large_lds_cache_attend() != hipSuccess || allow_large_lds_cache_prompt() != hipSuccess) return bail(fail(RTAMS_EHIP, "hipFuncSetAttribute failed"));
+  if (allow_large_lds_cache_attend() != hipSuccess || allow_large_lds_cache_prompt() != hipSuccess || allow_large_lds_cache_tree() != hipSuccess) return bail(fail(RTAMS_EHIP, "hipFuncSetAttribute failed"));
   void *hm = nullptr, *dm = nullptr;
   if (hipHostMalloc(&hm, sizeof(CacheMirror), hipHostMallocMapped) != hipSuccess) return bail(fail(RTAMS_EHIP, "hipHostMalloc failed"));
   c->mirror = static_cast<CacheMirror *>(hm);
@@ -298,6 +308,11 @@ int rtams_cache_read(rtams_cache *c, int32_t layer, int64_t n, const int32_t *d_
 
 int rtams_cache_attend(rtams_cache *c, const rtams_cache_query *q, int64_t n, const int32_t *d_seqs, const int32_t *d_starts, int64_t rows,
                        void *hip_stream) {
+  return rtams_cache_attend_sight(c, q, nullptr, n, d_seqs, d_starts, rows, hip_stream);
+}
+
+int rtams_cache_attend_sight(rtams_cache *c, const rtams_cache_query *q, const rtams_cache_sight *sight, int64_t n, const int32_t *d_seqs,
+                             const int32_t *d_starts, int64_t rows, void *hip_stream) {
   int rc = check_items(c, n, d_seqs);
   if (rc) return rc;
   if (!q) return fail(RTAMS_EINVAL, "query is NULL");
@@ -307,6 +322,12 @@ int rtams_cache_attend(rtams_cache *c, const rtams_cache_query *q, int64_t n, co
   if (q->type != RTAMS_TYPE_BF16 && q->type != RTAMS_TYPE_F16) return fail(RTAMS_EINVAL, "queries are bfloat16 or halves, got type %d", q->type);
   if (q->window < 0 || (q->window > 0 && !q->causal)) return fail(RTAMS_EINVAL, "window %d: not negative, and causal only", q->window);
   if (!std::isfinite(q->scale)) return fail(RTAMS_EINVAL, "scale must be finite");
+  if (sight && (sight->sinks < 0 || (sight->sinks > 0 && q->window == 0))) return fail(RTAMS_EINVAL, "sinks %d: not negative, and with a window only", sight->sinks);
+  if (sight && sight->d_tree) {
+    if (!q->causal) return fail(RTAMS_EINVAL, "a tree's rows see what lies before them: causal only");
+    if ((rc = check_tree(d_starts, rows, q->max_new, sight->tree_words))) return rc;
+    if ((uintptr_t)sight->d_tree % 4) return fail(RTAMS_EINVAL, "the tree's words are not aligned to their type");
+  }
   if (n == 0 || rows == 0) return RTAMS_OK;
   if (!q->d_q || !q->d_out) return fail(RTAMS_EINVAL, "queries or output are NULL");
   if (((uintptr_t)q->d_q | (uintptr_t)q->d_out) % 2 || (uintptr_t)q->d_lse % 4) return fail(RTAMS_EINVAL, "queries, output or logarithms are not aligned to their type");
@@ -339,8 +360,62 @@ int rtams_cache_attend(rtams_cache *c, const rtams_cache_query *q, int64_t n, co
   k.out_head = q->out_head_stride;
   k.lse = q->d_lse;
   k.vec = ((uintptr_t)q->d_q | (uintptr_t)q->d_out) % 16 == 0 && (k.q_row | k.q_head | k.out_row | k.out_head) % 8 == 0;
-  launch_cache_attend(c->dev, k, s);
+  if (sight && (sight->sinks || sight->d_tree)) {
+    const int most_tokens = c->cfg.max_pages * c->cfg.page_tokens;
+    const CacheSight g{sight->sinks < most_tokens ? sight->sinks : most_tokens, sight->tree_words, sight->d_tree};
+    launch_cache_attend(c->dev, k, &g, s);
+  } else {
+    launch_cache_attend(c->dev, k, nullptr, s);
+  }
   return launched("attend");
+}
+
+int rtams_cache_tree(rtams_cache *c, int64_t n, const int32_t *d_seqs, const int32_t *d_starts, int64_t rows, int32_t max_new, const int32_t *d_parents,
+                     uint32_t *d_tree, int32_t tree_words, int32_t *d_positions, void *hip_stream) {
+  int rc = check_items(c, n, d_seqs);
+  if (!rc) rc = check_rows(c, 0, n, d_starts, rows, max_new);
+  if (!rc && tree_words < 0) rc = fail(RTAMS_EINVAL, "tree_words must not be negative, got %d", tree_words);
+  if (!rc) rc = check_tree(d_starts, rows, max_new, tree_words);
+  if (rc || n == 0 || rows == 0) return rc;
+  if (!d_parents || !d_tree) return fail(RTAMS_EINVAL, "parents or tree are NULL");
+  if (((uintptr_t)d_parents | (uintptr_t)d_tree | (uintptr_t)d_positions) % 4) return fail(RTAMS_EINVAL, "parents, tree or positions are not aligned to their type");
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  std::lock_guard<std::mutex> g(c->mutex);
+  if ((rc = cache_enter(c, s))) return rc;
+  launch_cache_tree(c->dev, items_of(n, d_seqs, d_starts, rows, max_new), d_parents, d_tree, tree_words, d_positions, s);
+  return launched("tree");
+}
+
+int rtams_cache_walk(rtams_cache *c, int64_t n, const int32_t *d_starts, int64_t rows, int32_t max_new, const int32_t *d_parents, const int32_t *d_tokens,
+                     const int32_t *d_chosen, int32_t *d_path, int32_t *d_kept, int32_t *d_next, void *hip_stream) {
+  int rc = check_items(c, n, nullptr);
+  if (!rc) rc = check_rows(c, 0, n, d_starts, rows, max_new);
+  if (!rc) rc = check_tree(d_starts, rows, max_new, -1);
+  if (rc || n == 0) return rc;
+  if (!d_kept || !d_next) return fail(RTAMS_EINVAL, "kept or next are NULL");
+  if (rows > 0 && (!d_parents || !d_tokens || !d_chosen || !d_path)) return fail(RTAMS_EINVAL, "parents, tokens, choices or path are NULL");
+  if (((uintptr_t)d_parents | (uintptr_t)d_tokens | (uintptr_t)d_chosen | (uintptr_t)d_path | (uintptr_t)d_kept | (uintptr_t)d_next) % 4)
+    return fail(RTAMS_EINVAL, "an array is not aligned to its type");
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  std::lock_guard<std::mutex> g(c->mutex);
+  if ((rc = cache_enter(c, s))) return rc;
+  launch_cache_walk(c->dev, items_of(n, nullptr, d_starts, rows, max_new), d_parents, d_tokens, d_chosen, d_path, d_kept, d_next, s);
+  return launched("walk");
+}
+
+int rtams_cache_keep(rtams_cache *c, int64_t n, const int32_t *d_seqs, const int32_t *d_starts, int64_t rows, int32_t max_new, const int32_t *d_path,
+                     const int32_t *d_kept, void *hip_stream) {
+  int rc = check_items(c, n, d_seqs);
+  if (!rc) rc = check_rows(c, 0, n, d_starts, rows, max_new);
+  if (!rc) rc = check_tree(d_starts, rows, max_new, -1);
+  if (rc || n == 0 || rows == 0) return rc;
+  if (!d_path || !d_kept) return fail(RTAMS_EINVAL, "path or kept are NULL");
+  if (((uintptr_t)d_path | (uintptr_t)d_kept) % 4) return fail(RTAMS_EINVAL, "path or kept are not aligned to their type");
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  std::lock_guard<std::mutex> g(c->mutex);
+  if ((rc = cache_enter(c, s))) return rc;
+  launch_cache_keep(c->dev, items_of(n, d_seqs, d_starts, rows, max_new), d_path, d_kept, s);
+  return launched("keep");
 }
 
 int rtams_cache_fork(rtams_cache *c, int64_t n, const int32_t *d_src, const int32_t *d_dst, int32_t copy, void *hip_stream) {

@@ -30,7 +30,7 @@ constexpr int at_once(int head_dim, int tiles) {
 }
 
 struct Span {  // what an item asks for
-  int seq, count, length, low;  // low: first position that a row of it sees, rounded down to a block
+  int seq, count, length, low;  // low: first position that a row of it sees, rounded down to a block (with sinks: behind them, less what they take)
   int steps;
   int tiles;  // of its rows
   int64_t row0;
@@ -38,8 +38,8 @@ struct Span {  // what an item asks for
 
 // Items i + 64 k of the launch, for k of 0 .. N - 1; steps 0 behind the last one.  Loads are asked for together, whatever they find: each is
 // a trip to memory, at the beginning of a launch.
-template <int N, int ROWS>
-__device__ inline void find_spans(const CacheDev &d, const CacheQuery &q, int i, bool tell, Span (&s)[N]) {
+template <int N, int ROWS, bool SIGHT>
+__device__ inline void find_spans(const CacheDev &d, const CacheQuery &q, const CacheSight &g, int i, bool tell, Span (&s)[N]) {
   const int n = q.r.n;
   int first[N], past[N], seq[N], length[N];
 #pragma unroll
@@ -65,8 +65,9 @@ __device__ inline void find_spans(const CacheDev &d, const CacheQuery &q, int i,
     s[k].count = there && ok ? past[k] - first[k] : 0;
     s[k].length = length[k];
     if (tell && there && !ok) cache_raise(d, RTAMS_EINVAL);
-    const int low = length[k] - s[k].count - q.window + 1;
+    const int low = length[k] - s[k].count - q.window + (SIGHT && g.tree ? 0 : 1);
     s[k].low = q.window && low > 0 ? low & ~(kBlockTokens - 1) : 0;
+    if (SIGHT) s[k].low = max(0, s[k].low - sink_blocks(g));
     s[k].steps = s[k].count <= 0 ? 0 : length[k] > s[k].low ? (length[k] - s[k].low + kStep - 1) / kStep : 1;
     s[k].tiles = (q.share * s[k].count + ROWS - 1) / ROWS;
   }
@@ -97,14 +98,14 @@ struct alignas(16) Shared {
 
 // Which piece is workgroup blockIdx.x's: the items' steps, the size of a piece, and the pieces of the items in front.  One wavefront's work, EACH
 // items to a lane (lane, lane + 64, ...); false where there is none left.
-template <int EACH, int ROWS, class S>
-__device__ bool find_piece(const CacheDev &d, const CacheQuery &q, int tiles, uint32_t workers, S &sh) {
+template <int EACH, int ROWS, bool SIGHT, class S>
+__device__ bool find_piece(const CacheDev &d, const CacheQuery &q, const CacheSight &g, int tiles, uint32_t workers, S &sh) {
   constexpr int kItems = 64 * EACH;
   const int lane = threadIdx.x & 63, n = q.r.n;
   Span sp[EACH];
   uint32_t all = 0;
   for (int base = 0; base < n; base += kItems) {
-    find_spans<EACH, ROWS>(d, q, base + lane, blockIdx.x == 0, sp);
+    find_spans<EACH, ROWS, SIGHT>(d, q, g, base + lane, blockIdx.x == 0, sp);
     uint32_t sum = 0;
 #pragma unroll
     for (int k = 0; k < EACH; ++k) sum += (uint32_t)(sp[k].steps * sp[k].tiles);
@@ -125,7 +126,7 @@ __device__ bool find_piece(const CacheDev &d, const CacheQuery &q, int tiles, ui
   const float one_over = 1.0f / (float)size;
   uint32_t before = 0, parts_before = 0;
   for (int base = 0; base < n; base += kItems) {
-    if (n > kItems) find_spans<EACH, ROWS>(d, q, base + lane, false, sp);
+    if (n > kItems) find_spans<EACH, ROWS, SIGHT>(d, q, g, base + lane, false, sp);
 #pragma unroll
     for (int k = 0; k < EACH; ++k) {
       const uint32_t parts = div_up((uint32_t)sp[k].steps, size, one_over), pieces = parts * (uint32_t)(d.kv_heads * sp[k].tiles), shared = parts > 1 ? pieces : 0;
@@ -146,16 +147,18 @@ __device__ bool find_piece(const CacheDev &d, const CacheQuery &q, int tiles, ui
 typedef const __attribute__((address_space(4))) int32_t *ScalarInts;
 
 // The copies of a wavefront's blocks into its ring: its n-th block goes to slot n % kAhead.
-template <int D>
+template <int D, bool SIGHT>
 struct Copies {
   static constexpr int kCopies = (40 * D + 1023) / 1024;  // loads of a block
   ScalarInts table;
   int head, tok, to;   // next block's first token; end of the piece's tokens
   uint32_t ring, slot;
   uint32_t page, page2;  // of the next block and the one after
+  int sinks, gap;        // tokens are counted without the `gap` positions behind the first `sinks`
 
   // (pages are looked up by scalar loads, two blocks ahead: a vector load would wait for all copies under way)
-  __device__ __forceinline__ uint32_t look(const CacheDev &d, int at) { return (uint32_t)table[cache_page_of(d, (uint32_t)min(at, to - 1) / kBlockTokens)]; }
+  __device__ __forceinline__ int place(int at) const { return SIGHT && at >= sinks ? at + gap : at; }
+  __device__ __forceinline__ uint32_t look(const CacheDev &d, int at) { return (uint32_t)table[cache_page_of(d, (uint32_t)place(min(at, to - 1)) / kBlockTokens)]; }
   __device__ __forceinline__ void begin(const CacheDev &d) {
     if (tok >= to) return;
     page = look(d, tok);
@@ -163,7 +166,7 @@ struct Copies {
   }
   __device__ __forceinline__ void one(const CacheDev &d, int layer, int lane) {
     if (tok >= to) return;
-    const uint32_t block = (uint32_t)tok / kBlockTokens;
+    const uint32_t block = (uint32_t)place(tok) / kBlockTokens;
     const unsigned char *blk = cache_block(d, layer, (int)page, head, block - cache_page_of(d, block) * d.page_blocks);
 #pragma unroll
     for (int i = 0; i < kCopies; ++i)
@@ -175,15 +178,15 @@ struct Copies {
   }
 };
 
-template <int D, int NR>
-__global__ __launch_bounds__(kLanes, at_once(D, NR)) void k_cache_attend(CacheDev d, CacheQuery q, int tiles) {
+template <int D, int NR, bool SIGHT>
+__device__ __forceinline__ void attend(const CacheDev &d, const CacheQuery &q, const CacheSight &g, int tiles) {
   constexpr int NJ = D / 32, NT = D / 16;
   extern __shared__ uint4 lds[];
   Shared<D, NR> &sh = *reinterpret_cast<Shared<D, NR> *>(lds);
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 15, b = lane >> 4;
 
   if (wave == 0) {
-    const bool found = q.r.n <= 64 ? find_piece<1, 16 * NR>(d, q, tiles, kUnits * at_once(D, NR), sh) : find_piece<kRound / 64, 16 * NR>(d, q, tiles, kUnits * at_once(D, NR), sh);
+    const bool found = q.r.n <= 64 ? find_piece<1, 16 * NR, SIGHT>(d, q, g, tiles, kUnits * at_once(D, NR), sh) : find_piece<kRound / 64, 16 * NR, SIGHT>(d, q, g, tiles, kUnits * at_once(D, NR), sh);
     if (lane == 0) sh.last = found;
   }
   __syncthreads();
@@ -197,12 +200,16 @@ __global__ __launch_bounds__(kLanes, at_once(D, NR)) void k_cache_attend(CacheDe
     pc.sa = each * pc.nth + min(pc.nth, longer);
     pc.sb = pc.sa + each + (pc.nth < longer);
   }
-  const int row_first = pc.tile * 16 * NR, rows = min(16 * NR, q.share * sp.count - row_first), head = pc.head, first_tok = sp.low + pc.sa * kStep + wave * kBlockTokens;
-  Copies<D> cp;
+  const int row_first = pc.tile * 16 * NR, rows = min(16 * NR, q.share * sp.count - row_first), head = pc.head;
+  // (with a sight tokens are counted from the first one on, without those between the sinks and the window)
+  const int from = SIGHT ? 0 : sp.low, first_tok = from + pc.sa * kStep + wave * kBlockTokens;
+  Copies<D, SIGHT> cp;
   cp.table = (ScalarInts)(uintptr_t)(d.table + (int64_t)sp.seq * d.max_pages);
   cp.head = head;
   cp.tok = first_tok;
-  cp.to = min(sp.low + pc.sb * kStep, sp.length);
+  cp.to = min(from + pc.sb * kStep, SIGHT ? sp.length - sp.low : sp.length);
+  cp.sinks = SIGHT ? sink_blocks(g) : 0;
+  cp.gap = sp.low;
   cp.ring = (uint32_t)uniform((int)lds_address(sh.ring[wave][0]));
   cp.slot = 0;
   cp.begin(d);
@@ -211,19 +218,28 @@ __global__ __launch_bounds__(kLanes, at_once(D, NR)) void k_cache_attend(CacheDe
 
   half8 qf[NR][NJ];
   int see_to[NR], see_from[NR];
+  uint64_t kin[NR] = {};  // tree: of the item's rows, those that this row sees
+  const int base_pos = sp.length - sp.count;
 #pragma unroll
   for (int t = 0; t < NR; ++t) {
     const int row = t * 16 + col;
     const bool real = row < rows;
     const int j = real ? (row_first + row) / q.share : 0, h = real ? (row_first + row) % q.share : 0;
-    const int pos = sp.length - sp.count + j;
-    see_to[t] = q.causal ? pos + 1 : sp.length;
+    int pos = sp.length - sp.count + j;
+    if (SIGHT && g.tree) {  // (at most 64 rows)
+      const uint32_t *w = g.tree + (sp.row0 + j) * g.words;
+      kin[t] = w[0];
+      if (g.words > 1) kin[t] |= (uint64_t)w[1] << 32;
+      if (sp.count < 64) kin[t] &= ((uint64_t)1 << sp.count) - 1;
+      pos = base_pos + __popcll(kin[t]) - 1;
+    }
+    see_to[t] = SIGHT && g.tree ? base_pos : q.causal ? pos + 1 : sp.length;
     see_from[t] = q.window ? pos - q.window + 1 : 0;
     const uint16_t *p = q.q + (sp.row0 + j) * q.q_row + (int64_t)(head * q.share + h) * q.q_head + b * (D / 4);
 #pragma unroll
     for (int x = 0; x < NJ; ++x) qf[t][x] = real ? load_query(p + 8 * x, q.half_type, q.vec, q.scale_two) : half8{};
   }
-  const int all_to = q.causal ? sp.length - sp.count + 1 : sp.length;     // every row sees [all_from, all_to)
+  const int all_to = SIGHT && g.tree ? base_pos : q.causal ? sp.length - sp.count + 1 : sp.length;  // every row sees [all_from, all_to)
   const int all_from = q.window ? sp.length - q.window : 0;
 
   f32x4 o[NR][NT];
@@ -237,9 +253,9 @@ __global__ __launch_bounds__(kLanes, at_once(D, NR)) void k_cache_attend(CacheDe
   }
   const int to = cp.to;
   uint32_t slot = 0;
-  for (int tok0 = first_tok; tok0 < to; tok0 += kStep) {
+  for (int tok = first_tok; tok < to; tok += kStep) {
     static_assert(kAhead == 2, "one block behind this one");
-    if (tok0 + kStep < to) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Copies<D>::kCopies) : "memory");
+    if (tok + kStep < to) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Copies<D, SIGHT>::kCopies) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     const unsigned char *blk = sh.ring[wave][slot];
     KeyTile<D> kt[2];
@@ -262,7 +278,22 @@ __global__ __launch_bounds__(kLanes, at_once(D, NR)) void k_cache_attend(CacheDe
         for (int t = 0; t < NR; ++t) sc[t][x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, qf[t][j], sc[t][x], 0, 0, 0);
       }
     }
-    if (tok0 + kBlockTokens > all_to || tok0 < all_from) {
+    const int tok0 = cp.place(tok);
+    if constexpr (SIGHT) {
+      if (tok0 + kBlockTokens > all_to || (tok0 < all_from && tok0 + kBlockTokens > g.sinks)) {
+#pragma unroll
+        for (int t = 0; t < NR; ++t) {
+          uint32_t sees = low_bits(see_to[t] - tok0) & (~low_bits(see_from[t] - tok0) | low_bits(g.sinks - tok0));
+          if (g.tree && tok0 + kBlockTokens > base_pos) sees |= bits_at(kin[t], tok0 - base_pos);
+          sees >>= 16 * (b >> 1) + 4 * (b & 1);
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (!(sees >> (8 * x + r) & 1)) sc[t][x][r] = -INFINITY;
+        }
+      }
+    } else if (tok0 + kBlockTokens > all_to || tok0 < all_from) {
       const int first = tok0 + 16 * (b >> 1) + 4 * (b & 1);
 #pragma unroll
       for (int t = 0; t < NR; ++t)
@@ -363,10 +394,22 @@ __global__ __launch_bounds__(kLanes, at_once(D, NR)) void k_cache_attend(CacheDe
   }
 }
 
+template <int D, int NR>
+__global__ __launch_bounds__(kLanes, at_once(D, NR)) void k_cache_attend(CacheDev d, CacheQuery q, int tiles) {
+  attend<D, NR, false>(d, q, CacheSight{}, tiles);
+}
+
+template <int D, int NR>
+__global__ __launch_bounds__(kLanes, at_once(D, NR)) void k_cache_sight(CacheDev d, CacheQuery q, CacheSight g, int tiles) {
+  attend<D, NR, true>(d, q, g, tiles);
+}
+
 // (an even share makes no more pieces than run at once, and one more for each row tile of a head)
 template <int D, int NR>
-void launch(const CacheDev &d, const CacheQuery &q, int tiles, hipStream_t s) {
-  k_cache_attend<D, NR><<<(uint32_t)(kUnits * at_once(D, NR) + q.r.n * d.kv_heads * tiles), kLanes, sizeof(Shared<D, NR>), s>>>(d, q, tiles);
+void launch(const CacheDev &d, const CacheQuery &q, const CacheSight *g, int tiles, hipStream_t s) {
+  const uint32_t grid = (uint32_t)(kUnits * at_once(D, NR) + q.r.n * d.kv_heads * tiles);
+  if (g) k_cache_sight<D, NR><<<grid, kLanes, sizeof(Shared<D, NR>), s>>>(d, q, *g, tiles);
+  else k_cache_attend<D, NR><<<grid, kLanes, sizeof(Shared<D, NR>), s>>>(d, q, tiles);
 }
 
 // Up to 64 rows; a head's row tiles read its cache one beside the other, and the second finds it in the last-level cache.
@@ -387,7 +430,7 @@ size_t cache_arrived_words(int max_seqs, int kv_heads) {
   return few > many ? few : many;
 }
 
-void launch_cache_attend(const CacheDev &d, const CacheQuery &q, hipStream_t s) {
+void launch_cache_attend(const CacheDev &d, const CacheQuery &q, const CacheSight *g, hipStream_t s) {
   // Against the kernel for many rows, 8 sequences of up to 32,000 tokens and 8 heads: of 128 channels 32, 40, 64, 96, 128 rows take 69, 111, 108, 159,
   // 186 us here and 144 to 152 there; of 256 channels 24, 32, 40, 48, 64 rows 200, 201, 368, 369, 421 us and 420 to 433.  64 rows of 64, 96, 256 channels:
   // one sequence of 32,000 34, 42, 71 us and 66, 86, 160; 8 of up to 8,000 28, 36, 122 and 41, 49, 129; 32 of up to 2,000 29, 34, 105 and 44, 51, 153,
@@ -397,17 +440,19 @@ void launch_cache_attend(const CacheDev &d, const CacheQuery &q, hipStream_t s) 
   const int64_t tiles = (rows + each - 1) / each;
   // (steps of all row tiles are counted in 32 bits, and they are one launch)
   const int64_t heads = q.r.n * (int64_t)d.kv_heads * tiles;
-  if (rows > 64 || (tiles > 1 && (heads >= 1 << 22 || heads * ((int64_t)d.max_pages * d.page_blocks / kWaves + 1) >= (int64_t)1 << 32))) return launch_cache_prompt(d, q, s);
+  if (rows > 64 || (tiles > 1 && (heads >= 1 << 22 || heads * ((int64_t)d.max_pages * d.page_blocks / kWaves + 1) >= (int64_t)1 << 32))) return launch_cache_prompt(d, q, g, s);
   switch (d.head_dim) {
-    case 64: return each == 16 ? launch<64, 1>(d, q, 1, s) : launch<64, 2>(d, q, (int)tiles, s);
-    case 96: return each == 16 ? launch<96, 1>(d, q, 1, s) : launch<96, 2>(d, q, (int)tiles, s);
-    case 128: return each == 16 ? launch<128, 1>(d, q, 1, s) : launch<128, 2>(d, q, (int)tiles, s);
-    default: return launch<256, 1>(d, q, (int)tiles, s);
+    case 64: return each == 16 ? launch<64, 1>(d, q, g, 1, s) : launch<64, 2>(d, q, g, (int)tiles, s);
+    case 96: return each == 16 ? launch<96, 1>(d, q, g, 1, s) : launch<96, 2>(d, q, g, (int)tiles, s);
+    case 128: return each == 16 ? launch<128, 1>(d, q, g, 1, s) : launch<128, 2>(d, q, g, (int)tiles, s);
+    default: return launch<256, 1>(d, q, g, (int)tiles, s);
   }
 }
 
 hipError_t allow_large_lds_cache_attend() {
-  return hipFuncSetAttribute(reinterpret_cast<const void *>(k_cache_attend<256, 1>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Shared<256, 1>));
+  const auto allow = [](const void *f, size_t bytes) { return hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes); };
+  if (const hipError_t e = allow(reinterpret_cast<const void *>(k_cache_attend<256, 1>), sizeof(Shared<256, 1>))) return e;
+  return allow(reinterpret_cast<const void *>(k_cache_sight<256, 1>), sizeof(Shared<256, 1>));
 }
 
 }  // namespace rtams

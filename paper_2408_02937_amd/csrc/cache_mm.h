@@ -218,6 +218,13 @@ __device__ inline uint32_t div_up(uint32_t a, uint32_t b, float one_over_b) {
   return q + (r > 0);
 }
 
+// What rows see (CacheSight), 32 tokens at a time as the bits of a word.
+__device__ inline uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
+// Bits from number `at` on, -31 or more; those that are not there are 0.
+__device__ inline uint32_t bits_at(uint64_t x, int at) { return at >= 64 ? 0u : at >= 0 ? (uint32_t)(x >> at) : (uint32_t)x << -at; }
+// Positions that the sinks take, in whole blocks.
+__device__ inline int sink_blocks(const CacheSight &g) { return (g.sinks + kBlockTokens - 1) & ~(kBlockTokens - 1); }
+
 constexpr int kUnits = 256;  // compute units
 
 // Steps of a piece, of n items' steps.  Pieces are to run all at once, `workers` of them, and to leave the compute units alike much to do:

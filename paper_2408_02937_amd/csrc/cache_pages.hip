@@ -286,6 +286,50 @@ __global__ __launch_bounds__(256) void k_cache_trim_entries(CacheDev d, int32_t 
   });
 }
 
+// Of rows that are kept: the items, and whether the call holds.  src: position of the first row, off: rows kept, copy: rows.
+__global__ __launch_bounds__(kPlanLanes) void k_cache_keep_plan(CacheDev d, CacheRows r, const int32_t *path, const int32_t *kept) {
+  __shared__ Plan sh;
+  clear_seen(d, sh);
+  int bad = 0;
+  for (int i = threadIdx.x; i < r.n; i += kPlanLanes) {
+    int64_t first;
+    int count;
+    const int s = cache_item_seq(r, i), k = kept[i];
+    const bool rows = cache_item_rows(r, i, &first, &count);
+    if (!rows || (uint32_t)s >= (uint32_t)d.max_seqs || named_before(sh.seen, s)) {
+      bad = 1;
+      continue;
+    }
+    const int length = d.lengths[s], base = length - count;
+    if (count > length || k < 0 || k > count) {
+      bad = 1;
+      continue;
+    }
+    for (int j = 0, before = -1, looked = -1; j < k; ++j) {
+      const int p = path[first + j], page = (base + j) / d.page_tokens;
+      bad |= p <= before || p >= count;
+      before = p;
+      if (p != j && page != looked) {  // (another sequence's rows are not written over)
+        bad |= d.refs[d.table[(int64_t)s * d.max_pages + page]] != 1;
+        looked = page;
+      }
+    }
+    d.items[i] = CacheItem{s, base, pages_for(d, length), pages_for(d, (int64_t)base + k), (uint32_t)k, count, {}};
+  }
+  if (__syncthreads_or(bad)) return drop(d, RTAMS_EINVAL);
+  if (threadIdx.x == 0) d.ctrl->ok = d.ctrl->stopped == 0;
+}
+
+__global__ __launch_bounds__(256) void k_cache_keep_cut(CacheDev d, int32_t n) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (!d.ctrl->ok || i >= n) return;
+  const CacheItem it = d.items[i];
+  d.lengths[it.seq] = it.src + (int)it.off;
+  uint32_t gone = 0;
+  for (int p = it.want; p < it.have; ++p) gone += give_up(d, it.seq, p);
+  if (gone) atomicAdd(&d.ctrl->free, gone);
+}
+
 // Entry p of a fork's destination; copy: a page of its own, pair `pair` of the call.
 __device__ inline void take_over(const CacheDev &d, int32_t src, int32_t dst, int p, bool copy, uint32_t pair, int32_t own) {
   const int32_t page = d.table[(int64_t)src * d.max_pages + p];
@@ -465,6 +509,12 @@ void launch_cache_trim(const CacheDev &d, int32_t n, const int32_t *seqs, const 
   k_cache_trim<<<1, kPlanLanes, 0, s>>>(d, n, seqs, lengths, few);
   if (!few) k_cache_trim_entries<<<entry_groups(d, n), 256, 0, s>>>(d, n);
 }
+
+void launch_cache_keep_plan(const CacheDev &d, const CacheRows &r, const int32_t *path, const int32_t *kept, hipStream_t s) {
+  k_cache_keep_plan<<<1, kPlanLanes, 0, s>>>(d, r, path, kept);
+}
+
+void launch_cache_keep_cut(const CacheDev &d, int32_t n, hipStream_t s) { k_cache_keep_cut<<<(n + 255) / 256, 256, 0, s>>>(d, n); }
 
 void launch_cache_fork(const CacheDev &d, int32_t n, const int32_t *src, const int32_t *dst, bool copy, hipStream_t s) {
   const bool few = few_entries(d, n);

@@ -104,11 +104,12 @@ typedef const __attribute__((address_space(4))) int32_t *ScalarInts;
 
 struct Span {  // what the rows of a tile of an item go over
   int64_t row0;
-  int seq, count, length, from, steps;  // from: first position, at a block's begin
+  int seq, count, length, from, steps;  // from: first position, at a block's begin (with sinks: behind them, less what they take)
 };
 
 // Row tile `tile` (of `rows` rows) of an item; count 0: none.
-__device__ inline Span find_span(const CacheDev &d, const CacheQuery &q, int item, int tile, int rows, int step_tokens, bool tell) {
+template <bool SIGHT>
+__device__ inline Span find_span(const CacheDev &d, const CacheQuery &q, const CacheSight &g, int item, int tile, int rows, int step_tokens, bool tell) {
   Span s{};
   s.seq = cache_item_seq(q.r, item);
   if (!cache_item_rows(q.r, item, &s.row0, &s.count) || (uint32_t)s.seq >= (uint32_t)d.max_seqs) {
@@ -127,8 +128,14 @@ __device__ inline Span find_span(const CacheDev &d, const CacheQuery &q, int ite
     return s;
   }
   const int last = min(tile * rows + rows - 1, q.share * s.count - 1) / q.share;
-  const int to = q.causal ? s.length - s.count + last + 1 : s.length;
-  s.from = q.causal && q.window ? max(0, s.length - s.count + tile * rows / q.share - q.window + 1) & ~(kBlockTokens - 1) : 0;
+  const bool tree = SIGHT && g.tree;
+  int to = q.causal && !tree ? s.length - s.count + last + 1 : s.length;
+  // (a tree's row may see no row of its item, itself included)
+  s.from = q.causal && q.window ? max(0, s.length - s.count + (tree ? -1 : tile * rows / q.share) - q.window + 1) & ~(kBlockTokens - 1) : 0;
+  if (SIGHT) {
+    s.from = max(0, s.from - sink_blocks(g));
+    to = max(to, s.from);  // (a first row's window may begin behind the last one's end)
+  }
   s.steps = to > s.from ? (to - s.from + step_tokens - 1) / step_tokens : 1;  // (one, also where the rows see nothing)
   return s;
 }
@@ -156,13 +163,14 @@ union Shared {
 };
 
 // Which piece is workgroup blockIdx.x's, where tokens are split (find_piece in cache_attend.hip has the same for few rows).  One wavefront's work.
-__device__ inline bool find_piece(const CacheDev &d, const CacheQuery &q, int tiles, int rows, int step_tokens, uint32_t workers, float *steps, Piece *piece) {
+template <bool SIGHT>
+__device__ inline bool find_piece(const CacheDev &d, const CacheQuery &q, const CacheSight &g, int tiles, int rows, int step_tokens, uint32_t workers, float *steps, Piece *piece) {
   const int lane = threadIdx.x & 63, n = q.r.n * tiles;
   uint32_t all = 0;
   float longest = 1.0f;
   for (int base = 0; base < (n + 255) / 256 * 256; base += 64) {
     const int e = base + lane;
-    const Span sp = e < n ? find_span(d, q, e % q.r.n, tiles - 1 - e / q.r.n, rows, step_tokens, blockIdx.x == 0) : Span{};
+    const Span sp = e < n ? find_span<SIGHT>(d, q, g, e % q.r.n, tiles - 1 - e / q.r.n, rows, step_tokens, blockIdx.x == 0) : Span{};
     const int mine = sp.count ? sp.steps : 0;
     steps[e] = (float)mine;
     longest = fmaxf(longest, (float)mine);
@@ -206,8 +214,8 @@ __device__ __forceinline__ void reads_ahead() {
   __builtin_amdgcn_sched_group_barrier(kMfma, kAhead, 0);
 }
 
-template <int D, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(CacheDev d, CacheQuery q, int tiles, int tile_rows, int split, uint32_t first) {
+template <int D, int WAVES, bool SIGHT>
+__device__ __forceinline__ void attend_many(const CacheDev &d, const CacheQuery &q, const CacheSight &g, int tiles, int tile_rows, int split, uint32_t first) {
   constexpr int kLanes = WAVES * 64, NS = D / 16, NC = D / 32, NP = (2 * kPairs<D> + kLanes - 1) / kLanes;
   constexpr int TB = tile_blocks(D), kTile = TB * kBlockTokens;
   extern __shared__ uint4 lds[];
@@ -218,7 +226,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(C
   Piece pc;
   if (split) {
     if (threadIdx.x < 64) {
-      const bool found = find_piece(d, q, tiles, tile_rows, kTile, kUnits * at_once(D, WAVES), shared.steps, &piece);
+      const bool found = find_piece<SIGHT>(d, q, g, tiles, tile_rows, kTile, kUnits * at_once(D, WAVES), shared.steps, &piece);
       if (threadIdx.x == 0) flag = found;
     }
     __syncthreads();
@@ -230,7 +238,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(C
     pc = Piece{(int)(x / d.kv_heads), (int)(x % d.kv_heads), 1, 0, 0};
   }
   const int item = pc.entry % q.r.n, tile = tiles - 1 - pc.entry / q.r.n, head = pc.head;
-  const Span sp = find_span(d, q, item, tile, tile_rows, kTile, !split && tile == 0 && head == 0 && threadIdx.x == 0);
+  const Span sp = find_span<SIGHT>(d, q, g, item, tile, tile_rows, kTile, !split && tile == 0 && head == 0 && threadIdx.x == 0);
   const int count = uniform(sp.count);
   if (!count) return;
   const int64_t row0 = sp.row0;
@@ -241,9 +249,28 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(C
   const int row = wave * 32 + col, mine = tile * tile_rows + row;
   const bool real = row < min(rows, tile_rows);
   const int j = real ? mine / q.share : 0, qh = head * q.share + (real ? mine % q.share : 0);
-  const int pos = length - count + j;
+  const bool tree = SIGHT && g.tree;
+  const int base_pos = length - count;
+  const uint32_t *const kin = tree ? g.tree + (row0 + j) * g.words : nullptr;
+  int pos = length - count + j;
+  if (tree && q.window) {
+    pos = base_pos - 1;
+    for (int w = 0; w * 32 < count; ++w) pos += __popc(kin[w] & low_bits(count - w * 32));
+  }
   const int see_from = q.causal && q.window ? pos - q.window + 1 : 0;
   const uint32_t sees = !real ? 0 : (uint32_t)max(0, (q.causal ? pos + 1 : length) - see_from);  // positions from see_from on
+  // with a sight: of the 32 positions from tok on, as bits
+  const auto sees_at = [&](int tok) {
+    if (!real) return 0u;
+    uint32_t x = low_bits((tree ? base_pos : q.causal ? pos + 1 : length) - tok) & (~low_bits(see_from - tok) | low_bits(g.sinks - tok));
+    const int at = tok - base_pos;
+    if (tree && at > -32 && at < count) {
+      const int w = at >> 5, by = at & 31;
+      const uint32_t lo = w >= 0 ? kin[w] : 0, hi = (w + 1) * 32 < count ? kin[w + 1] : 0;
+      x |= (uint32_t)(((uint64_t)hi << 32 | lo) >> by) & low_bits(count - at);
+    }
+    return x;
+  };
   half8 qf[NS];
   {
     const uint16_t *p = q.q + (row0 + j) * q.q_row + (int64_t)qh * q.q_head + h * 8;
@@ -254,8 +281,9 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(C
   const int w_first = tile * tile_rows + wave * 32, w_last = min(w_first + 31, q.share * count - 1);  // (tile_rows: whole wavefronts)
   const bool busy = wave * 32 < min(rows, tile_rows);
   const int j_first = w_first / q.share, j_last = w_last / q.share;
-  const int any_to = !busy ? INT_MIN : q.causal ? length - count + j_last + 1 : length, all_to = q.causal ? length - count + j_first + 1 : length;
-  const int any_from = q.causal && q.window ? length - count + j_first - q.window + 1 : 0, all_from = q.causal && q.window ? length - count + j_last - q.window + 1 : 0;
+  const int any_to = !busy ? INT_MIN : q.causal && !tree ? length - count + j_last + 1 : length, all_to = tree ? base_pos : q.causal ? length - count + j_first + 1 : length;
+  const int any_from = q.causal && q.window ? length - count + (tree ? -1 : j_first) - q.window + 1 : 0;
+  const int all_from = q.causal && q.window ? length - count + (tree ? count - 1 : j_last) - q.window + 1 : 0;
   const int each = steps / pc.parts, longer = steps - each * pc.parts;  // steps in equal pieces, the first ones one longer
   const int t0 = each * pc.nth + min(pc.nth, longer), t1 = t0 + each + (pc.nth < longer);
 
@@ -276,10 +304,13 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(C
     const uint32_t b = (uint32_t)min(block, last_block), pg = cache_page_of(d, b);
     return cache_block(d, q.layer, table[pg], head, b - pg * d.page_blocks);
   };
+  // (with a sight a tile's tokens are counted from the first one on, without those between the sinks and the window)
+  const int sinks = SIGHT ? sink_blocks(g) : 0;
+  const auto place = [&](int at) { return at >= sinks ? at + from : at; };
   Words<D> next[NP];
   const auto load_tile = [&](Words<D> (&to)[NP], int t) {
-    const int block = (from + t * kTile) / kBlockTokens;
-    const unsigned char *b0 = block_at(block), *b1 = TB == 2 ? block_at(block + 1) : b0;
+    const int block = (SIGHT ? place(t * kTile) : from + t * kTile) / kBlockTokens;
+    const unsigned char *b0 = block_at(block), *b1 = TB == 2 ? block_at(SIGHT ? place(t * kTile + kBlockTokens) / kBlockTokens : block + 1) : b0;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       const int u = i * kLanes + threadIdx.x;
@@ -328,8 +359,18 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(C
     constexpr _Float16 kMost = (_Float16)(1 << (int)(kTop + kLag));
     return most[0] > kMost || most[1] > kMost;
   };
-  const auto probabilities = [&](int tok0) {
-    if (tok0 + kTile > all_to || tok0 < all_from) {
+  const auto probabilities = [&](int tok0, int tok1) {
+    if constexpr (SIGHT) {
+#pragma unroll
+      for (int x = 0; x < TB; ++x) {
+        const int tok = x ? tok1 : tok0;
+        if (tok + kBlockTokens <= all_to && (tok >= all_from || tok + kBlockTokens <= g.sinks)) continue;
+        const uint32_t mine = sees_at(tok) >> (4 * h);
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (!(mine >> (8 * (e >> 2) + (e & 3)) & 1)) sc[x][e] = -INFINITY;
+      }
+    } else if (tok0 + kTile > all_to || tok0 < all_from) {
       const uint32_t at = (uint32_t)(tok0 + 4 * h - see_from);
 #pragma unroll
       for (int x = 0; x < TB; ++x)
@@ -383,8 +424,10 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(C
     }
     __syncthreads();
     for (int t = t0; t < t1; ++t) {
-      const int tok0 = from + t * kTile, now = (t - t0) & 1;
-      const bool some = tok0 < any_to && tok0 + kTile > any_from;
+      const int tok0 = SIGHT ? place(t * kTile) : from + t * kTile, now = (t - t0) & 1;
+      const int tok1 = SIGHT && TB == 2 ? place(t * kTile + kBlockTokens) : tok0;
+      const auto seen = [&](int tok) { return tok < any_to && (tok + kBlockTokens > any_from || tok < g.sinks); };
+      const bool some = SIGHT ? seen(tok0) || seen(tok1) : tok0 < any_to && tok0 + kTile > any_from;
       if (t + 1 < t1) put_tile(next, sh.k[now ^ 1], sh.v[now ^ 1]);
       if (t + 2 < t1) load_tile(next, t + 2);
       if (some) {
@@ -392,7 +435,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(C
         __builtin_amdgcn_s_setprio(1);
         scores(sh.k[now]);
         __builtin_amdgcn_s_setprio(0);
-        probabilities(tok0);
+        probabilities(tok0, tok1);
         __builtin_amdgcn_s_setprio(1);
         weigh(sh.v[now]);
         __builtin_amdgcn_s_setprio(0);
@@ -454,7 +497,17 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(C
 }
 
 template <int D, int WAVES>
-void launch(const CacheDev &d, const CacheQuery &q, hipStream_t s) {
+__global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(CacheDev d, CacheQuery q, int tiles, int tile_rows, int split, uint32_t first) {
+  attend_many<D, WAVES, false>(d, q, CacheSight{}, tiles, tile_rows, split, first);
+}
+
+template <int D, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt_sight(CacheDev d, CacheQuery q, CacheSight g, int tiles, int tile_rows, int split, uint32_t first) {
+  attend_many<D, WAVES, true>(d, q, g, tiles, tile_rows, split, first);
+}
+
+template <int D, int WAVES>
+void launch(const CacheDev &d, const CacheQuery &q, const CacheSight *g, hipStream_t s) {
   constexpr int kWorkers = kUnits * at_once(D, WAVES);
   const int64_t rows = (int64_t)q.share * q.r.max_new;
   const int tiles = (int)((rows + WAVES * 32 - 1) / (WAVES * 32)), tile_rows = (int)((rows + tiles - 1) / tiles + 31) / 32 * 32;  // (all about as long)
@@ -463,8 +516,11 @@ void launch(const CacheDev &d, const CacheQuery &q, hipStream_t s) {
   // (steps of all row tiles are counted in 32 bits)
   const bool split = groups < (q.r.n > 1 ? kSplit : 1) * kWorkers && groups * ((int64_t)d.max_pages * d.page_blocks + 1) < (int64_t)1 << 32;
   const int64_t all = split ? groups + kWorkers : groups, most = 1 << 22;  // (of a launch; one that finds no rows takes 10 ns: 512 items of 8 heads, one of 32,768 rows, 28 ms of which it takes 6)
-  for (int64_t at = 0; at < all; at += most)
-    k_cache_prompt<D, WAVES><<<(uint32_t)(all - at < most ? all - at : most), WAVES * 64, sizeof(Shared<D>), s>>>(d, q, tiles, tile_rows, split, (uint32_t)at);
+  for (int64_t at = 0; at < all; at += most) {
+    const uint32_t grid = (uint32_t)(all - at < most ? all - at : most);
+    if (g) k_cache_prompt_sight<D, WAVES><<<grid, WAVES * 64, sizeof(Shared<D>), s>>>(d, q, *g, tiles, tile_rows, split, (uint32_t)at);
+    else k_cache_prompt<D, WAVES><<<grid, WAVES * 64, sizeof(Shared<D>), s>>>(d, q, tiles, tile_rows, split, (uint32_t)at);
+  }
 }
 
 }  // namespace
@@ -473,18 +529,20 @@ void launch(const CacheDev &d, const CacheQuery &q, hipStream_t s) {
 size_t cache_prompt_part_rows() { return (size_t)2 * kUnits * kRows; }
 size_t cache_prompt_groups() { return (size_t)4 * kUnits; }
 
-void launch_cache_prompt(const CacheDev &d, const CacheQuery &q, hipStream_t s) {
+void launch_cache_prompt(const CacheDev &d, const CacheQuery &q, const CacheSight *g, hipStream_t s) {
   switch (d.head_dim) {
-    case 64: return launch<64, 8>(d, q, s);
-    case 96: return launch<96, 8>(d, q, s);
-    case 128: return launch<128, 8>(d, q, s);
-    default: return launch<256, 4>(d, q, s);
+    case 64: return launch<64, 8>(d, q, g, s);
+    case 96: return launch<96, 8>(d, q, g, s);
+    case 128: return launch<128, 8>(d, q, g, s);
+    default: return launch<256, 4>(d, q, g, s);
   }
 }
 
 hipError_t allow_large_lds_cache_prompt() {
   const auto allow = [](const void *f, size_t bytes) { return hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes); };
   if (const hipError_t e = allow(reinterpret_cast<const void *>(k_cache_prompt<128, 8>), sizeof(Shared<128>))) return e;
+  if (const hipError_t e = allow(reinterpret_cast<const void *>(k_cache_prompt_sight<128, 8>), sizeof(Shared<128>))) return e;
+  if (const hipError_t e = allow(reinterpret_cast<const void *>(k_cache_prompt_sight<256, 4>), sizeof(Shared<256>))) return e;
   return allow(reinterpret_cast<const void *>(k_cache_prompt<256, 4>), sizeof(Shared<256>));
 }
 

@@ -79,6 +79,16 @@ class CacheQuery(C.Structure):
                 ("out_head_stride", C.c_int64), ("d_lse", C.c_void_p)]
 
 
+class CacheSight(C.Structure):
+    _fields_ = [("sinks", C.c_int32), ("tree_words", C.c_int32), ("d_tree", C.c_void_p)]
+
+
+class LogitsQuery(C.Structure):  # (logits.py)
+    _fields_ = [("rows", C.c_int64), ("row_stride", C.c_int64), ("vocab", C.c_int32), ("type", C.c_int32), ("top", C.c_int32), ("tokens", C.c_int32),
+                ("scale", C.c_float), ("d_logits", C.c_void_p), ("d_tokens", C.c_void_p), ("d_lse", C.c_void_p), ("d_entropy", C.c_void_p),
+                ("d_logprobs", C.c_void_p), ("d_top", C.c_void_p), ("d_top_logprobs", C.c_void_p), ("d_scratch", C.c_void_p), ("scratch_bytes", C.c_size_t)]
+
+
 class RtamsError(RuntimeError):
     def __init__(self, code: int, what: str, detail: str):
         super().__init__(f"{what}: {_NAMES.get(code, code)}: {detail}")
@@ -146,12 +156,19 @@ def lib():
         L.rtams_cache_write.argtypes = [vp, i32, i64, vp, vp, i64, i32, vp, vp, i64, i64, i32, vp]
         L.rtams_cache_read.argtypes = [vp, i32, i64, vp, vp, i64, i32, vp, vp, i32, vp]
         L.rtams_cache_attend.argtypes = [vp, vp, i64, vp, vp, i64, vp]  # (a packed CacheQuery)
+        L.rtams_cache_attend_sight.argtypes = [vp, vp, vp, i64, vp, vp, i64, vp]  # (... and a packed CacheSight)
+        L.rtams_cache_tree.argtypes = [vp, i64, vp, vp, i64, i32, vp, vp, i32, vp, vp]
+        L.rtams_cache_walk.argtypes = [vp, i64, vp, i64, i32, vp, vp, vp, vp, vp, vp, vp]
+        L.rtams_cache_keep.argtypes = [vp, i64, vp, vp, i64, i32, vp, vp, vp]
         L.rtams_cache_fork.argtypes = [vp, i64, vp, vp, i32, vp]
         L.rtams_cache_trim.argtypes = [vp, i64, vp, vp, vp]
         L.rtams_cache_compact.argtypes = [vp, vp]
         L.rtams_cache_free_pages.argtypes = [vp, C.POINTER(i64)]
         L.rtams_cache_poll_error.argtypes = [vp]
         L.rtams_cache_clear_error.argtypes = [vp]
+        L.rtams_logits_scratch_bytes_for.restype = C.c_size_t
+        L.rtams_logits_scratch_bytes_for.argtypes = [vp]  # (a packed LogitsQuery)
+        L.rtams_logits_score.argtypes = [vp, vp]
         L.rtams_copy_plain.argtypes = [vp, vp, C.c_size_t, vp]
         L.rtams_read_plain.argtypes = [vp, C.c_size_t, vp, vp]
         _lib = L

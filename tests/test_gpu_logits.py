@@ -1,0 +1,270 @@
+"""Scores of rows of logits against 64 bits and a stable sort.
+
+How far the numbers may be off is derived, with u = 2^-24 the rounding of a number in 32 bits.  A power's exponent z = c (x - m) is off by 3 u |z| (difference,
+product, c), a power by that times ln 2 and its own 4 u.  Sums: 32 terms in a lane's accumulator of a panel, 2 to join those, one a panel, 12 over
+lanes, wavefronts and pieces, each off by u, with a factor of 4 u where sums are moved to another largest: (60 + 5 panels) u in all.  So
+log S is off by s = (64 + 5 panels) u + 3 u sum p |z|, and what is made of it by that and 4 u of each of its terms; the entropy's T / S by s (1 + sum p |z|) + 3 u sum p z^2."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2408_02937_amd.logits import score
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+U = 2.0 ** -24
+END = 2.0 ** 128 * (1 - 2.0 ** -25)  # what is further from 0 is infinite in 32 bits: the largest number, 2^128 (1 - 2^-24), and half a step
+TYPES = [torch.bfloat16, torch.float16, torch.float32]
+
+
+def gen(seed):
+    return torch.Generator(device=DEV).manual_seed(seed)
+
+
+def some(rows, vocab, dtype, seed=0, width=3.0, ahead=0, stride=None):
+    """Rows that begin `ahead` elements into their memory, `stride` apart."""
+    stride = stride or vocab
+    x = torch.empty(ahead + rows * stride, dtype=dtype, device=DEV)
+    y = x[ahead:].as_strided((rows, vocab), (stride, 1))
+    y.copy_(torch.randn((rows, vocab), device=DEV, generator=gen(seed)) * width)
+    return y
+
+
+def check(x, tokens=None, top=0, scale=1.0, got=None):
+    r = got or score(x, tokens, top=top, scale=scale)
+    torch.cuda.synchronize()
+    f = x.float().cpu().numpy().astype(np.float64)
+    panels = f.shape[1] // (65_536 // x.element_size()) + 2
+    c = np.float64(np.float32(scale))
+    with np.errstate(all="ignore"):
+        wrong = np.isnan(f).any(-1) | (f == np.inf).any(-1)
+        none = ~wrong & (f == -np.inf).all(-1)
+        fine = ~wrong & ~none
+        m = np.where(fine, f.max(-1), 0.0)
+        z = (f - m[:, None]) * c
+        e = np.exp(z)
+        s = e.sum(-1)
+        p = e / s[:, None]
+        zz = np.where(p > 0, z, 0.0)
+        mean, square = (p * np.abs(zz)).sum(-1), (p * zz * zz).sum(-1)
+        entropy, lse = np.log(s) + mean, m * c + np.log(s)
+        logp = z - np.log(s)[:, None]
+    off = (64 + 5 * panels) * U + 3 * U * mean
+    num = lambda t: t.double().cpu().numpy()
+    ent, ls = num(r.entropy), num(r.lse)
+    assert np.isnan(ent[wrong]).all() and np.isnan(ls[wrong]).all() and (ent[none] == 0).all() and (ls[none] == -np.inf).all()
+    far = np.abs(lse) > END
+    assert (ls[far & fine] == np.sign(lse[far & fine]) * np.inf).all()
+    fine_lse = fine & ~far
+    assert (np.abs(ls - lse) <= off + 4 * U * (np.abs(m * c) + np.abs(np.log(s))))[fine_lse].all()
+    assert (np.abs(ent - entropy) <= off * (1 + mean) + 3 * U * square + 4 * U * (np.abs(np.log(s)) + mean) + 1e-30)[fine].all()
+
+    def check_logprobs(got, at):  # at: tokens, -1: none
+        there = (at >= 0) & (at < f.shape[1])
+        want = np.where(there, np.take_along_axis(logp, np.where(there, at, 0), 1), -np.inf)
+        want[none] = -np.inf
+        got = num(got)
+        assert np.isnan(got[wrong]).all()
+        low = (want < -END) & ~wrong[:, None]
+        assert (got[low] == -np.inf).all()
+        ok = fine[:, None] & ~low
+        with np.errstate(all="ignore"):
+            bound = off[:, None] + 4 * U * (np.abs(np.log(s))[:, None] + np.abs(want))
+            assert (np.abs(got - want) <= bound)[ok].all()
+
+    if tokens is not None:
+        assert r.logprobs.shape == tokens.shape
+        check_logprobs(r.logprobs.reshape(len(f), -1), tokens.cpu().numpy().reshape(len(f), -1))
+    if top:
+        k = min(top, f.shape[1])
+        order = np.argsort(-f + 0.0, axis=-1, kind="stable")[:, :k]
+        want = np.full((len(f), top), -1)
+        want[:, :k] = np.where(np.take_along_axis(f, order, 1) == -np.inf, -1, order)
+        want[wrong] = -1
+        assert np.array_equal(r.top.cpu().numpy(), want)
+        check_logprobs(r.top_logprobs, want)
+    return r
+
+
+def tokens_for(rows, vocab, m, seed=5):
+    t = torch.randint(0, vocab, (rows, m) if m != 1 else (rows,), dtype=torch.int32, device=DEV, generator=gen(seed))
+    return t
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab", [1, 2, 7, 8, 9, 255, 2047, 4096, 16_383, 16_385, 32_761, 32_768, 32_769, 100_003])
+def test_sizes(vocab, dtype):
+    for rows, top, m, scale in ((1, 5, 1, 1.0), (3, 64, 4, 0.7), (7, 1, 0, 2.0)):
+        x = some(rows, vocab, dtype, seed=vocab + rows)
+        check(x, tokens_for(rows, vocab, m) if m else None, top, scale)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("ahead,more", [(0, 0), (1, 0), (3, 5), (7, 1), (8, 64)])
+def test_addresses_and_strides(dtype, ahead, more):
+    for rows, vocab in ((5, 1000), (2, 33_333), (1030, 513)):
+        x = some(rows, vocab, dtype, seed=ahead, ahead=ahead, stride=vocab + more)
+        check(x, tokens_for(rows, vocab, 2), 9)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows", [1, 2, 33, 511, 1023, 1024, 1500])
+def test_rows_in_pieces_and_whole(dtype, rows):
+    vocab = 70_001 if rows < 600 else 9_001
+    check(some(rows, vocab, dtype, seed=rows), tokens_for(rows, vocab, 1), 20, 1.3)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_a_long_row(dtype):
+    check(some(2, 3_000_017, dtype, seed=1), tokens_for(2, 3_000_017, 3), 64)
+
+
+def shapes_of_rows(vocab, dtype):
+    """Rows whose most likely tokens are hard to tell."""
+    t = torch.arange(vocab, device=DEV)
+    g = gen(9)
+    rows = [torch.zeros(vocab, device=DEV), torch.full((vocab,), -2.5, device=DEV), t * 1.0, -t * 1.0, (t % 7) * 1.0, (t % 2) * -1.0, torch.where(t % 3 == 0, -0.0, 0.0),
+            torch.randint(-3, 3, (vocab,), device=DEV, generator=g) * 0.5, torch.where(t < vocab - 70, 0.0, 1.0), torch.where(t >= 70, 0.0, 1.0)]
+    one = torch.full((vocab,), -4.0, device=DEV)
+    one[5::2048] = 3.0  # one lane's
+    rows.append(one)
+    rows.append(torch.where(t % 2048 < 24, torch.randn(vocab, device=DEV, generator=g), torch.tensor(-9.0, device=DEV)))  # three lanes'
+    rows.append(torch.randn(vocab, device=DEV, generator=g).sort().values)
+    rows.append(torch.randn(vocab, device=DEV, generator=g).sort(descending=True).values)
+    rows.append(torch.randn(vocab, device=DEV, generator=g) * 1e-3)
+    rows.append(torch.randn(vocab, device=DEV, generator=g) * 1e-40)
+    return torch.stack(rows).to(dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab", [100, 5_000, 40_000, 140_000])
+@pytest.mark.parametrize("top", [1, 20, 64])
+def test_rows_of_equal_and_ordered_logits(dtype, vocab, top):
+    x = shapes_of_rows(vocab, dtype)
+    check(x, None, top)
+    check(x.repeat(65, 1), None, top)  # (whole rows)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("copies", [1, 100])
+def test_masks_infinities_and_nan(dtype, copies):
+    vocab = 35_000
+    lowest = torch.finfo(dtype).min
+    x = some(12, vocab, dtype, seed=3)
+    hide = torch.rand(x.shape, device=DEV, generator=gen(4)) < 0.95
+    x[0][hide[0]] = -math.inf
+    x[1][hide[1]] = lowest
+    x[2] = -math.inf
+    x[3] = lowest
+    x[4] = -math.inf
+    x[4, 20_000] = 1.5
+    x[5] = lowest
+    x[5, 34_999] = -7.0
+    x[6, 123] = math.nan
+    x[7, 30_000] = math.inf
+    x[8] = -math.inf
+    x[8, 8::3000] = 2.0
+    x[9] = -math.inf
+    x[9, 77] = math.nan
+    x[10, 4_000] = torch.finfo(dtype).max
+    x[11, :16_000] = -math.inf
+    x = x.repeat(copies, 1)
+    t = torch.tensor([20_000, 34_999, 123, 77, -1, vocab, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32, device=DEV).repeat(len(x), 1)
+    for scale in (1.0, 0.5, 3.0):
+        check(x, t, 40, scale)
+
+
+def test_peaked_and_flat_rows():
+    for dtype in TYPES:
+        for width in (0.0, 1e-3, 0.1, 30.0, 300.0):
+            check(some(4, 50_000, dtype, seed=11, width=width), tokens_for(4, 50_000, 2), 8)
+        check(some(3, 50_000, dtype, seed=12) + 500.0, tokens_for(3, 50_000, 2), 8)
+
+
+def test_places_beyond_32_bits():
+    rows, vocab, stride = 20, 5_000, 250_000_000  # halves: 10 GB
+    x = torch.zeros((rows - 1) * stride + vocab, dtype=torch.float16, device=DEV).as_strided((rows, vocab), (stride, 1))
+    x.copy_(torch.randn((rows, vocab), device=DEV, generator=gen(6)) * 2)
+    check(x, tokens_for(rows, vocab, 2), 5)
+
+
+def test_no_rows_and_no_tokens():
+    x = some(0, 50, torch.float32)
+    r = score(x, torch.zeros((0, 3), dtype=torch.int32, device=DEV), top=2)
+    assert r.lse.shape == (0,) and r.logprobs.shape == (0, 3) and r.top.shape == (0, 2)
+    x = some(4, 50, torch.float32)
+    r = score(x, torch.zeros((4, 0), dtype=torch.int32, device=DEV))
+    assert r.logprobs.shape == (4, 0) and r.top is None and r.top_logprobs is None
+    check(x, None, 0, got=r)
+
+
+def test_the_same_bits_every_time():
+    for rows, vocab in ((2, 140_000), (1500, 9_000)):
+        x, t = some(rows, vocab, torch.bfloat16, seed=2), tokens_for(rows, vocab, 2)
+        a = score(x, t, top=30)
+        for _ in range(5):
+            for u, v in zip(a, score(x, t, top=30)):
+                assert torch.equal(u, v)
+
+
+def test_another_stream_and_two_at_once():
+    x, y = some(40, 60_000, torch.float32, seed=1), some(3, 131_072, torch.bfloat16, seed=2)
+    t = tokens_for(40, 60_000, 2)
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    out = []
+    for _ in range(4):
+        out.append((score(x, t, top=10, stream=a), score(y, top=10, stream=b)))
+    torch.cuda.synchronize()
+    for r, s in out:
+        check(x, t, 10, got=r)
+        check(y, None, 10, got=s)
+    with torch.cuda.stream(a):
+        r = score(x, t, top=10)
+    check(x, t, 10, got=r)
+
+
+def test_recorded_calls():
+    x, y = some(5, 80_000, torch.bfloat16, seed=1), some(1200, 3_001, torch.float32, seed=2)
+    t = tokens_for(5, 80_000, 3)
+    score(x, t, top=7), score(y, top=3)
+    graphs = []
+    for _ in range(2):  # two that live at once
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = score(x, t, top=7), score(y, top=3)
+        graphs.append((g, out))
+    for turn in range(3):
+        x.copy_(torch.randn(x.shape, device=DEV, generator=gen(30 + turn)) * 2)
+        y.copy_(torch.randn(y.shape, device=DEV, generator=gen(40 + turn)) * 2)
+        for g, _ in graphs:
+            g.replay()
+        eager = score(x, t, top=7)
+        torch.cuda.synchronize()
+        for _, (a, b) in graphs:
+            check(x, t, 7, got=a)
+            check(y, None, 3, got=b)
+            assert all(torch.equal(u, v) for u, v in zip(a, eager))
+
+
+def test_refusals():
+    x = some(4, 100, torch.float32)
+    t = torch.zeros(4, dtype=torch.int32, device=DEV)
+    for bad in (x.double(), x[0], x.t(), x.cpu(), x[:, :0], x[:, ::2]):
+        with pytest.raises(ValueError):
+            score(bad)
+    for bad in (t.long(), t[:3], t.cpu(), torch.zeros((4, 2, 1), dtype=torch.int32, device=DEV), torch.zeros((4, 4), dtype=torch.int32, device=DEV)[:, ::2]):
+        with pytest.raises(ValueError):
+            score(x, bad)
+    for kw in (dict(top=65), dict(top=-1), dict(scale=0.0), dict(scale=-1.0), dict(scale=math.nan), dict(scale=math.inf)):
+        with pytest.raises(Exception):
+            score(x, **kw)
+    y = x.clone().requires_grad_()
+    with pytest.raises(ValueError):
+        score(y)
+    with torch.no_grad():
+        check(y.detach(), t, 3, got=score(y, t, top=3))

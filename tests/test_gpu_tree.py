@@ -1,0 +1,620 @@
+"""Trees of drafted tokens over the cache, and windows with sinks: attention against 64 bits under any mask, ancestors, paths and kept rows
+against Python, and a drafted step with all of them.  The bound of attention is that of test_gpu_cache.py."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2408_02937_amd import rtams
+from paper_2408_02937_amd.cache import Cache
+from tests.test_gpu_cache import DEV, U, Filled, check_attention, floats, held, ints, starts_of, unit_of
+
+pytestmark = pytest.mark.gpu
+
+
+def plain(q, k, v, share, scale, see):
+    """plain_attention of test_gpu_cache.py under a mask [rows][tokens]."""
+    rows, heads, d = q.shape
+    out, lse = np.zeros((rows, heads, d)), np.full((rows, heads), -np.inf)
+    off, mass = np.zeros((rows, heads)), np.zeros((rows, heads, d))
+    for h in range(heads):
+        kk, vv = k[:, h // share], v[:, h // share]
+        s = scale * (q[:, h] @ kk.T)
+        big = 2.1 * U * abs(scale) * (np.abs(q[:, h]) @ np.abs(kk).T)
+        s = np.where(see, s, -np.inf)
+        some = see.any(-1)
+        m = np.where(some, s.max(-1, initial=-np.inf), 0.0)
+        p = np.exp(s - m[:, None])
+        total = np.where(some, p.sum(-1), 1.0)
+        out[:, h] = p @ vv / total[:, None]
+        off[:, h] = np.where(see, big, 0.0).max(-1, initial=0.0)
+        mass[:, h] = p @ np.abs(vv) / total[:, None] + see.sum(-1)[:, None] * 2.0 ** -24 * np.abs(vv).max(0, initial=0.0)
+        lse[some, h] = (m + np.log(total))[some]
+    return out, lse, off, mass
+
+
+def sight(length, count, window=0, sinks=0, seen=None):
+    """[count][length]: seen: of each row the rows of its item that it sees."""
+    t, base = np.arange(length), length - count
+    see = np.zeros((count, length), dtype=bool)
+    for j in range(count):
+        pos = base + (j if seen is None else len(seen[j]) - 1)
+        see[j] = t <= pos
+        if window:
+            see[j] &= (t > pos - window) | (t < sinks)
+        if seen is not None:
+            see[j, base:] = False
+            see[j, [base + i for i in seen[j]]] = True
+    return see
+
+
+def random_tree(rng, count, wide=8):
+    return [-1] + [int(rng.integers(max(0, j - wide), j)) for j in range(1, count)] if count else []
+
+
+def ancestors(parents):
+    out = []
+    for j, p in enumerate(parents):
+        out.append((out[p] if p >= 0 else []) + [j])
+    return out
+
+
+def words_of(seen_of_items, words, junk=None):
+    """The rows' bits; junk: bits beyond the item's rows, which say nothing."""
+    flat = []
+    for seen in seen_of_items:
+        for s in seen:
+            bits = sum(1 << i for i in s)
+            if junk is not None:
+                bits |= int(junk.integers(0, 1 << 62)) << len(seen)
+            flat.append([(bits >> (32 * w)) & 0xffffffff for w in range(words)])
+    return torch.from_numpy(np.array(flat, dtype=np.uint32).reshape(-1, words).view(np.int32)).to(DEV)
+
+
+def run(f, counts, heads, seen=None, window=0, sinks=0, scale=None, seed=1, extra_words=0, junk=None, same_to=None):
+    """Attention of a Filled cache's last rows against the plain one."""
+    q = f.query(counts, heads, seed)
+    lse = torch.full(q.shape[:2], 123.0, device=DEV)
+    one = all(c == 1 for c in counts)
+    tree = None if seen is None else words_of(seen, -(-max(counts) // 32) + extra_words, junk)
+    kw = dict(scale=scale, window=window, sinks=sinks, tree=tree)
+    args = (ints(f.seqs), None if one else starts_of(counts), None if one else max(counts))
+    out = f.cache.attend(0, q, *args, lse=lse, **kw)
+    torch.cuda.synchronize()
+    assert f.cache.poll_error() == 0
+    qs, at, parts = floats(q).astype(np.float64), 0, []
+    for i, ((k, v), c) in enumerate(zip(f.plain, counts)):
+        see = sight(len(k), c, window, sinks, None if seen is None else seen[i])
+        parts.append(plain(qs[at:at + c], k, v, heads // f.kv_heads, f.dim ** -0.5 if scale is None else scale, see))
+        at += c
+    check_attention(out, lse, [np.concatenate(x) for x in zip(*parts)], unit_of(q.dtype))
+    for _ in range(2):
+        assert torch.equal(out, f.cache.attend(0, q, *args, **kw))
+    return q, out
+
+
+SHAPES = [(8, 2, 64), (12, 12, 96), (6, 2, 96), (32, 8, 128), (17, 1, 128), (8, 2, 256), (10, 5, 256)]
+
+
+# ------------------------------------------------------------------ windows with sinks
+@pytest.mark.parametrize("heads,kv,dim", SHAPES)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_sinks_of_single_tokens(heads, kv, dim, dtype):
+    f = Filled([1, 2, 31, 33, 127, 128, 129, 300, 777], kv, dim, page=64, dtype=dtype, seed=heads)
+    for window, sinks in ((1, 1), (40, 4), (100, 33), (64, 64), (500, 10), (7, 1000)):
+        run(f, [1] * 9, heads, window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("heads,kv,dim", [(8, 2, 64), (12, 12, 96), (32, 8, 128), (8, 2, 256), (16, 1, 128)])
+@pytest.mark.parametrize("counts", [[2, 1, 3, 2], [9, 17, 0, 8], [40, 0, 64, 65], [130, 200, 1, 333]])
+def test_sinks_of_several_rows(heads, kv, dim, counts):
+    f = Filled([130, 200, 64, 733], kv, dim, page=32, seed=dim)
+    for window, sinks in ((50, 4), (1, 40), (129, 32), (20, 2 ** 31 - 1)):
+        run(f, counts, heads, window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("lengths,count,heads,kv,dim", [([20_011, 64], 1, 8, 2, 64), ([9_000, 17, 30_001], 7, 4, 1, 128), ([6_000], 900, 4, 1, 128), ([2_500] * 3, 2_500, 2, 2, 96),
+                                                        ([12_345], 20, 16, 2, 256), ([3_300, 1_700], 700, 8, 2, 256)])
+def test_sinks_of_long_sequences(lengths, count, heads, kv, dim):
+    f = Filled(lengths, kv, dim, page=128, seed=5)
+    counts = [min(x, count) for x in lengths]
+    for window, sinks in ((5000, 4), (300, 100), (1000, 3)):
+        run(f, counts, heads, window=window, sinks=sinks)
+
+
+def test_sinks_of_many_sequences():
+    lengths = [(i * 53) % 197 for i in range(700)]
+    f = Filled(lengths, 1, 64, page=32, seed=6)
+    run(f, [min(x, i % 4) for i, x in enumerate(lengths)], 2, window=30, sinks=5)
+
+
+# ------------------------------------------------------------------ attention of trees
+@pytest.mark.parametrize("heads,kv,dim", SHAPES)
+@pytest.mark.parametrize("counts", [[1, 1, 1, 1], [2, 1, 3, 2], [5, 17, 0, 8], [40, 0, 64, 65], [130, 200, 1, 333]])
+def test_trees(heads, kv, dim, counts):
+    rng = np.random.default_rng(dim + sum(counts))
+    f = Filled([130, 200, 64, 733], kv, dim, page=32, dtype=torch.float16 if heads % 3 else torch.bfloat16, seed=dim)
+    counts = [min(c, x) for c, x in zip(counts, f.lengths)]
+    seen = [ancestors(random_tree(rng, c)) for c in counts]
+    run(f, counts, heads, seen)
+    run(f, counts, heads, seen, window=60)
+    run(f, counts, heads, seen, window=25, sinks=6)
+
+
+@pytest.mark.parametrize("counts", [[3, 1, 5], [30, 20, 33], [64, 1, 63], [100, 129, 20]])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_any_rows_may_be_seen(counts, dim):
+    """Bits in no order, rows that see no row of their item, bits beyond them, more words than rows need, sequences that are all tree."""
+    rng = np.random.default_rng(sum(counts) + dim)
+    f = Filled([counts[0], 129, 300], 2, dim, page=64, seed=dim)
+    seen = [[sorted(rng.permutation(c)[:rng.integers(0, c + 1)].tolist()) if rng.random() < 0.8 else [] for _ in range(c)] for c in counts]
+    q, out = run(f, counts, 4, seen, extra_words=2, junk=np.random.default_rng(0))
+    for r, s in enumerate(seen[0]):  # nothing lies before this item
+        assert bool(out[r].any()) == bool(s)
+    run(f, counts, 4, seen, window=40, extra_words=1)
+    run(f, counts, 4, seen, window=9, sinks=3)
+
+
+@pytest.mark.parametrize("lengths,count,heads,kv,dim", [([20_011, 300], 6, 8, 2, 64), ([9_000, 17, 30_001], 13, 16, 4, 128), ([6_100], 40, 4, 1, 128), ([4_500] * 3, 63, 8, 2, 96),
+                                                        ([12_345], 20, 16, 2, 256), ([5_000, 2_000], 300, 4, 2, 128), ([1_500, 7_000], 1_024, 2, 1, 64)])
+def test_trees_behind_long_sequences(lengths, count, heads, kv, dim):
+    rng = np.random.default_rng(count)
+    f = Filled(lengths, kv, dim, page=128, seed=5)
+    counts = [min(x, count) for x in lengths]
+    seen = [ancestors(random_tree(rng, c, 20)) for c in counts]
+    run(f, counts, heads, seen)
+    run(f, counts, heads, seen, window=1_100, sinks=4)
+
+
+@pytest.mark.parametrize("n", [90, 300, 700])
+def test_trees_of_many_sequences(n):
+    rng = np.random.default_rng(n)
+    lengths = [(i * 53) % 97 for i in range(n)]
+    f = Filled(lengths, 1, 64, page=32, seed=24)
+    counts = [min(x, i % 6) for i, x in enumerate(lengths)]
+    run(f, counts, 12 if n < 700 else 2, [ancestors(random_tree(rng, c)) for c in counts])
+
+
+@pytest.mark.parametrize("count", [4, 70])
+def test_a_chain_is_what_no_tree_is(count):
+    f = Filled([300, 129], 2, 128, page=64, seed=26)
+    counts = [count, count]
+    seen = [[list(range(j + 1)) for j in range(count)]] * 2
+    q, out = run(f, counts, 8, seen)
+    for kw in (dict(), dict(window=100)):
+        a = f.cache.attend(0, q, starts=starts_of(counts), max_new=count, tree=words_of(seen, -(-count // 32)), **kw)
+        b = f.cache.attend(0, q, starts=starts_of(counts), max_new=count, **kw)
+        assert (a.float() - b.float()).abs().max() <= 2.0 ** -7 * b.float().abs().max()
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.2, 1.0, 0.3])
+def test_scales_of_the_scores(scale):
+    rng = np.random.default_rng(0)
+    f = Filled([300, 129], 2, 64, seed=26, dtype=torch.float16)
+    for count in (6, 90):
+        run(f, [count] * 2, 4, [ancestors(random_tree(rng, count)) for _ in range(2)], scale=scale)
+
+
+@pytest.mark.parametrize("lengths,counts,heads", [([3, 40, 0], [5, 5, 2], 4), ([30, 200, 64], [90, 100, 65], 4)])
+def test_more_rows_than_tokens_are_refused_and_left(lengths, counts, heads):
+    rng = np.random.default_rng(1)
+    f = Filled(lengths, 2, 128, seed=40)
+    q = f.query(counts, heads)
+    seen = [ancestors(random_tree(rng, c)) for c in counts]
+    tree = words_of(seen, -(-max(counts) // 32))
+    out, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 5.0, device=DEV)
+    f.cache.attend(0, q, starts=starts_of(counts), max_new=max(counts), out=out, lse=lse, tree=tree, window=20, sinks=2)
+    torch.cuda.synchronize()
+    assert f.cache.poll_error() == rtams.EINVAL
+    f.cache.clear_error()
+    at = np.concatenate([[0], np.cumsum(counts)])
+    for i, (n, c) in enumerate(zip(lengths, counts)):
+        rows = slice(at[i], at[i + 1])
+        if c > n:
+            assert (out[rows] == 7.0).all() and (lse[rows] == 5.0).all(), i
+        else:
+            k, v = f.plain[i]
+            want = plain(floats(q[rows]).astype(np.float64), k, v, heads // 2, 128 ** -0.5, sight(n, c, 20, 2, seen[i]))
+            check_attention(out[rows], lse[rows], want, unit_of(q.dtype))
+
+
+def test_a_row_that_is_not_finite_spoils_itself_only():
+    rng = np.random.default_rng(2)
+    f = Filled([200, 90], 2, 64, seed=9)
+    for counts in ([3, 2], [40, 33]):
+        q = f.query(counts, 8)
+        kw = dict(starts=starts_of(counts), max_new=max(counts), tree=words_of([ancestors(random_tree(rng, c)) for c in counts], -(-max(counts) // 32)))
+        clean = f.cache.attend(0, q, **kw)
+        q2 = q.clone()
+        q2[0, 3, 5] = float("nan")
+        out = f.cache.attend(0, q2, **kw)
+        same = torch.ones(q.shape[:2], dtype=torch.bool, device=DEV)
+        same[0, 3] = False
+        assert not torch.isfinite(out[0, 3]).any() and torch.equal(out[same], clean[same])
+
+
+# ------------------------------------------------------------------ ancestors and positions
+@pytest.mark.parametrize("counts", [[1], [5, 0, 33, 64, 1], [1024, 7], [300, 1000]])
+def test_ancestors_and_positions(counts):
+    rng = np.random.default_rng(sum(counts))
+    lengths = [c + int(rng.integers(0, 50)) for c in counts]
+    c = Cache(1, 64, page_tokens=32, pages=200, max_seqs=9, device=DEV)
+    seqs = ints(rng.permutation(9)[:len(counts)])
+    c.extend(seqs, starts_of(lengths))
+    kinds = [random_tree, lambda r, n: list(range(-1, n - 1)), lambda r, n: [-1] * n, lambda r, n: [int(r.integers(-1, j)) if j else -1 for j in range(n)],
+             lambda r, n: [-1] + [0] * (n - 1) if n else []]
+    for kind in kinds:
+        parents = [kind(rng, n) for n in counts]
+        tree, positions = c.tree(ints(sum(parents, [])), seqs, starts_of(counts), max(counts))
+        torch.cuda.synchronize()
+        assert c.poll_error() == 0
+        seen = [ancestors(p) for p in parents]
+        assert torch.equal(tree, words_of(seen, -(-max(counts) // 32)))
+        assert positions.tolist() == [x - n + len(s) - 1 for x, n, item in zip(lengths, counts, seen) for s in item]
+    tree, positions = c.tree(ints([-1] * len(counts)), seqs)  # a row each
+    assert tree.flatten().tolist() == [1] * len(counts) or min(lengths) == 0
+    assert positions.tolist() == [x - 1 for x in lengths] or min(lengths) == 0
+
+
+@pytest.mark.parametrize("bad", [[0, -1, 1], [-1, 1, 0], [-1, 0, -2], [-1, 0, 5], [-1, 2, 0]])
+def test_parents_that_are_none(bad):
+    c = Cache(1, 64, page_tokens=32, pages=10, max_seqs=3, device=DEV)
+    c.extend(starts=ints([0, 9, 18, 27]))
+    parents = ints([-1, 0, 0] + bad + [-1, 0, 1])
+    st = ints([0, 3, 6, 9])
+    tree, positions = torch.full((9, 1), 77, dtype=torch.int32, device=DEV), torch.full((9,), 77, dtype=torch.int32, device=DEV)
+    L = rtams.lib()
+    assert L.rtams_cache_tree(c._h, 3, None, st.data_ptr(), 9, 3, parents.data_ptr(), tree.data_ptr(), 1, positions.data_ptr(), c._stream(None)) == 0
+    torch.cuda.synchronize()
+    assert c.poll_error() == rtams.EINVAL
+    assert tree.flatten().tolist() == [1, 3, 5, 77, 77, 77, 1, 3, 7] and positions.tolist() == [6, 7, 7, 77, 77, 77, 6, 7, 8]
+    c.clear_error()
+    path, kept, following = c.walk(parents, ints(range(9)), ints(range(1, 10)), st, 3)
+    torch.cuda.synchronize()
+    assert c.poll_error() == rtams.EINVAL and kept.tolist()[1] == -1 and following.tolist()[1] == -1 and path.tolist()[3:6] == [-1] * 3
+    assert kept.tolist()[0::2] == [2, 3]
+
+
+# ------------------------------------------------------------------ paths
+def walked(parents, tokens, chosen):
+    if not parents:
+        return [], -1
+    path = [0]
+    while True:
+        want = chosen[path[-1]]
+        child = [j for j in range(len(parents)) if parents[j] == path[-1] and tokens[j] == want and want >= 0]
+        if not child:
+            return path, chosen[path[-1]]
+        path.append(child[0])
+
+
+@pytest.mark.parametrize("counts", [[1], [6, 0, 1, 30], [64, 65, 128], [1024, 3, 700], [2] * 200])
+@pytest.mark.parametrize("vocab", [2, 50])
+def test_paths(counts, vocab):
+    rng = np.random.default_rng(sum(counts) + vocab)
+    c = Cache(1, 64, page_tokens=32, pages=10, max_seqs=200, device=DEV)
+    for kind in range(4):
+        parents = [random_tree(rng, n, 4) if kind < 3 else list(range(-1, n - 1)) for n in counts]
+        tokens = [[int(rng.integers(-1, vocab)) for _ in range(n)] for n in counts]
+        chosen = [[int(rng.integers(-1 if kind == 0 else 0, vocab)) for _ in range(n)] for n in counts]
+        if kind >= 2:  # long paths
+            for p, t, ch in zip(parents, tokens, chosen):
+                for j in range(len(p) - 1, 0, -1):
+                    ch[p[j]] = t[j]
+        path, kept, following = c.walk(*(ints(sum(x, [])) for x in (parents, tokens, chosen)), starts_of(counts), max(counts))
+        torch.cuda.synchronize()
+        want = [walked(*x) for x in zip(parents, tokens, chosen)]
+        assert kept.tolist() == [len(w[0]) for w in want] and following.tolist() == [w[1] for w in want]
+        assert path.tolist() == sum([w[0] + [-1] * (n - len(w[0])) for w, n in zip(want, counts)], [])
+        assert c.poll_error() == 0
+    path, kept, following = c.walk(ints([-1] * len(counts)), ints([3] * len(counts)), ints(range(len(counts))))
+    assert path.tolist() == [0] * len(counts) and kept.tolist() == [1] * len(counts) and following.tolist() == list(range(len(counts)))
+
+
+# ------------------------------------------------------------------ kept rows
+def all_rows(c, lengths, layers):
+    st = starts_of(lengths)
+    return [[x.cpu() for x in c.read(i, sum(lengths), starts=st, max_new=max(max(lengths), 1))] for i in range(layers)]
+
+
+@pytest.mark.parametrize("dim,kv,layers,page", [(64, 1, 1, 32), (96, 3, 2, 32), (128, 2, 3, 64), (256, 2, 1, 96)])
+@pytest.mark.parametrize("counts", [[3, 1, 0, 7], [40, 64, 33, 1], [200, 5, 1024, 77]])
+def test_kept_rows(dim, kv, layers, page, counts):
+    rng = np.random.default_rng(dim + sum(counts))
+    before = [int(x) for x in rng.integers(0, 90, len(counts))]
+    before[1] = 31
+    n = len(counts)
+    lengths = [b + x for b, x in zip(before, counts)]
+    pages = sum(-(-x // page) for x in lengths) + 3
+    c = Cache(kv, dim, layers=layers, page_tokens=page, pages=pages, max_seqs=n + 1, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    for turn in range(4):
+        c.extend(starts=starts_of([x // 2 for x in lengths]))
+        c.extend(starts=starts_of([x - x // 2 for x in lengths]))
+        for layer in range(layers):
+            k, v = (torch.randn((sum(lengths), kv, dim), device=DEV, generator=g).bfloat16() for _ in range(2))
+            c.write(layer, k, v, starts=starts_of(lengths), max_new=max(lengths))
+        old = all_rows(c, lengths, layers)
+        if turn == 0:
+            paths = [sorted(rng.permutation(x)[:rng.integers(0, x + 1)].tolist()) for x in counts]
+        elif turn == 1:
+            paths = [list(range(x)) for x in counts]  # nothing moves
+        elif turn == 2:
+            paths = [list(range(1, x)) for x in counts]  # all by one
+        else:
+            paths = [list(range(x))[-(x // 3):] if x > 2 else [] for x in counts]
+        flat = [p + [-1] * (x - len(p)) for p, x in zip(paths, counts)]
+        c.keep(ints(sum(flat, [])), ints([len(p) for p in paths]), starts=starts_of(counts), max_new=max(counts))
+        torch.cuda.synchronize()
+        assert c.poll_error() == 0
+        now = [b + len(p) for b, p in zip(before, paths)]
+        assert c.lengths.tolist() == now + [0]
+        held_pages = [-(-x // page) for x in now]
+        assert c.free_pages == pages - sum(held_pages) and int(c.refs.sum()) == sum(held_pages)
+        assert ((c.table >= 0).sum(1).cpu() == torch.tensor(held_pages + [0])).all()
+        at, rows = np.concatenate([[0], np.cumsum(lengths)]), []
+        for i, p in enumerate(paths):
+            rows += list(range(at[i], at[i] + before[i])) + [at[i] + before[i] + j for j in p]
+        new = all_rows(c, now, layers)
+        for a, b in zip(old, new):
+            for x, y in zip(a, b):
+                assert torch.equal(x[rows], y)
+        c.trim(n=n)
+
+
+def kept_state(c):
+    return [c.table.clone(), c.lengths.clone(), c.refs.clone(), c.pages.clone()]
+
+
+@pytest.mark.parametrize("what", ["order", "twice", "beyond", "negative", "many", "none", "seq", "names", "rows", "short"])
+def test_bad_kept_rows_change_nothing(what):
+    c = Cache(2, 64, layers=2, page_tokens=32, pages=20, max_seqs=4, device=DEV)
+    c.extend(starts=ints([0, 40, 50, 90, 90]))
+    c.pages.copy_(torch.randint(0, 255, c.pages.shape, dtype=torch.uint8, device=DEV, generator=torch.Generator(device=DEV).manual_seed(0)))
+    path, kept, seqs, st = [0, 2, 5, 1, 3, -1], [2, 2], [0, 1], [0, 3, 6]
+    path[2] = -1
+    path[3:] = [0, 2, -1]
+    bad = dict(order=([2, 0, -1], 2), twice=([1, 1, -1], 2), beyond=([0, 3, -1], 2), negative=([-1, 1, -1], 2), many=([0, 1, 2], 4), none=([0, 1, 2], -1))
+    if what in bad:
+        path[:3], kept[0] = bad[what]
+    elif what == "seq":
+        seqs[0] = 4
+    elif what == "names":
+        seqs[0] = 1
+    elif what == "rows":
+        st = [0, 3, 7]
+    else:
+        seqs[0] = 3
+    state = kept_state(c)
+    c.keep(ints(path), ints(kept), ints(seqs), ints(st), 3)
+    torch.cuda.synchronize()
+    assert c.poll_error() == rtams.EINVAL
+    assert all(torch.equal(a, b) for a, b in zip(state, kept_state(c)))
+    c.clear_error()
+    c.keep(ints([0, 2, -1, 0, 2, -1]), ints([2, 2]), ints([0, 1]), ints([0, 3, 6]), 3)
+    torch.cuda.synchronize()
+    assert c.poll_error() == 0 and c.lengths.tolist() == [39, 9, 40, 0]
+
+
+def test_pages_that_are_shared_are_not_written_into():
+    c = Cache(1, 64, page_tokens=32, pages=20, max_seqs=3, device=DEV)
+    c.extend(ints([0]), ints([0, 40]))
+    c.pages.copy_(torch.randint(0, 255, c.pages.shape, dtype=torch.uint8, device=DEV, generator=torch.Generator(device=DEV).manual_seed(0)))
+    c.fork(ints([0]), ints([1]))
+    state = kept_state(c)
+    c.keep(ints([1, 2, -1]), ints([2]), ints([0]), ints([0, 3]), 3)
+    torch.cuda.synchronize()
+    assert c.poll_error() == rtams.EINVAL and all(torch.equal(a, b) for a, b in zip(state, kept_state(c)))
+    c.clear_error()
+    c.keep(ints([0, 1, -1]), ints([2]), ints([0]), ints([0, 3]), 3)  # nothing moves: what is shared is only cut
+    torch.cuda.synchronize()
+    assert c.poll_error() == 0 and c.lengths.tolist() == [39, 40, 0] and torch.equal(c.pages, state[3])
+    c.trim(ints([1]))
+    c.keep(ints([1, 2, -1]), ints([2]), ints([0]), ints([0, 3]), 3)
+    torch.cuda.synchronize()
+    assert c.poll_error() == 0 and c.lengths.tolist() == [38, 0, 0]
+
+
+def test_after_an_extend_that_was_dropped_nothing_is_cut():
+    c = Cache(1, 64, page_tokens=32, pages=2, max_seqs=2, max_pages=3, device=DEV)
+    c.extend(ints([0]), ints([0, 60]))
+    c.extend(ints([0]), ints([0, 8]))  # too few pages
+    c.keep(ints([0, 3, -1, -1, -1, -1, -1, -1]), ints([2]), ints([0]), ints([0, 8]), 8)
+    torch.cuda.synchronize()
+    assert c.poll_error() == rtams.EPOOL and c.lengths.tolist() == [60, 0]
+    c.clear_error()
+    c.extend(ints([0]), ints([0, 4]))
+    c.keep(ints([0, 3, -1, -1]), ints([2]), ints([0]), ints([0, 4]), 4)
+    torch.cuda.synchronize()
+    assert c.poll_error() == 0 and c.lengths.tolist() == [62, 0]
+
+
+def test_many_items_are_kept():
+    n = 1500
+    rng = np.random.default_rng(3)
+    c = Cache(1, 64, page_tokens=32, pages=2 * n, max_seqs=n, max_pages=2, device=DEV)
+    lengths = [int(x) for x in rng.integers(4, 60, n)]
+    c.extend(starts=starts_of(lengths))
+    k, v = (torch.randn((sum(lengths), 1, 64), device=DEV, generator=torch.Generator(device=DEV).manual_seed(1)).half() for _ in range(2))
+    c.write(0, k, v, starts=starts_of(lengths), max_new=60)
+    old = all_rows(c, lengths, 1)[0]
+    c.keep(ints([1, 3, -1, -1] * n), ints([2] * n), starts=ints(range(0, 4 * n + 1, 4)), max_new=4)
+    torch.cuda.synchronize()
+    assert c.poll_error() == 0 and c.lengths.tolist() == [x - 2 for x in lengths]
+    at, rows = np.concatenate([[0], np.cumsum(lengths)]), []
+    for i, x in enumerate(lengths):
+        rows += list(range(at[i], at[i] + x - 4)) + [at[i] + x - 3, at[i] + x - 1]
+    new = all_rows(c, [x - 2 for x in lengths], 1)[0]
+    assert all(torch.equal(x[rows], y) for x, y in zip(old, new))
+
+
+# ------------------------------------------------------------------ a step with all of them
+class Steps:
+    """Drafted steps of some sequences, with everything in the plain form beside them."""
+
+    def __init__(self, seed=0, n=5, layers=2, kv=2, heads=8, dim=64, nodes=9, page=32):
+        self.rng = np.random.default_rng(seed)
+        self.n, self.layers, self.kv, self.heads, self.dim, self.nodes = n, layers, kv, heads, dim, nodes
+        self.cache = Cache(kv, dim, layers=layers, page_tokens=page, pages=n * 8, max_seqs=n + 2, device=DEV)
+        self.seqs = ints(self.rng.permutation(n + 2)[:n])
+        first = [int(x) for x in self.rng.integers(1, 70, n)]
+        self.rows = [[(np.zeros((0, kv, dim)), np.zeros((0, kv, dim))) for _ in range(n)] for _ in range(layers)]
+        g = torch.Generator(device=DEV).manual_seed(seed)
+        self.random = lambda rows, heads: torch.randn((rows, heads, dim), device=DEV, generator=g).bfloat16()
+        self.cache.extend(self.seqs, starts_of(first))
+        for layer in range(layers):
+            k, v = self.random(sum(first), kv), self.random(sum(first), kv)
+            self.cache.write(layer, k, v, self.seqs, starts_of(first), max(first))
+            self.add(layer, k, v, first)
+        # what a step reads
+        self.starts = ints(range(0, n * nodes + 1, nodes))
+        self.parents, self.tokens, self.chosen = (torch.zeros(n * nodes, dtype=torch.int32, device=DEV) for _ in range(3))
+        self.k, self.v = ([self.random(n * nodes, kv) for _ in range(layers)] for _ in range(2))
+        self.q = [self.random(n * nodes, heads) for _ in range(layers)]
+
+    def add(self, layer, k, v, counts, pick=None):
+        at = 0
+        hk, hv = held(floats(k)), held(floats(v))
+        for i, c in enumerate(counts):
+            which = slice(at, at + c) if pick is None else [at + j for j in pick[i]]
+            a, b = self.rows[layer][i]
+            self.rows[layer][i] = (np.concatenate([a, hk[which]]), np.concatenate([b, hv[which]]))
+            at += c
+
+    def draft(self):
+        self.drafts = [random_tree(self.rng, self.nodes) for _ in range(self.n)]
+        tokens = [[int(x) for x in self.rng.integers(0, 6, self.nodes)] for _ in range(self.n)]
+        chosen = [[int(x) for x in self.rng.integers(0, 6, self.nodes)] for _ in range(self.n)]
+        for dst, src in ((self.parents, self.drafts), (self.tokens, tokens), (self.chosen, chosen)):
+            dst.copy_(ints(sum(src, [])))
+        self.want = [walked(*x) for x in zip(self.drafts, tokens, chosen)]
+        for layer in range(self.layers):
+            for t, heads in ((self.k[layer], self.kv), (self.v[layer], self.kv), (self.q[layer], self.heads)):
+                t.copy_(self.random(len(t), heads))
+
+    def step(self):
+        c, args = self.cache, (self.seqs, self.starts, self.nodes)
+        c.extend(self.seqs, self.starts)
+        tree, positions = c.tree(self.parents, *args)
+        out = []
+        for layer in range(self.layers):
+            c.write(layer, self.k[layer], self.v[layer], *args)
+            out.append(c.attend(layer, self.q[layer], *args, tree=tree))
+        path, kept, following = c.walk(self.parents, self.tokens, self.chosen, self.starts, self.nodes)
+        c.keep(path, kept, *args)
+        return positions, out, path, kept, following
+
+    def check(self, got):
+        positions, out, path, kept, following = got
+        torch.cuda.synchronize()
+        assert self.cache.poll_error() == 0
+        seen = [ancestors(p) for p in self.drafts]
+        base = [len(k) for k, _ in self.rows[0]]
+        assert positions.tolist() == [b + len(s) - 1 for b, item in zip(base, seen) for s in item]
+        assert kept.tolist() == [len(w[0]) for w in self.want] and following.tolist() == [w[1] for w in self.want]
+        for layer in range(self.layers):
+            hk, hv, q = held(floats(self.k[layer])), held(floats(self.v[layer])), floats(self.q[layer]).astype(np.float64)
+            for i in range(self.n):
+                rows = slice(i * self.nodes, (i + 1) * self.nodes)
+                k, v = (np.concatenate([a, b[rows]]) for a, b in zip(self.rows[layer][i], (hk, hv)))
+                check_attention(out[layer][rows], None, plain(q[rows], k, v, self.heads // self.kv, self.dim ** -0.5, sight(len(k), self.nodes, seen=seen[i])), 2.0 ** -9)
+            self.add(layer, self.k[layer], self.v[layer], [self.nodes] * self.n, [w[0] for w in self.want])
+        assert self.cache.lengths[self.seqs.long()].tolist() == [len(k) for k, _ in self.rows[0]]
+        assert self.cache.free_pages == self.n * 8 - sum(-(-len(k) // 32) for k, _ in self.rows[0])
+
+    def check_rows(self):
+        lengths = [len(k) for k, _ in self.rows[0]]
+        for layer in range(self.layers):
+            got = self.cache.read(layer, sum(lengths), self.seqs, starts_of(lengths), max(lengths))
+            for g, w in zip(got, zip(*self.rows[layer])):
+                w = np.concatenate(w)
+                assert np.all(np.abs(g.cpu().numpy() - w) <= np.spacing(np.abs(w).astype(np.float32)))
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(seed=1, n=3, heads=12, kv=12, dim=96, layers=1, nodes=20), dict(seed=2, n=2, heads=4, kv=1, dim=128, nodes=33)])
+def test_drafted_steps(kw):
+    s = Steps(**kw)
+    for turn in range(5):
+        print(f"[case] step {turn}", flush=True)
+        s.draft()
+        s.check(s.step())
+    s.check_rows()
+
+
+def test_recorded_steps():
+    s = Steps(seed=3)
+    s.draft()
+    s.check(s.step())
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = s.step()
+    for turn in range(5):
+        print(f"[case] replay {turn}", flush=True)
+        s.draft()
+        g.replay()
+        s.check(got)
+        if turn == 2:  # a step that is not recorded in between
+            s.draft()
+            s.check(s.step())
+    s.check_rows()
+
+
+def test_steps_on_another_stream():
+    s = Steps(seed=4)
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    for turn in range(3):
+        s.draft()
+        torch.cuda.synchronize()
+        c, args = s.cache, (s.seqs, s.starts, s.nodes)
+        c.extend(s.seqs, s.starts, stream=a)
+        tree, positions = c.tree(s.parents, *args, stream=b)
+        out = []
+        for layer in range(s.layers):
+            c.write(layer, s.k[layer], s.v[layer], *args, stream=a)
+            out.append(c.attend(layer, s.q[layer], *args, tree=tree, stream=b))
+        path, kept, following = c.walk(s.parents, s.tokens, s.chosen, s.starts, s.nodes, stream=a)
+        c.keep(path, kept, *args, stream=b)
+        s.check((positions, out, path, kept, following))
+    s.check_rows()
+
+
+# ------------------------------------------------------------------ refusals
+def test_refusals():
+    c = Cache(2, 64, page_tokens=32, pages=60, max_seqs=4, device=DEV)
+    c.extend(starts=ints([0, 1100, 1105]))
+    q = torch.zeros((6, 4, 64), device=DEV).half()
+    st, ok = ints([0, 3, 6]), torch.ones((6, 1), dtype=torch.int32, device=DEV)
+    for kw in (dict(sinks=4), dict(sinks=-1, window=5), dict(tree=ok, causal=False), dict(tree=torch.ones((6, 33), dtype=torch.int32, device=DEV))):
+        with pytest.raises(rtams.RtamsError):
+            c.attend(0, q, starts=st, max_new=3, **kw)
+    for bad in (ok[:, :0], ok[:5], ok.long(), ok.cpu(), ok.flatten(), torch.ones((6, 2), dtype=torch.int32, device=DEV)[:, :1]):
+        with pytest.raises(ValueError):
+            c.attend(0, q, starts=st, max_new=3, tree=bad)
+    q = torch.zeros((1030, 2, 64), device=DEV).half()
+    for words in (32, 33):
+        with pytest.raises(rtams.RtamsError):
+            c.attend(0, q, starts=ints([0, 1030]), max_new=1030, tree=torch.ones((1030, words), dtype=torch.int32, device=DEV))
+    many = ints([-1] + list(range(1029)))
+    for call in (lambda: c.tree(many, starts=ints([0, 1030]), max_new=1030), lambda: c.walk(many, many, many, ints([0, 1030]), 1030),
+                 lambda: c.keep(many, ints([1]), starts=ints([0, 1030]), max_new=1030)):
+        with pytest.raises(rtams.RtamsError):
+            call()
+    p = ints([-1, 0])
+    for call in (lambda: c.tree(p.long()), lambda: c.tree(p, starts=ints([0, 2])), lambda: c.walk(p, p[:1], p), lambda: c.walk(p, p, p.cpu()), lambda: c.keep(p, p[:1]),
+                 lambda: c.keep(p, p.float()), lambda: c.tree(p[None])):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(ValueError):
+        c.attend(0, torch.zeros((2, 2, 64), device=DEV).half().requires_grad_(), tree=torch.ones((2, 1), dtype=torch.int32, device=DEV))
+    assert c.poll_error() == 0
+    # calls without rows
+    empty = ints([])
+    assert c.attend(0, q[:0], starts=ints([0, 0]), max_new=1, tree=torch.ones((0, 1), dtype=torch.int32, device=DEV)).shape[0] == 0
+    tree, positions = c.tree(empty, starts=ints([0, 0]), max_new=1)
+    path, kept, following = c.walk(empty, empty, empty, ints([0, 0, 0]), 1)
+    torch.cuda.synchronize()
+    assert tree.shape[0] == 0 and positions.shape[0] == 0 and kept.tolist() == [0, 0] and following.tolist() == [-1, -1]
+    c.keep(empty, ints([0]), starts=ints([0, 0]), max_new=1)
+    assert c.poll_error() == 0 and c.lengths.tolist() == [1100, 5, 0, 0]
