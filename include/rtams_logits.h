@@ -39,7 +39,7 @@ typedef struct rtams_logits_query {
   size_t scratch_bytes;
 } rtams_logits_query;
 
-/* Scratch that a call needs (d_* ignored): 0 where rows are many.  (size_t)-1 on bad arguments. */
+/* Scratch that a call needs (it goes by the alignment of d_logits too): 0 where rows are many.  (size_t)-1 on bad arguments. */
 size_t rtams_logits_scratch_bytes_for(const rtams_logits_query *q);
 
 int rtams_logits_score(const rtams_logits_query *q, void *hip_stream);

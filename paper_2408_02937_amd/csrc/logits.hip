@@ -1,15 +1,16 @@
 // Log probabilities of given tokens, entropy and the most likely tokens of rows of logits (include/rtams_logits.h).
 //
-//   S = sum 2^(c (x - m)),  T = sum 2^(c (x - m)) c (x - m),  c = scale * log2 e, m the largest so far
-//   lse = scale m + ln 2 log2 S,  entropy = ln 2 (log2 S - T / S),  log probability = scale (x - m) - ln 2 log2 S
+//   1 + R = sum 2^(c (x - m)),  T = sum 2^(c (x - m)) c (x - m),  c = scale * log2 e, m the row's largest, whose own 1 is not in R
+//   lse = scale m + log(1 + R),  entropy = log(1 + R) - ln 2 T / (1 + R),  log probability = scale (x - m) - log(1 + R)
 //
-// (Differences are taken first: rows masked with the type's lowest number have that as their largest, and c times it is none.)
+// (Of a peaked row R is far below 1, and log(1 + R) and the entropy are as exact as R.)
 //
 // Bound by reading the logits once.  A workgroup takes a row, or where rows are few a piece of one, in panels that its lanes hold in registers, 256
-// bytes each: all of a panel's loads go out before the first is needed, and its largest is known before the first power, so that sums are scaled
+// bytes each: all of a panel's loads go out before the first is needed, and a lane's largest is known before its first power, so that sums are scaled
 // once a panel.  The most likely tokens: of the first panel the k-th largest of the lanes' largest is a bound that the k largest of all reach, and few
-// others do; what reaches it goes to LDS and is ranked there.  Later panels are held against the k-th so far.  Where too many reach the
-// bound (one lane has them all, or they are equal) it is found by bisection, and of those equal to it the lowest tokens are counted off.
+// others do; the lanes that have some are listed, all lanes look through their vectors, and what reaches the bound goes to LDS and is ranked there.  Later
+// panels are held against the k-th so far.  Where too many reach the bound (one lane has them all, or they are equal) it is found by bisection, and of
+// those equal to it the lowest tokens are counted off.
 #include "../../include/rtams_logits.h"
 
 #include "host.h"
@@ -79,47 +80,50 @@ __device__ inline float unordered(uint32_t u) {
 __device__ inline uint64_t key_of(float x, int token) { return (uint64_t)ordered(x) << 32 | (uint32_t)~token; }
 
 struct Sums {
-  float m, s, t;  // largest, as it is; the sums relative to it
+  float m, s, t;  // of a lane: largest, as it is; the sums relative to it.  Of lanes together: s is R, or -1 where there are no logits
 };
 
-// Sums relative to another largest, which is no smaller.
+// A lane's sums relative to another largest, which is no smaller.
 __device__ inline void move_to(Sums &a, float m, float c) {
-  if (a.m == m) return;
   const float by = a.m == -INFINITY ? kFar : (a.m - m) * c, shrink = __builtin_amdgcn_exp2f(by);
   a.t = shrink * fmaf(a.s, fmaxf(by, kFar), a.t);
   a.s *= shrink;
   a.m = m;
 }
 
-__device__ inline void join(Sums &a, Sums b, float c) {
-  const float m = fmaxf(a.m, b.m);
-  move_to(a, m, c);
-  move_to(b, m, c);
-  a.s += b.s;
-  a.t += b.t;
+__device__ inline float wave_sum(float x) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
+  return x;
+}
+
+__device__ inline float wave_largest(float x) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) x = fmaxf(x, __shfl_xor(x, o));
+  return x;
 }
 
 struct Shared {
   uint64_t best[kMostTop + kRoom];  // the best so far, then what is ranked with them
   uint64_t sorted[kMostTop];
-  uint32_t most[kLanes];
+  alignas(16) uint32_t most[kLanes];
+  uint16_t listed[kLanes];          // lanes whose vectors are looked through
   uint32_t waves[kWaves];
-  Sums sums[kWaves];
-  uint32_t count, have;
+  float largest[kWaves], sums[kWaves], weighted[kWaves], rest;
+  uint32_t count, lanes, near, have;
   float bound;
 };
 
-// The numbers of a row, one workgroup or wavefront of `lanes` lanes.
+// The numbers of a row, by `lanes` lanes.
 template <int TYPE>
 __device__ void put_row(const LogitsDev &q, int64_t row, const Sums &a, const uint64_t *best, int have, int lane, int lanes) {
-  constexpr float kLn2 = 0.6931471805599453f;
-  const bool none = a.m == -INFINITY && a.s == 0.0f, wrong = !(a.s >= 0.0f) || a.m == INFINITY;
-  const float log_s = __builtin_amdgcn_logf(a.s), nan = __uint_as_float(0x7fc00000u);
+  const bool wrong = a.s != a.s, none = !wrong && a.m == -INFINITY;
+  const float log_s = log1pf(a.s), nan = __uint_as_float(0x7fc00000u);
   if (lane == 0) {
-    if (q.lse) q.lse[row] = wrong ? nan : none ? -INFINITY : fmaf(a.m, q.scale, kLn2 * log_s);
-    if (q.entropy) q.entropy[row] = wrong ? nan : none ? 0.0f : kLn2 * (log_s - a.t / a.s);
+    if (q.lse) q.lse[row] = wrong ? nan : none ? -INFINITY : fmaf(a.m, q.scale, log_s);
+    if (q.entropy) q.entropy[row] = wrong ? nan : none ? 0.0f : fmaf(-0.6931471805599453f, a.t / (1.0f + a.s), log_s);
   }
-  const auto log_probability = [&](float x) { return wrong ? nan : x == -INFINITY ? -INFINITY : fmaf(x - a.m, q.scale, -kLn2 * log_s); };
+  const auto log_probability = [&](float x) { return wrong ? nan : x == -INFINITY ? -INFINITY : fmaf(x - a.m, q.scale, -log_s); };
   const char *x = static_cast<const char *>(q.logits) + row * q.row_stride * (TYPE == RTAMS_TYPE_F32 ? 4 : 2);
   for (int i = lane; i < q.tokens; i += lanes) {
     const int t = q.given[row * q.tokens + i];
@@ -163,6 +167,7 @@ __device__ inline void rank(int n, int top, Shared &sh) {
   for (int i = threadIdx.x; i < n; i += kLanes) {
     const uint64_t mine = sh.best[i];
     int above = 0;
+#pragma unroll 8
     for (int j = 0; j < n; ++j) above += sh.best[j] > mine;
     if (above < top) sh.sorted[above] = mine;
   }
@@ -177,17 +182,65 @@ __device__ inline void rank(int n, int top, Shared &sh) {
   __syncthreads();
 }
 
-// Takes a panel's most likely tokens to those so far.  first: token of the lane's first logit; most: the lane's largest.  (Few lanes look at their
-// logits again, most of them once in a row: they read them again.  Out of registers every look is 128 steps of code, and registers spill.)
+// Takes a panel's most likely tokens to those so far.  panel: token of the panel's first logit; most: the lane's largest.  (Logits are read again: out of
+// registers every look is 128 steps of code, and registers spill.)
 template <int TYPE>
-__device__ void take_best(const char *x, int vocab, int first, float most, int top, Shared &sh) {
+__device__ void take_best(const char *x, int vocab, int panel, float most, int top, Shared &sh) {
   constexpr int E = each_of<TYPE>();
-  if (!__syncthreads_or(most > sh.bound)) return;
   const float bound = sh.bound;
+  const int lanes = __syncthreads_count(most > bound);
+  if (!lanes) return;
   const int have = sh.have;
+  // Those that reach `least` go behind the best so far, as far as there is room; how many they are.
+  const auto collect = [&](float least) {
+    if (threadIdx.x == 0) sh.count = sh.lanes = 0;
+    __syncthreads();
+    if (most >= least) sh.listed[atomicAdd(&sh.lanes, 1u)] = (uint16_t)threadIdx.x;
+    __syncthreads();
+    const uint32_t all = sh.lanes * kVectors;
+    for (uint32_t u = threadIdx.x; u < all; u += kLanes) {
+      const int at = panel + ((int)(u % kVectors) * kLanes + sh.listed[u / kVectors]) * E;
+      const uint4 raw = load_vector<TYPE>(x, at, vocab);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float l = logit<TYPE>(raw, e);
+        if (l >= least) {
+          const uint32_t slot = atomicAdd(&sh.count, 1u);
+          if (slot < kRoom) sh.best[have + slot] = key_of(l, at + e);
+        }
+      }
+    }
+    __syncthreads();
+    return sh.count;
+  };
+  // The top-th largest of the lanes' largest.
+  const auto near = [&]() {
+    const uint32_t mine = most > bound ? ordered(most) : 0;
+    sh.most[threadIdx.x] = mine;
+    if (threadIdx.x == 0) sh.near = ~0u;
+    __syncthreads();
+    int above = 0;
+#pragma unroll 8
+    for (int j = 0; j < kLanes / 4; ++j) {
+      const uint4 y = reinterpret_cast<const uint4 *>(sh.most)[j];
+      above += (int)(y.x > mine) + (int)(y.y > mine) + (int)(y.z > mine) + (int)(y.w > mine);
+    }
+    if (mine && above < top) atomicMin(&sh.near, mine);
+    __syncthreads();
+    return unordered(sh.near);
+  };
+  float from = unordered(ordered(bound) + 1);  // the least that exceeds it (of -inf the least number)
+  if (have < top && lanes >= top) from = near();
+  uint32_t all = collect(from);
+  if (all > kRoom && have == top && lanes >= top) {
+    from = near();
+    all = collect(from);
+  }
+  if (all <= kRoom) return rank(have + (int)all, top, sh);
+  const int first = panel + (int)threadIdx.x * E;
   const auto each = [&](float least, auto f) {  // f(token, logit) in the order of the lane's tokens
     if (!(most >= least)) return;
-#pragma unroll 2
+#pragma unroll 1
     for (int v = 0; v < kVectors; ++v) {
       const int at = first + v * kLanes * E;
       const uint4 raw = load_vector<TYPE>(x, at, vocab);
@@ -211,25 +264,7 @@ __device__ void take_best(const char *x, int vocab, int first, float most, int t
     if (n) each(least, [&](int token, float l) { sh.best[at++] = key_of(l, token); });
     __syncthreads();
   };
-  float from = unordered(ordered(bound) + 1);  // the least that exceeds it (of -inf the least number)
-  uint32_t mine = 0, all = kRoom + 1;
-  if (have == top) all = reaching(from, &mine);
-  if (all > kRoom) {
-    // the top-th largest of the lanes' largest
-    const uint32_t largest = most > bound ? ordered(most) : 0;
-    sh.most[threadIdx.x] = largest;
-    __syncthreads();
-    int above = 0;
-    for (int j = 0; j < kLanes; ++j) above += sh.most[j] > largest || (sh.most[j] == largest && j < (int)threadIdx.x);
-    if (above == top - 1) sh.count = largest;
-    __syncthreads();
-    if (sh.count) from = unordered(sh.count);
-    all = reaching(from, &mine);
-  }
-  if (all <= kRoom) {
-    append(from, mine);
-    return rank(have + (int)all, top, sh);
-  }
+  uint32_t mine = 0;
   // the top-th largest, exactly: the highest that as many reach
   uint32_t low = ordered(from), high = ordered(INFINITY);
   while (low < high) {
@@ -242,6 +277,7 @@ __device__ void take_best(const char *x, int vocab, int first, float most, int t
   all = reaching(over, &mine);
   append(over, mine);
   uint32_t filled = have + all, need = top - all;
+#pragma unroll 1
   for (int v = 0; v < kVectors && need; ++v) {  // in the order of the tokens
     const int at = first + v * kLanes * E;
     const uint4 raw = load_vector<TYPE>(x, at, vocab);
@@ -271,115 +307,222 @@ __device__ void take_best(const char *x, int vocab, int first, float most, int t
   rank((int)filled, top, sh);
 }
 
+// A lane's largest logit.
+template <int TYPE>
+__device__ __forceinline__ float largest_of(uint4 (&raw)[kVectors]) {
+  if constexpr (TYPE == RTAMS_TYPE_F32) {
+    float most = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < kVectors; ++v)
+      most = fmaxf(fmaxf(fmaxf(most, __uint_as_float(raw[v].x)), __uint_as_float(raw[v].y)), fmaxf(__uint_as_float(raw[v].z), __uint_as_float(raw[v].w)));
+    return most;
+  } else if constexpr (TYPE == RTAMS_TYPE_F16) {
+    typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+    half2v most = {(_Float16)-INFINITY, (_Float16)-INFINITY};
+#pragma unroll
+    for (int v = 0; v < kVectors; ++v) {
+      const uint32_t w[4] = {raw[v].x, raw[v].y, raw[v].z, raw[v].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) most = __builtin_elementwise_max(most, __builtin_bit_cast(half2v, w[j]));
+    }
+    return fmaxf((float)most[0], (float)most[1]);
+  } else {
+    // as whole numbers two at a time: the largest of them if one is not negative, of negative numbers the least
+    typedef int16_t short2v __attribute__((ext_vector_type(2)));
+    short2v most = {-32768, -32768}, least = {32767, 32767};
+#pragma unroll
+    for (int v = 0; v < kVectors; ++v) {
+      const uint32_t w[4] = {raw[v].x, raw[v].y, raw[v].z, raw[v].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        most = __builtin_elementwise_max(most, __builtin_bit_cast(short2v, w[j]));
+        least = __builtin_elementwise_min(least, __builtin_bit_cast(short2v, w[j]));
+      }
+    }
+    const int high = max(most[0], most[1]), low = min(least[0], least[1]);
+    return __uint_as_float((uint32_t)(uint16_t)(high >= 0 ? high : low) << 16);
+  }
+}
+
 template <int TYPE>
 __global__ __launch_bounds__(kLanes, 4) void k_logits(LogitsDev q, int64_t first_unit) {
   constexpr int E = each_of<TYPE>(), kPanel = kLanes * kVectors * E, kSize = 16 / E;
+  constexpr uint32_t kNone = TYPE == RTAMS_TYPE_F32 ? 0xff800000u : TYPE == RTAMS_TYPE_BF16 ? 0xff80ff80u : 0xfc00fc00u;  // -inf
   __shared__ Shared sh;
   const int64_t unit = first_unit + blockIdx.x, row = unit / q.pieces;
   const int piece = (int)(unit % q.pieces), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const char *const x = static_cast<const char *>(q.logits) + row * q.row_stride * kSize;
-  // vectors begin at whole 16 bytes: the first may begin in front of the row
+  // vectors lie at whole 16 bytes: the first may begin in front of the row
   const int ahead = (int)(((uintptr_t)x & 15) / kSize);
-  const char *const x16 = x - ahead * kSize;
   if (threadIdx.x == 0) {
     sh.have = 0;
     sh.bound = -INFINITY;
   }
   Sums a{-INFINITY, 0.0f, 0.0f};
+  const int panel0 = piece * q.panels * kPanel - ahead;  // (below 2^30 and a panel)
   for (int p = 0; p < q.panels; ++p) {
-    const int64_t begin = ((int64_t)piece * q.panels + p) * kPanel;  // counted from x16
-    if (begin >= (int64_t)q.vocab + ahead) break;
-    const int first = (int)(begin - ahead) + (int)threadIdx.x * E;  // token of this lane's first logit
+    const int panel = panel0 + p * kPanel, first = panel + (int)threadIdx.x * E;  // tokens of the panel's first logit and of the lane's
+    if (panel >= q.vocab) break;
     uint4 raw[kVectors];
-    if (first - (int)threadIdx.x * E >= 0 && begin - ahead + kPanel <= q.vocab) {
+    const char *const from = x + (int64_t)panel * kSize;
+    const uint32_t own = threadIdx.x * 16;
+    if (panel >= 0 && panel + kPanel <= q.vocab) {
 #pragma unroll
-      for (int v = 0; v < kVectors; ++v) raw[v] = *reinterpret_cast<const uint4 *>(x16 + begin * kSize + (v * kLanes + threadIdx.x) * 16);
-    } else {
+      for (int v = 0; v < kVectors; ++v) raw[v] = *reinterpret_cast<const uint4 *>(from + v * kLanes * 16 + own);
+    } else {  // whole vectors, then those that begin in front of the row or end behind it
 #pragma unroll
       for (int v = 0; v < kVectors; ++v) {
-        raw[v] = load_vector<TYPE>(x, first + v * kLanes * E, q.vocab);
-        __builtin_amdgcn_sched_barrier(0);
+        const int at = first + v * kLanes * E;
+        raw[v] = make_uint4(kNone, kNone, kNone, kNone);
+        if (at >= 0 && at + E <= q.vocab) raw[v] = *reinterpret_cast<const uint4 *>(from + v * kLanes * 16 + own);
+      }
+      if (first < 0) raw[0] = load_vector<TYPE>(x, first, q.vocab);
+      const int last = (q.vocab - panel) / E;  // the panel's vector that the row's end is in
+      if (last % kLanes == (int)threadIdx.x && (q.vocab - panel) % E && last < kVectors * kLanes) {
+        const uint4 end = load_vector<TYPE>(x, panel + last * E, q.vocab);
+#pragma unroll
+        for (int v = 0; v < kVectors; ++v)
+          if (v == last / kLanes) raw[v] = end;
       }
     }
-    // (one vector after the other: registers hold the logits as they came, not all of them turned into 32 bits)
-    const auto each = [&](auto f) {
+    const float most = largest_of<TYPE>(raw);
+    move_to(a, fmaxf(a.m, most), q.c);
+    const float m = a.m == -INFINITY ? 0.0f : a.m, mc = m * q.c;
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, t[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    // (NaN, and +inf less +inf, are NaN in the sums; -inf is 0 in both.  One vector after the other: registers hold the logits as they came, not
+    // all of them turned into 32 bits.)
+    const auto add_up = [&](auto power) {
 #pragma unroll
       for (int v = 0; v < kVectors; ++v) {
         asm("" : "+v"(raw[v].x), "+v"(raw[v].y), "+v"(raw[v].z), "+v"(raw[v].w));
 #pragma unroll
-        for (int e = 0; e < E; ++e) f(e, logit<TYPE>(raw[v], e));
+        for (int e = 0; e < E; ++e) {
+          const float z = power(logit<TYPE>(raw[v], e)), y = __builtin_amdgcn_exp2f(z);
+          s[e % 4] += y;
+          t[e % 4] = fmaf(y, fmaxf(z, kFar), t[e % 4]);
+        }
         __builtin_amdgcn_sched_barrier(0);
       }
     };
-    float most = -INFINITY;
-    each([&](int, float l) { most = fmaxf(most, l); });
-    move_to(a, fmaxf(a.m, most), q.c);
-    const float m = a.m == -INFINITY ? 0.0f : a.m;
-    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, t[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    each([&](int e, float l) {
-      // (NaN, and +inf less +inf, are NaN in the sums; -inf is 0 in both)
-      const float z = (l - m) * q.c, y = __builtin_amdgcn_exp2f(z);
-      s[e % 4] += y;
-      t[e % 4] = fmaf(y, fmaxf(z, kFar), t[e % 4]);
-    });
-    a.s += (s[0] + s[1]) + (s[2] + s[3]);
-    a.t += (t[0] + t[1]) + (t[2] + t[3]);
+    float off = 0.0f;
+    if (!__any(!(fabsf(mc) < 1048576.0f))) {
+      add_up([&](float l) { return fmaf(l, q.c, -mc); });
+      off = fmaf(m, q.c, -mc);  // what the product's rounding left in every power
+    } else {  // (masks of the type's lowest number: c times it may be none, differences come first)
+      add_up([&](float l) { return (l - m) * q.c; });
+    }
+    const float by = __builtin_amdgcn_exp2f(-off), sum = (s[0] + s[1]) + (s[2] + s[3]), weighted = (t[0] + t[1]) + (t[2] + t[3]);
+    a.s = fmaf(sum, by, a.s);
+    a.t = fmaf(fmaf(-off, sum, weighted), by, a.t);
     if (q.top) {
       if (p == 0) __syncthreads();
-      take_best<TYPE>(x, q.vocab, first, most, q.top, sh);
+      take_best<TYPE>(x, q.vocab, panel, most, q.top, sh);
     }
   }
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) join(a, Sums{__shfl_xor(a.m, o), __shfl_xor(a.s, o), __shfl_xor(a.t, o)}, q.c);
-  if (lane == 0) sh.sums[wave] = a;
+  // The lanes' sums, without the 1 of the first that has the largest.
+  float m = wave_largest(a.m);
+  if (lane == 0) sh.largest[wave] = m;
   __syncthreads();
-  a = sh.sums[0];
-  for (int w = 1; w < kWaves; ++w) join(a, sh.sums[w], q.c);
+  m = fmaxf(fmaxf(sh.largest[0], sh.largest[1]), fmaxf(sh.largest[2], sh.largest[3]));
+  const uint64_t who = __ballot(a.m == m);
+  int owner = kLanes;
+  for (int w = kWaves - 1; w >= 0; --w)
+    if (sh.largest[w] == m) owner = w * 64;
+  const bool mine = wave * 64 == owner && lane == __ffsll((unsigned long long)who) - 1;
+  move_to(a, m, q.c);
+  const auto together = [&](float s) {
+    const float ws = wave_sum(s), wt = wave_sum(a.t);
+    __syncthreads();
+    if (lane == 0) {
+      sh.sums[wave] = ws;
+      sh.weighted[wave] = wt;
+    }
+    __syncthreads();
+    return Sums{m, (sh.sums[0] + sh.sums[1]) + (sh.sums[2] + sh.sums[3]), (sh.weighted[0] + sh.weighted[1]) + (sh.weighted[2] + sh.weighted[3])};
+  };
+  Sums all = together(mine ? a.s - 1.0f : a.s);
+  if (all.s >= 0.0f && all.s < 0.0625f) {
+    // A peaked row: what that lane has beside the 1 is summed once more, by the first wavefront.
+    if (mine) sh.listed[0] = (uint16_t)threadIdx.x;
+    __syncthreads();
+    if (wave == 0) {
+      float rest = 0.0f;
+      for (int u = lane; u < q.panels * kVectors; u += 64) {
+        const int at = panel0 + (u * kLanes + sh.listed[0]) * E;
+        if (at >= q.vocab) break;
+        const uint4 raw = load_vector<TYPE>(x, at, q.vocab);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float l = logit<TYPE>(raw, e);
+          rest += l == m ? 0.0f : __builtin_amdgcn_exp2f((l - m) * q.c);  // (a second one would make R 1)
+        }
+      }
+      rest = wave_sum(rest);
+      if (lane == 0) sh.rest = rest;
+    }
+    __syncthreads();
+    all = together(mine ? sh.rest : a.s);
+  }
   const int have = q.top ? (int)sh.have : 0;
   if (q.pieces == 1) {
-    put_row<TYPE>(q, row, a, sh.sorted, have, threadIdx.x, kLanes);
+    put_row<TYPE>(q, row, all, sh.sorted, have, threadIdx.x, kLanes);
   } else {
-    if (threadIdx.x == 0) q.part[unit] = make_float4(a.m, a.s, a.t, 0.0f);
+    if (threadIdx.x == 0) q.part[unit] = make_float4(all.m, all.s, all.t, 0.0f);
     for (int i = threadIdx.x; i < q.top; i += kLanes) q.part_best[unit * q.top + i] = i < have ? sh.sorted[i] : 0;
   }
 }
 
-// A wavefront joins the pieces of a row: sums, and the heads of the pieces' lists, which are in order.
+// Joins the pieces of a row: sums, and the pieces' lists, which are in order.  A token's place is how many of each list are in front of it.
 template <int TYPE>
-__global__ __launch_bounds__(64) void k_logits_join(LogitsDev q, int64_t first_row) {
-  __shared__ uint64_t best[kMostTop];
+__global__ __launch_bounds__(kLanes) void k_logits_join(LogitsDev q, int64_t first_row) {
+  __shared__ uint64_t lists[kMostPieces * kMostTop], best[kMostTop];
+  __shared__ uint32_t count;
   const int64_t row = first_row + blockIdx.x;
-  const int lane = threadIdx.x;
-  Sums a{-INFINITY, 0.0f, 0.0f};
+  const int lane = threadIdx.x & 63, n = q.pieces * q.top;
+  if (threadIdx.x == 0) count = 0;
+  for (int i = threadIdx.x; i < n; i += kLanes) lists[i] = q.part_best[row * n + i];
+  Sums a{-INFINITY, -1.0f, 0.0f};
   if (lane < q.pieces) {
     const float4 p = q.part[row * q.pieces + lane];
     a = Sums{p.x, p.y, p.z};
   }
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) join(a, Sums{__shfl_xor(a.m, o), __shfl_xor(a.s, o), __shfl_xor(a.t, o)}, q.c);
-  const uint64_t *list = q.part_best + (row * q.pieces + min(lane, q.pieces - 1)) * q.top;
-  int at = 0, have = 0;
-  uint64_t head = lane < q.pieces && q.top ? list[0] : 0;
-  for (; have < q.top; ++have) {
-    uint64_t most = head;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint64_t other = (uint64_t)__shfl_xor((unsigned long long)most, o);
-      most = other > most ? other : most;
+  const float m = wave_largest(a.m);
+  const bool mine = lane == __ffsll((unsigned long long)__ballot(a.m == m)) - 1;
+  const float rest = a.s;
+  a.s += 1.0f;
+  move_to(a, m, q.c);
+  a.s = wave_sum(mine ? rest : a.s);
+  a.t = wave_sum(a.t);
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += kLanes) {
+    const uint64_t key = lists[i];
+    if (!key) continue;
+    atomicAdd(&count, 1u);
+    int place = i % q.top;
+    for (int b = 0; b < q.pieces && place < q.top; ++b) {
+      if (b == i / q.top) continue;
+      int lo = 0, hi = q.top;
+      while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if (lists[b * q.top + mid] > key) lo = mid + 1;
+        else hi = mid;
+      }
+      place += lo;
     }
-    if (most == 0) break;
-    if (lane == 0) best[have] = most;
-    if (head == most) head = ++at < q.top ? list[at] : 0;  // (keys differ: one lane)
+    if (place < q.top) best[place] = key;
   }
   __syncthreads();
-  put_row<TYPE>(q, row, a, best, have, lane, 64);
+  put_row<TYPE>(q, row, a, best, min((int)count, q.top), threadIdx.x, kLanes);
 }
 
 constexpr int panel_of(int type) { return kLanes * kVectors * (type == RTAMS_TYPE_F32 ? 4 : 8); }
 
 // Pieces of a row, and the panels of a piece.
 void split(const rtams_logits_query *q, int *pieces, int *panels) {
-  const int64_t all = ((int64_t)q->vocab + 7 + panel_of(q->type) - 1) / panel_of(q->type);
+  // (a row that does not begin at whole 16 bytes has some logits less in its first panel)
+  const int size = q->type == RTAMS_TYPE_F32 ? 4 : 2, each = 16 / size;
+  const bool whole = (uintptr_t)q->d_logits % 16 == 0 && (q->rows == 1 || q->row_stride % each == 0);
+  const int64_t all = ((int64_t)q->vocab + (whole ? 0 : each - 1) + panel_of(q->type) - 1) / panel_of(q->type);
   int64_t want = q->rows < kSplitBelow ? (kSplitBelow + q->rows - 1) / q->rows : 1;
   if (want > kMostPieces) want = kMostPieces;
   if (want > all) want = all;
@@ -447,7 +590,7 @@ int rtams_logits_score(const rtams_logits_query *q, void *hip_stream) {
   const auto go = [&](auto kernel, auto joiner) {
     const int64_t units = q->rows * d.pieces, most = 1 << 22;
     for (int64_t at = 0; at < units; at += most) kernel<<<(uint32_t)(units - at < most ? units - at : most), kLanes, 0, s>>>(d, at);
-    if (d.pieces > 1) joiner<<<(uint32_t)q->rows, 64, 0, s>>>(d, 0);
+    if (d.pieces > 1) joiner<<<(uint32_t)q->rows, kLanes, 0, s>>>(d, 0);
   };
   switch (q->type) {
     case RTAMS_TYPE_BF16: go(k_logits<RTAMS_TYPE_BF16>, k_logits_join<RTAMS_TYPE_BF16>); break;
