@@ -44,12 +44,13 @@ struct LogitsDev {
   uint64_t *part_best;   // [rows][pieces][top]
 };
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
 template <int TYPE>
 constexpr int each_of() { return TYPE == RTAMS_TYPE_F32 ? 4 : 8; }  // logits of a vector
 
 template <int TYPE>
-__device__ inline float logit(const uint4 &v, int e) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+__device__ __forceinline__ float logit(const u32x4 &w, int e) {
   if (TYPE == RTAMS_TYPE_F32) return __uint_as_float(w[e]);
   if (TYPE == RTAMS_TYPE_BF16) return __uint_as_float(e % 2 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
   const uint16_t u = (uint16_t)(e % 2 ? w[e / 2] >> 16 : w[e / 2]);
@@ -109,14 +110,23 @@ struct Shared {
   alignas(16) uint32_t most[kLanes];
   uint16_t listed[kLanes];          // lanes whose vectors are looked through
   uint32_t waves[kWaves];
-  float largest[kWaves], sums[kWaves], weighted[kWaves], rest;
+  float largest[kWaves], sums[kWaves], weighted[kWaves];
+  float2 rest;
   uint32_t count, lanes, near, have;
   float bound;
 };
 
-// The numbers of a row, by `lanes` lanes.
+// The logit of the i-th token given for a row.
 template <int TYPE>
-__device__ void put_row(const LogitsDev &q, int64_t row, const Sums &a, const uint64_t *best, int have, int lane, int lanes) {
+__device__ inline float given_logit(const LogitsDev &q, int64_t row, int i) {
+  if (i >= q.tokens) return -INFINITY;
+  const int t = q.given[row * q.tokens + i];
+  return (uint32_t)t < (uint32_t)q.vocab ? logit_at<TYPE>(static_cast<const char *>(q.logits) + row * q.row_stride * (TYPE == RTAMS_TYPE_F32 ? 4 : 2), t) : -INFINITY;
+}
+
+// The numbers of a row, by `lanes` lanes; given: the logit of token number `lane`, asked for ahead.
+template <int TYPE>
+__device__ void put_row(const LogitsDev &q, int64_t row, const Sums &a, const uint64_t *best, int have, int lane, int lanes, float given) {
   const bool wrong = a.s != a.s, none = !wrong && a.m == -INFINITY;
   const float log_s = log1pf(a.s), nan = __uint_as_float(0x7fc00000u);
   if (lane == 0) {
@@ -124,11 +134,7 @@ __device__ void put_row(const LogitsDev &q, int64_t row, const Sums &a, const ui
     if (q.entropy) q.entropy[row] = wrong ? nan : none ? 0.0f : fmaf(-0.6931471805599453f, a.t / (1.0f + a.s), log_s);
   }
   const auto log_probability = [&](float x) { return wrong ? nan : x == -INFINITY ? -INFINITY : fmaf(x - a.m, q.scale, -log_s); };
-  const char *x = static_cast<const char *>(q.logits) + row * q.row_stride * (TYPE == RTAMS_TYPE_F32 ? 4 : 2);
-  for (int i = lane; i < q.tokens; i += lanes) {
-    const int t = q.given[row * q.tokens + i];
-    q.logprobs[row * q.tokens + i] = log_probability((uint32_t)t < (uint32_t)q.vocab ? logit_at<TYPE>(x, t) : -INFINITY);
-  }
+  for (int i = lane; i < q.tokens; i += lanes) q.logprobs[row * q.tokens + i] = log_probability(i == lane ? given : given_logit<TYPE>(q, row, i));
   for (int i = lane; i < q.top; i += lanes) {
     const bool there = i < have && !wrong;
     q.best[row * q.top + i] = there ? (int32_t)~(uint32_t)best[i] : -1;
@@ -138,10 +144,10 @@ __device__ void put_row(const LogitsDev &q, int64_t row, const Sums &a, const ui
 
 // Logits at .. at + E - 1 of a row, 16 bytes that lie at whole 16; -inf where the row has none.
 template <int TYPE>
-__device__ __forceinline__ uint4 load_vector(const char *x, int at, int vocab) {
+__device__ __forceinline__ u32x4 load_vector(const char *x, int at, int vocab) {
   constexpr int E = each_of<TYPE>(), kSize = 16 / E;
   constexpr uint32_t kNone = TYPE == RTAMS_TYPE_F32 ? 0xff800000u : TYPE == RTAMS_TYPE_BF16 ? 0xff80ff80u : 0xfc00fc00u;
-  if (at >= 0 && at + E <= vocab) return *reinterpret_cast<const uint4 *>(x + (int64_t)at * kSize);
+  if (at >= 0 && at + E <= vocab) return *reinterpret_cast<const u32x4 *>(x + (int64_t)at * kSize);
   uint32_t w[4] = {kNone, kNone, kNone, kNone};
   if (at + E > 0 && at < vocab)
 #pragma unroll
@@ -150,7 +156,7 @@ __device__ __forceinline__ uint4 load_vector(const char *x, int at, int vocab) {
         if (E == 4) w[e] = reinterpret_cast<const uint32_t *>(x)[at + e];
         else w[e / 2] = (e % 2 ? w[e / 2] & 0xffffu : w[e / 2] & 0xffff0000u) | (uint32_t)reinterpret_cast<const uint16_t *>(x)[at + e] << (e % 2 * 16);
       }
-  return make_uint4(w[0], w[1], w[2], w[3]);
+  return u32x4{w[0], w[1], w[2], w[3]};
 }
 
 // Sum over the workgroup, to every lane.
@@ -200,7 +206,7 @@ __device__ void take_best(const char *x, int vocab, int panel, float most, int t
     const uint32_t all = sh.lanes * kVectors;
     for (uint32_t u = threadIdx.x; u < all; u += kLanes) {
       const int at = panel + ((int)(u % kVectors) * kLanes + sh.listed[u / kVectors]) * E;
-      const uint4 raw = load_vector<TYPE>(x, at, vocab);
+      const u32x4 raw = load_vector<TYPE>(x, at, vocab);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const float l = logit<TYPE>(raw, e);
@@ -243,7 +249,7 @@ __device__ void take_best(const char *x, int vocab, int panel, float most, int t
 #pragma unroll 1
     for (int v = 0; v < kVectors; ++v) {
       const int at = first + v * kLanes * E;
-      const uint4 raw = load_vector<TYPE>(x, at, vocab);
+      const u32x4 raw = load_vector<TYPE>(x, at, vocab);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const float l = logit<TYPE>(raw, e);
@@ -280,7 +286,7 @@ __device__ void take_best(const char *x, int vocab, int panel, float most, int t
 #pragma unroll 1
   for (int v = 0; v < kVectors && need; ++v) {  // in the order of the tokens
     const int at = first + v * kLanes * E;
-    const uint4 raw = load_vector<TYPE>(x, at, vocab);
+    const u32x4 raw = load_vector<TYPE>(x, at, vocab);
     uint32_t n = 0;
 #pragma unroll
     for (int e = 0; e < E; ++e) n += logit<TYPE>(raw, e) == equal;
@@ -307,38 +313,37 @@ __device__ void take_best(const char *x, int vocab, int panel, float most, int t
   rank((int)filled, top, sh);
 }
 
-// A lane's largest logit.
+// A lane's largest logit, of its first `some` vectors.
 template <int TYPE>
-__device__ __forceinline__ float largest_of(uint4 (&raw)[kVectors]) {
+__device__ __forceinline__ float largest_of(const u32x4 (&raw)[kVectors], int some) {
   if constexpr (TYPE == RTAMS_TYPE_F32) {
     float most = -INFINITY;
 #pragma unroll
     for (int v = 0; v < kVectors; ++v)
-      most = fmaxf(fmaxf(fmaxf(most, __uint_as_float(raw[v].x)), __uint_as_float(raw[v].y)), fmaxf(__uint_as_float(raw[v].z), __uint_as_float(raw[v].w)));
+      if (v < some)
+        most = fmaxf(fmaxf(fmaxf(most, __uint_as_float(raw[v].x)), __uint_as_float(raw[v].y)), fmaxf(__uint_as_float(raw[v].z), __uint_as_float(raw[v].w)));
     return most;
   } else if constexpr (TYPE == RTAMS_TYPE_F16) {
     typedef _Float16 half2v __attribute__((ext_vector_type(2)));
     half2v most = {(_Float16)-INFINITY, (_Float16)-INFINITY};
 #pragma unroll
-    for (int v = 0; v < kVectors; ++v) {
-      const uint32_t w[4] = {raw[v].x, raw[v].y, raw[v].z, raw[v].w};
+    for (int v = 0; v < kVectors; ++v)
+      if (v < some)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) most = __builtin_elementwise_max(most, __builtin_bit_cast(half2v, w[j]));
-    }
+        for (int j = 0; j < 4; ++j) most = __builtin_elementwise_max(most, __builtin_bit_cast(half2v, (uint32_t)raw[v][j]));
     return fmaxf((float)most[0], (float)most[1]);
   } else {
     // as whole numbers two at a time: the largest of them if one is not negative, of negative numbers the least
     typedef int16_t short2v __attribute__((ext_vector_type(2)));
     short2v most = {-32768, -32768}, least = {32767, 32767};
 #pragma unroll
-    for (int v = 0; v < kVectors; ++v) {
-      const uint32_t w[4] = {raw[v].x, raw[v].y, raw[v].z, raw[v].w};
+    for (int v = 0; v < kVectors; ++v)
+      if (v < some)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        most = __builtin_elementwise_max(most, __builtin_bit_cast(short2v, w[j]));
-        least = __builtin_elementwise_min(least, __builtin_bit_cast(short2v, w[j]));
-      }
-    }
+        for (int j = 0; j < 4; ++j) {
+          most = __builtin_elementwise_max(most, __builtin_bit_cast(short2v, (uint32_t)raw[v][j]));
+          least = __builtin_elementwise_min(least, __builtin_bit_cast(short2v, (uint32_t)raw[v][j]));
+        }
     const int high = max(most[0], most[1]), low = min(least[0], least[1]);
     return __uint_as_float((uint32_t)(uint16_t)(high >= 0 ? high : low) << 16);
   }
@@ -358,34 +363,36 @@ __global__ __launch_bounds__(kLanes, 4) void k_logits(LogitsDev q, int64_t first
     sh.have = 0;
     sh.bound = -INFINITY;
   }
+  const float given = q.pieces == 1 ? given_logit<TYPE>(q, row, threadIdx.x) : 0.0f;
   Sums a{-INFINITY, 0.0f, 0.0f};
   const int panel0 = piece * q.panels * kPanel - ahead;  // (below 2^30 and a panel)
   for (int p = 0; p < q.panels; ++p) {
     const int panel = panel0 + p * kPanel, first = panel + (int)threadIdx.x * E;  // tokens of the panel's first logit and of the lane's
     if (panel >= q.vocab) break;
-    uint4 raw[kVectors];
+    u32x4 raw[kVectors];
     const char *const from = x + (int64_t)panel * kSize;
     const uint32_t own = threadIdx.x * 16;
     if (panel >= 0 && panel + kPanel <= q.vocab) {
 #pragma unroll
-      for (int v = 0; v < kVectors; ++v) raw[v] = *reinterpret_cast<const uint4 *>(from + v * kLanes * 16 + own);
+      for (int v = 0; v < kVectors; ++v) raw[v] = *reinterpret_cast<const u32x4 *>(from + v * kLanes * 16 + own);
     } else {  // whole vectors, then those that begin in front of the row or end behind it
 #pragma unroll
       for (int v = 0; v < kVectors; ++v) {
         const int at = first + v * kLanes * E;
-        raw[v] = make_uint4(kNone, kNone, kNone, kNone);
-        if (at >= 0 && at + E <= q.vocab) raw[v] = *reinterpret_cast<const uint4 *>(from + v * kLanes * 16 + own);
+        raw[v] = u32x4{kNone, kNone, kNone, kNone};
+        if (at >= 0 && at + E <= q.vocab) raw[v] = *reinterpret_cast<const u32x4 *>(from + v * kLanes * 16 + own);
       }
       if (first < 0) raw[0] = load_vector<TYPE>(x, first, q.vocab);
       const int last = (q.vocab - panel) / E;  // the panel's vector that the row's end is in
       if (last % kLanes == (int)threadIdx.x && (q.vocab - panel) % E && last < kVectors * kLanes) {
-        const uint4 end = load_vector<TYPE>(x, panel + last * E, q.vocab);
+        const u32x4 end = load_vector<TYPE>(x, panel + last * E, q.vocab);
 #pragma unroll
         for (int v = 0; v < kVectors; ++v)
           if (v == last / kLanes) raw[v] = end;
       }
     }
-    const float most = largest_of<TYPE>(raw);
+    const int some = min(kVectors, (q.vocab - panel + kLanes * E - 1) / (kLanes * E));  // vectors that hold some: the others cost nothing
+    const float most = largest_of<TYPE>(raw, some);
     move_to(a, fmaxf(a.m, most), q.c);
     const float m = a.m == -INFINITY ? 0.0f : a.m, mc = m * q.c;
     float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, t[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -394,7 +401,8 @@ __global__ __launch_bounds__(kLanes, 4) void k_logits(LogitsDev q, int64_t first
     const auto add_up = [&](auto power) {
 #pragma unroll
       for (int v = 0; v < kVectors; ++v) {
-        asm("" : "+v"(raw[v].x), "+v"(raw[v].y), "+v"(raw[v].z), "+v"(raw[v].w));
+        if (v >= some) break;
+        asm("" : "+v"(raw[v]));
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           const float z = power(logit<TYPE>(raw[v], e)), y = __builtin_amdgcn_exp2f(z);
@@ -441,31 +449,35 @@ __global__ __launch_bounds__(kLanes, 4) void k_logits(LogitsDev q, int64_t first
     return Sums{m, (sh.sums[0] + sh.sums[1]) + (sh.sums[2] + sh.sums[3]), (sh.weighted[0] + sh.weighted[1]) + (sh.weighted[2] + sh.weighted[3])};
   };
   Sums all = together(mine ? a.s - 1.0f : a.s);
-  if (all.s >= 0.0f && all.s < 0.0625f) {
-    // A peaked row: what that lane has beside the 1 is summed once more, by the first wavefront.
+  if (all.s > -0.5f && all.s < 0.0625f) {  // (-1: no logits)
+    // A peaked row: what that lane has beside the 1, and the weighted sum, in which the largest's roundings stand, are summed once more, by the first wavefront.
     if (mine) sh.listed[0] = (uint16_t)threadIdx.x;
     __syncthreads();
     if (wave == 0) {
-      float rest = 0.0f;
+      float rest = 0.0f, weighted = 0.0f;
       for (int u = lane; u < q.panels * kVectors; u += 64) {
         const int at = panel0 + (u * kLanes + sh.listed[0]) * E;
         if (at >= q.vocab) break;
-        const uint4 raw = load_vector<TYPE>(x, at, q.vocab);
+        const u32x4 raw = load_vector<TYPE>(x, at, q.vocab);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           const float l = logit<TYPE>(raw, e);
-          rest += l == m ? 0.0f : __builtin_amdgcn_exp2f((l - m) * q.c);  // (a second one would make R 1)
+          const float z = (l - m) * q.c, y = l == m ? 0.0f : __builtin_amdgcn_exp2f(z);  // (a second one would make R 1)
+          rest += y;
+          weighted = fmaf(y, fmaxf(z, kFar), weighted);
         }
       }
       rest = wave_sum(rest);
-      if (lane == 0) sh.rest = rest;
+      weighted = wave_sum(weighted);
+      if (lane == 0) sh.rest = make_float2(rest, weighted);
     }
     __syncthreads();
-    all = together(mine ? sh.rest : a.s);
+    if (mine) a.t = sh.rest.y;
+    all = together(mine ? sh.rest.x : a.s);
   }
   const int have = q.top ? (int)sh.have : 0;
   if (q.pieces == 1) {
-    put_row<TYPE>(q, row, all, sh.sorted, have, threadIdx.x, kLanes);
+    put_row<TYPE>(q, row, all, sh.sorted, have, threadIdx.x, kLanes, given);
   } else {
     if (threadIdx.x == 0) q.part[unit] = make_float4(all.m, all.s, all.t, 0.0f);
     for (int i = threadIdx.x; i < q.top; i += kLanes) q.part_best[unit * q.top + i] = i < have ? sh.sorted[i] : 0;
@@ -479,6 +491,7 @@ __global__ __launch_bounds__(kLanes) void k_logits_join(LogitsDev q, int64_t fir
   __shared__ uint32_t count;
   const int64_t row = first_row + blockIdx.x;
   const int lane = threadIdx.x & 63, n = q.pieces * q.top;
+  const float given = given_logit<TYPE>(q, row, threadIdx.x);
   if (threadIdx.x == 0) count = 0;
   for (int i = threadIdx.x; i < n; i += kLanes) lists[i] = q.part_best[row * n + i];
   Sums a{-INFINITY, -1.0f, 0.0f};
@@ -512,7 +525,7 @@ __global__ __launch_bounds__(kLanes) void k_logits_join(LogitsDev q, int64_t fir
     if (place < q.top) best[place] = key;
   }
   __syncthreads();
-  put_row<TYPE>(q, row, a, best, min((int)count, q.top), threadIdx.x, kLanes);
+  put_row<TYPE>(q, row, a, best, min((int)count, q.top), threadIdx.x, kLanes, given);
 }
 
 constexpr int panel_of(int type) { return kLanes * kVectors * (type == RTAMS_TYPE_F32 ? 4 : 8); }

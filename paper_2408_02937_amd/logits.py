@@ -23,7 +23,8 @@ _query = struct.Struct(_FORMAT).pack  # LogitsQuery
 assert struct.calcsize(_FORMAT) == sizeof(LogitsQuery)
 _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 _TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
-_MANY = 1024  # rows: of so many or more no call takes scratch
+_MANY = 1024  # rows: of so many or more no call takes scratch,
+_ONE = 65_520  # nor of rows of so many bytes
 
 
 class Scores(NamedTuple):
@@ -48,20 +49,26 @@ def score(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, top: int 
         if not (tokens.dtype == torch.int32 and tokens.dim() in (1, 2) and tokens.shape[0] == rows and tokens.is_contiguous() and tokens.device == device):
             raise ValueError(f"tokens must be a contiguous int32 tensor [rows] or [rows][m] on {device}")
         given = tokens.shape[1] if tokens.dim() == 2 else 1
+    if top < 0 or top > 64:
+        raise ValueError("top must be in 0..64")
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            made = _outputs(rows, given, top, device)
+    else:
+        made = _outputs(rows, given, top, device)
+    lse, entropy, logprobs, top_logprobs, best = made
+    fields = (rows, logits.stride(0), vocab, _TYPES[logits.dtype], top, given, scale, logits.data_ptr(), tokens.data_ptr() if given else 0, lse.data_ptr(),
+              entropy.data_ptr(), logprobs.data_ptr() if given else 0, best.data_ptr() if top else 0, top_logprobs.data_ptr() if top else 0)
     L = lib()
-    # one tensor for all outputs of 32 bits, one for the tokens
-    with nullcontext() if stream is None else torch.cuda.stream(stream):
-        out = torch.empty(rows * (2 + given + max(top, 0)), dtype=torch.float32, device=device)
-        best = torch.empty((rows, top), dtype=torch.int32, device=device) if top > 0 else None
-        at = out.data_ptr()
-        fields = [rows, logits.stride(0), vocab, _TYPES[logits.dtype], top, given, scale, logits.data_ptr(), tokens.data_ptr() if given else 0, at, at + 4 * rows,
-                  at + 8 * rows, best.data_ptr() if top > 0 else 0, at + 4 * rows * (2 + given), 0, 0]
-        scratch = None
-        if rows < _MANY:
-            size = L.rtams_logits_scratch_bytes_for(_query(*fields))
-            if 0 < size < 1 << 62:
-                scratch = torch.empty(size, dtype=torch.uint8, device=device)
-                fields[-2:] = [scratch.data_ptr(), size]
+    at = size = 0
+    if rows < _MANY and vocab * logits.element_size() > _ONE:
+        size = L.rtams_logits_scratch_bytes_for(_query(*fields, 0, 0))
+        if 0 < size < 1 << 62:
+            with nullcontext() if stream is None else torch.cuda.stream(stream):
+                scratch = torch.empty(size, dtype=torch.uint8, device=device)  # (the allocator hands it to later work of this stream only)
+            at = scratch.data_ptr()
+        else:
+            size = 0
     if stream is None:
         pointer = _current_stream(device.index)
     else:
@@ -69,12 +76,25 @@ def score(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, top: int 
         for t in (logits, tokens):
             if t is not None:
                 t.record_stream(stream)
-        for t in (out, best):
+        now = torch.cuda.current_stream(device)
+        for t in (lse, best):  # (the others are views of the first)
             if t is not None:
-                t.record_stream(torch.cuda.current_stream(device))
-    with nullcontext() if torch.cuda.current_device() == device.index else torch.cuda.device(device):
-        _chk(L.rtams_logits_score(_query(*fields), pointer), "rtams_logits_score")
-    logprobs = None
-    if tokens is not None:
-        logprobs = out[2 * rows:(2 + given) * rows].view(tokens.shape)
-    return Scores(out[:rows], out[rows:2 * rows], logprobs, best, out[(2 + given) * rows:].view(rows, top) if top > 0 else None)
+                t.record_stream(now)
+    query = _query(*fields, at, size)
+    if torch.cuda.current_device() == device.index:
+        _chk(L.rtams_logits_score(query, pointer), "rtams_logits_score")
+    else:
+        with torch.cuda.device(device):
+            _chk(L.rtams_logits_score(query, pointer), "rtams_logits_score")
+    if tokens is not None and logprobs.shape != tokens.shape:
+        logprobs = logprobs.view(tokens.shape)
+    return Scores(lse, entropy, logprobs if tokens is not None else None, best, top_logprobs)
+
+
+def _outputs(rows: int, given: int, top: int, device):
+    """(lse, entropy, logprobs, top_logprobs, top): views of one tensor, and one for the tokens."""
+    out = torch.empty(rows * (2 + given + top), dtype=torch.float32, device=device)
+    lse, entropy, logprobs, top_logprobs = out.split_with_sizes((rows, rows, rows * given, rows * top))
+    if top == 0:
+        return lse, entropy, logprobs, None, None
+    return lse, entropy, logprobs, top_logprobs.view(rows, top), torch.empty((rows, top), dtype=torch.int32, device=device)

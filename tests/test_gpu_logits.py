@@ -184,6 +184,24 @@ def test_peaked_and_flat_rows():
         check(some(3, 50_000, dtype, seed=12) + 500.0, tokens_for(3, 50_000, 2), 8)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,vocab", [(1, 4_096), (2, 131_072), (1100, 9_000)])
+def test_peaked_rows_keep_their_entropy(dtype, rows, vocab):
+    """One token nearly certain: what is left is 2^-10 to 2^-40, and the entropy is as exact as that, relative to itself."""
+    x = some(rows, vocab, dtype, seed=13, width=0.5)
+    at = tokens_for(rows, vocab, 1, seed=14)
+    gaps = torch.linspace(17.0, 36.0, rows, device=DEV) if rows > 1 else torch.tensor([24.0], device=DEV)
+    x[torch.arange(rows, device=DEV), at.long()] = gaps.to(dtype)
+    r = check(x, at, 3)
+    f = x.double()
+    z = f - f.amax(-1, keepdim=True)
+    rest = torch.where(z < 0, z.exp(), torch.zeros_like(z)).sum(-1)
+    want = torch.log1p(rest) - (z.exp() * z).sum(-1) / (1.0 + rest)
+    # powers off by 3 u |z| + 4 u each, their sums by 100 u and more panels, of some 25 times the rest
+    assert ((r.entropy.double() - want).abs() <= (200 + 3 * 40 * 2) * U * want).all()
+    assert ((r.logprobs.double() + torch.log1p(rest)).abs() <= (200 + 3 * 40 * 2) * U * rest).all()
+
+
 def test_places_beyond_32_bits():
     rows, vocab, stride = 20, 5_000, 250_000_000  # halves: 10 GB
     x = torch.zeros((rows - 1) * stride + vocab, dtype=torch.float16, device=DEV).as_strided((rows, vocab), (stride, 1))
