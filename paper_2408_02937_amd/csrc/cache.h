@@ -60,6 +60,7 @@ struct CacheDev {
   float *part;        // attention: parts of rows
   float *part_ml;     // their maxima and sums
   uint32_t *arrived;  // parts of an item that are there
+  uint32_t *joins;    // of a head's row tile: how many parts (upper half) and the first of them, for a launch that joins them
 };
 
 struct CacheRows {  // the items of a call, and rows that lie `row_stride` elements apart

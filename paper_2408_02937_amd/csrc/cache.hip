@@ -163,7 +163,7 @@ size_t rtams_cache_pool_bytes_for(const rtams_cache_config *cfg, int64_t pages) 
 
 size_t rtams_cache_scratch_bytes_for(const rtams_cache_config *cfg) {
   if (!cache_config_ok(cfg, false)) return 0;
-  return up(cache_arrived_words(cfg->max_seqs, cfg->kv_heads) * 4, kAlign) + up(cache_part_ml_floats(cfg->head_dim) * 4, kAlign) +
+  return 2 * up(cache_arrived_words(cfg->max_seqs, cfg->kv_heads) * 4, kAlign) + up(cache_part_ml_floats(cfg->head_dim) * 4, kAlign) +
          up(cache_part_floats(cfg->head_dim) * 4, kAlign);
 }
 
@@ -215,6 +215,8 @@ int rtams_cache_create(const rtams_cache_config *cfg, rtams_cache **out) {
   char *q = static_cast<char *>(cfg->d_scratch);
   const size_t arrived = cache_arrived_words(cfg->max_seqs, cfg->kv_heads);
   d.arrived = reinterpret_cast<uint32_t *>(q);
+  q += up(arrived * 4, kAlign);
+  d.joins = reinterpret_cast<uint32_t *>(q);
   q += up(arrived * 4, kAlign);
   d.part_ml = reinterpret_cast<float *>(q);
   q += up(cache_part_ml_floats(cfg->head_dim) * 4, kAlign);

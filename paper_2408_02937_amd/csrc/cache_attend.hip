@@ -26,8 +26,12 @@ constexpr int kLanes = 256, kWaves = 4, kStep = kWaves * kBlockTokens;
 
 // Workgroups that a compute unit runs at once: registers decide, and from 128 channels on LDS (40 * D * 8 bytes of blocks).
 constexpr int at_once(int head_dim, int tiles) {
-  return tiles == 2 ? (head_dim == 64 ? 3 : 2) : head_dim == 64 ? 5 : head_dim == 96 ? 4 : head_dim == 128 ? 3 : 1;
+  return tiles == 4 ? (head_dim == 64 ? 2 : 1) : tiles == 2 ? (head_dim == 64 ? 3 : 2) : head_dim == 64 ? 5 : head_dim == 96 ? 4 : head_dim == 128 ? 3 : 1;
 }
+
+// Whether parts of rows are joined by a launch of their own: a row tile of 32 rows or more is too much for the last workgroup to arrive, which
+// reads its parts a few at a time.  JOIN_FIGURES
+constexpr bool joined(int tiles, bool sight) { return sight && tiles > 1; }
 
 struct Span {  // what an item asks for
   int seq, count, length, low;  // low: first position that a row of it sees, rounded down to a block (with sinks: behind them, less what they take)
@@ -181,6 +185,7 @@ struct Copies {
 template <int D, int NR, bool SIGHT>
 __device__ __forceinline__ void attend(const CacheDev &d, const CacheQuery &q, const CacheSight &g, int tiles) {
   constexpr int NJ = D / 32, NT = D / 16;
+  constexpr bool JOINED = joined(NR, SIGHT);
   extern __shared__ uint4 lds[];
   Shared<D, NR> &sh = *reinterpret_cast<Shared<D, NR> *>(lds);
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 15, b = lane >> 4;
@@ -310,9 +315,9 @@ __device__ __forceinline__ void attend(const CacheDev &d, const CacheQuery &q, c
     for (int t = 0; t < NR; ++t) {
       float top = fmaxf(fmaxf(fmaxf(sc[t][0][0], sc[t][0][1]), fmaxf(sc[t][0][2], sc[t][0][3])),
                         fmaxf(fmaxf(sc[t][1][0], sc[t][1][1]), fmaxf(sc[t][1][2], sc[t][1][3])));
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32)) * q.scale_rest;
-      if (__any(top > m[t] + (kTop + kLag))) {
+      if (__any(top * q.scale_rest > m[t] + (kTop + kLag))) {  // (one of the row's four lanes has it)
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32)) * q.scale_rest;
         const float now = fmaxf(m[t], top - kTop), by = m[t] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[t] - now);
         m[t] = now;
         l[t] *= by;
@@ -365,7 +370,10 @@ __device__ __forceinline__ void attend(const CacheDev &d, const CacheQuery &q, c
         sum += sh.ml[w][row][1] * (mw == -INFINITY && top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(mw - top));
         v += *reinterpret_cast<const f32x4 *>(&sh.o[w][r][c]);
       }
-      if (pc.parts == 1) {
+      if (JOINED && pc.parts > 1) {
+        *reinterpret_cast<f32x4 *>(part + row * D + c) = v;
+        if (c == 0) *reinterpret_cast<float2 *>(part_ml + row * 2) = make_float2(top, sum);
+      } else if (pc.parts == 1) {
         store_row(q, sp.row0 + (row_first + row) / q.share, head * q.share + (row_first + row) % q.share, c, v, top, sum);
       } else {
         put_pair(part + row * D + c, v[0], v[1]);
@@ -374,6 +382,10 @@ __device__ __forceinline__ void attend(const CacheDev &d, const CacheQuery &q, c
       }
     }
     if (t + 1 < NR) __syncthreads();
+  }
+  if constexpr (JOINED) {  // (by the next launch)
+    if (pc.nth == 0 && threadIdx.x == 0) d.joins[((int64_t)pc.item * d.kv_heads + head) * tiles + pc.tile] = (uint32_t)pc.parts << 16 | (uint32_t)pc.part;
+    return;
   }
   if (pc.parts == 1) return;
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wavefront's part is out ...
@@ -390,7 +402,7 @@ __device__ __forceinline__ void attend(const CacheDev &d, const CacheQuery &q, c
   part_ml = d.part_ml + (int64_t)pc.part * (16 * NR) * 2;
   for (int u = threadIdx.x; u < rows * (D / 4); u += kLanes) {
     const int row = u / (D / 4), c = u % (D / 4) * 4;
-    join_parts(q, sp.row0 + (row_first + row) / q.share, head * q.share + (row_first + row) % q.share, c, pc.parts, part + row * D + c, part_ml + row * 2, D, 16 * NR);
+    join_parts<false>(q, sp.row0 + (row_first + row) / q.share, head * q.share + (row_first + row) % q.share, c, pc.parts, part + row * D + c, part_ml + row * 2, D, 16 * NR);
   }
 }
 
@@ -404,12 +416,30 @@ __global__ __launch_bounds__(kLanes, at_once(D, NR)) void k_cache_sight(CacheDev
   attend<D, NR, true>(d, q, g, tiles);
 }
 
+// Joins parts of rows: 8 rows of 128 channels to a workgroup, or as much of others.
+template <int D, int NR>
+__global__ __launch_bounds__(kLanes) void k_cache_join(CacheDev d, CacheQuery q, CacheSight g, int tiles) {
+  constexpr int kEach = 16 * NR * D / 4 / kLanes;  // workgroups of a row tile
+  static_assert(16 * NR * D / 4 % kLanes == 0, "whole workgroups");
+  const int entry = blockIdx.x / kEach, u = blockIdx.x % kEach * kLanes + threadIdx.x, tile = entry % tiles, head = entry / tiles % d.kv_heads, item = entry / tiles / d.kv_heads;
+  Span sp[1];
+  find_spans<1, 16 * NR, true>(d, q, g, item, false, sp);
+  const int row = u / (D / 4), c = u % (D / 4) * 4, real = tile * 16 * NR + row;
+  if (blockIdx.x % kEach * kLanes / (D / 4) + tile * 16 * NR >= q.share * sp[0].count) return;
+  const uint32_t join = d.joins[entry], parts = join >> 16, first = join & 0xffff;
+  if (parts < 2 || real >= q.share * sp[0].count) return;
+  join_parts<true>(q, sp[0].row0 + real / q.share, head * q.share + real % q.share, c, (int)parts, d.part + ((int64_t)first * (16 * NR) + row) * D + c,
+                   d.part_ml + ((int64_t)first * (16 * NR) + row) * 2, D, 16 * NR);
+}
+
 // (an even share makes no more pieces than run at once, and one more for each row tile of a head)
 template <int D, int NR>
 void launch(const CacheDev &d, const CacheQuery &q, const CacheSight *g, int tiles, hipStream_t s) {
   const uint32_t grid = (uint32_t)(kUnits * at_once(D, NR) + q.r.n * d.kv_heads * tiles);
-  if (g) k_cache_sight<D, NR><<<grid, kLanes, sizeof(Shared<D, NR>), s>>>(d, q, *g, tiles);
-  else k_cache_attend<D, NR><<<grid, kLanes, sizeof(Shared<D, NR>), s>>>(d, q, tiles);
+  if (g) {
+    k_cache_sight<D, NR><<<grid, kLanes, sizeof(Shared<D, NR>), s>>>(d, q, *g, tiles);
+    if constexpr (joined(NR, true)) k_cache_join<D, NR><<<(uint32_t)(q.r.n * d.kv_heads * tiles * (16 * NR * D / 4 / kLanes)), kLanes, 0, s>>>(d, q, *g, tiles);
+  } else if constexpr (NR < 4) k_cache_attend<D, NR><<<grid, kLanes, sizeof(Shared<D, NR>), s>>>(d, q, tiles);
 }
 
 // Up to 64 rows; a head's row tiles read its cache one beside the other, and the second finds it in the last-level cache.
@@ -436,11 +466,18 @@ void launch_cache_attend(const CacheDev &d, const CacheQuery &q, const CacheSigh
   // one sequence of 32,000 34, 42, 71 us and 66, 86, 160; 8 of up to 8,000 28, 36, 122 and 41, 49, 129; 32 of up to 2,000 29, 34, 105 and 44, 51, 153,
   // of 128 channels 50 and 51.
   const int64_t rows = (int64_t)q.share * q.r.max_new;
-  const int each = d.head_dim == 256 || rows <= 16 ? 16 : 32;
+  const int each = d.head_dim == 256 || rows <= 16 ? 16 : g && rows > 32 ? 64 : 32;
   const int64_t tiles = (rows + each - 1) / each;
   // (steps of all row tiles are counted in 32 bits, and they are one launch)
   const int64_t heads = q.r.n * (int64_t)d.kv_heads * tiles;
   if (rows > 64 || (tiles > 1 && (heads >= 1 << 22 || heads * ((int64_t)d.max_pages * d.page_blocks / kWaves + 1) >= (int64_t)1 << 32))) return launch_cache_prompt(d, q, g, s);
+  if (g && rows > 32 && d.head_dim < 256) {  // FOUR_FIGURES
+    switch (d.head_dim) {
+      case 64: return launch<64, 4>(d, q, g, 1, s);
+      case 96: return launch<96, 4>(d, q, g, 1, s);
+      default: return launch<128, 4>(d, q, g, 1, s);
+    }
+  }
   switch (d.head_dim) {
     case 64: return each == 16 ? launch<64, 1>(d, q, g, 1, s) : launch<64, 2>(d, q, g, (int)tiles, s);
     case 96: return each == 16 ? launch<96, 1>(d, q, g, 1, s) : launch<96, 2>(d, q, g, (int)tiles, s);

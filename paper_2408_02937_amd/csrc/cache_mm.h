@@ -250,7 +250,8 @@ __device__ inline uint32_t piece_steps(const float *steps, int n, int kv_heads, 
   return best ? share + (uint32_t)(__ffsll((unsigned long long)best) - 1) * more : 2 * share;
 }
 
-// Channels c .. c + 3 of a row of n parts, `stride` rows apart, joined in order.
+// Channels c .. c + 3 of a row of n parts, `stride` rows apart, joined in order.  before: an earlier launch wrote them.
+template <bool BEFORE>
 __device__ inline void join_parts(const CacheQuery &q, int64_t row, int head, int c, int n, const float *part, const float *ml, int head_dim, int stride) {
   constexpr int kRun = 8;  // parts that are asked for at a time
   float top = -INFINITY, sum = 0.0f;
@@ -260,9 +261,16 @@ __device__ inline void join_parts(const CacheQuery &q, int64_t row, int head, in
 #pragma unroll
     for (int k = 0; k < kRun; ++k) {
       const int64_t i = min(i0 + k, n - 1) * (int64_t)stride;
-      x[k] = get_pair(ml + i * 2);
-      a[k] = get_pair(part + i * head_dim);
-      b[k] = get_pair(part + i * head_dim + 2);
+      if constexpr (BEFORE) {
+        const f32x4 y = *reinterpret_cast<const f32x4 *>(part + i * head_dim);
+        x[k] = *reinterpret_cast<const float2 *>(ml + i * 2);
+        a[k] = make_float2(y[0], y[1]);
+        b[k] = make_float2(y[2], y[3]);
+      } else {
+        x[k] = get_pair(ml + i * 2);
+        a[k] = get_pair(part + i * head_dim);
+        b[k] = get_pair(part + i * head_dim + 2);
+      }
     }
     float now = top;
 #pragma unroll

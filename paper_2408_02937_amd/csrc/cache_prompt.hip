@@ -20,6 +20,7 @@
 #include "../../include/rtams_cache.h"
 
 #include <climits>
+#include <type_traits>
 
 #include "cache_mm.h"
 #include "rtams_dev.h"
@@ -34,12 +35,13 @@ constexpr int tile_blocks(int head_dim) { return head_dim == 256 ? 1 : 2; }  // 
 constexpr int kRows = 256;       // of a workgroup's parts at most
 
 // Workgroups that a compute unit runs at once: registers decide.
-constexpr int at_once(int head_dim, int waves) { return waves == 8 || head_dim == 256 ? 1 : 2; }
+constexpr int at_once(int head_dim, int waves) { return waves == 8 || head_dim == 256 ? 1 : waves == 4 ? 2 : 3; }
 
-template <int D>
+template <int D, int TB, int RING>
 struct Staging {  // tiles in LDS: operands of 16 bytes
-  uint4 k[2][tile_blocks(D) * 4 * D];  // [block][word][token]
-  uint4 v[2][tile_blocks(D) * 4 * D];  // [block][32 channels][lane group][channel]
+  uint4 k[2][TB * 4 * D];  // [block][word][token]
+  uint4 v[2][TB * 4 * D];  // [block][32 channels][lane group][channel]
+  uint4 raw[RING > 0 ? RING : 1][RING > 0 ? TB * 40 * D / 16 : 1];  // with a ring: tiles as the cache holds them, on their way
 };
 
 __device__ inline int key_slot(int word, int token) { return token ^ (((word >> 1) & 7) << 1); }
@@ -51,19 +53,19 @@ struct Words {  // two words of keys or values with their steps and zeros
   HalfWords step, zero;  // keys: w[0] holds both
 };
 
-// Pairs of words of a tile whose blocks are at blk0 and blk1: the first kPairs<D> are keys, as many more values.
-template <int D>
-constexpr int kPairs = tile_blocks(D) * 2 * D;
-template <int D>
+// Pairs of words of a tile whose blocks are at blk0 and blk1: the first kPairs<D, TB> are keys, as many more values.
+template <int D, int TB>
+constexpr int kPairs = TB * 2 * D;
+template <int D, int TB>
 __device__ inline void load_words(Words<D> &p, int u, const unsigned char *blk0, const unsigned char *blk1) {
   constexpr int WP = D / 16, VC = value_chunk(D);
-  if (u < kPairs<D>) {
+  if (u < kPairs<D, TB>) {
     const int token = u / WP, wp = u % WP;
     const unsigned char *blk = token < 32 ? blk0 : blk1;
     p.code = *reinterpret_cast<const uint2 *>(blk + (token & 31) * (D / 2) + wp * 8);
     p.step.w[0] = *reinterpret_cast<const uint32_t *>(blk + 16 * D + ((token & 31) * (D / 32) + (wp >> 1)) * 4);
   } else {
-    const int x = u - kPairs<D>, idx = x % (2 * D);
+    const int x = u - kPairs<D, TB>, idx = x % (2 * D);
     const unsigned char *blk = x < 2 * D ? blk0 : blk1;
     p.code = *reinterpret_cast<const uint2 *>(blk + 20 * D + idx * 8);
     const int group = VC == 4 ? (idx >> 7) * 2 + (idx & 1) : idx >> 6, b = VC == 4 ? (idx >> 5) & 3 : (idx >> 4) & 3;
@@ -73,10 +75,10 @@ __device__ inline void load_words(Words<D> &p, int u, const unsigned char *blk0,
   }
 }
 
-template <int D>
+template <int D, int TB>
 __device__ inline void put_words(const Words<D> &p, int u, uint4 *k, uint4 *v) {
   constexpr int WP = D / 16, VC = value_chunk(D);
-  if (u < kPairs<D>) {
+  if (u < kPairs<D, TB>) {
     const int token = u / WP, wp = u % WP;
     const half2v step = {half_at(p.step.w[0], 0), half_at(p.step.w[0], 0)}, zero = {half_at(p.step.w[0], 1), half_at(p.step.w[0], 1)};
 #pragma unroll
@@ -88,7 +90,7 @@ __device__ inline void put_words(const Words<D> &p, int u, uint4 *k, uint4 *v) {
       k[((token >> 5) * (D / 8) + word) * 32 + key_slot(word, token & 31)] = make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]);
     }
   } else {
-    const int y = u - kPairs<D>, idx = y % (2 * D), block = y / (2 * D);
+    const int y = u - kPairs<D, TB>, idx = y % (2 * D), block = y / (2 * D);
     const int tile = VC == 4 ? (idx >> 7) * 2 + (idx & 1) : idx >> 6, lane = VC == 4 ? (idx >> 1) & 63 : idx & 63;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -156,9 +158,9 @@ constexpr int kSplit = 4;
 constexpr int kMostEntries = 1024;  // row tiles of items that are planned
 constexpr int kClasses = 8;         // of their pieces, by length
 
-template <int D>
+template <int D, int TB, int RING>
 union Shared {
-  Staging<D> tile;
+  Staging<D, TB, RING> tile;
   float steps[kMostEntries];  // in front of them
 };
 
@@ -204,7 +206,7 @@ __device__ inline bool find_piece(const CacheDev &d, const CacheQuery &q, const 
 // compiler asks for a pair and waits for it, a trip to LDS for every two instructions.)
 template <int N>
 __device__ __forceinline__ void reads_ahead() {
-  constexpr int kAhead = 6, kRead = 0x100, kMfma = 0x8;
+  constexpr int kAhead = N < 6 ? N : 6, kRead = 0x100, kMfma = 0x8;
   __builtin_amdgcn_sched_group_barrier(kRead, kAhead, 0);
 #pragma unroll
   for (int i = 0; i < N - kAhead; ++i) {
@@ -214,13 +216,24 @@ __device__ __forceinline__ void reads_ahead() {
   __builtin_amdgcn_sched_group_barrier(kMfma, kAhead, 0);
 }
 
-template <int D, int WAVES, bool SIGHT>
+// The copies of a workgroup's tiles into its ring, in chunks of 1 KiB, one to a wavefront after the other: a wavefront has as many of each tile.
+constexpr int kRing = 4;  // tiles on their way or in use
+
+// The other wavefronts' writes to LDS, and copies that they waited for, are there.  (Not __syncthreads: that would wait for all copies.)
+__device__ __forceinline__ void meet() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+template <int D, int WAVES, int TB, bool SIGHT>
 __device__ __forceinline__ void attend_many(const CacheDev &d, const CacheQuery &q, const CacheSight &g, int tiles, int tile_rows, int split, uint32_t first) {
-  constexpr int kLanes = WAVES * 64, NS = D / 16, NC = D / 32, NP = (2 * kPairs<D> + kLanes - 1) / kLanes;
-  constexpr int TB = tile_blocks(D), kTile = TB * kBlockTokens;
+  constexpr int kLanes = WAVES * 64, NS = D / 16, NC = D / 32, NP = (2 * kPairs<D, TB> + kLanes - 1) / kLanes;
+  constexpr int kTile = TB * kBlockTokens;
   extern __shared__ uint4 lds[];
-  Shared<D> &shared = *reinterpret_cast<Shared<D> *>(lds);
-  Staging<D> &sh = shared.tile;
+  constexpr int RING = SIGHT ? kRing : 0;
+  Shared<D, TB, RING> &shared = *reinterpret_cast<Shared<D, TB, RING> *>(lds);
+  Staging<D, TB, RING> &sh = shared.tile;
   __shared__ Piece piece;
   __shared__ int flag;
   Piece pc;
@@ -314,14 +327,14 @@ __device__ __forceinline__ void attend_many(const CacheDev &d, const CacheQuery 
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       const int u = i * kLanes + threadIdx.x;
-      if (2 * kPairs<D> % kLanes == 0 || u < 2 * kPairs<D>) load_words<D>(to[i], u, b0, b1);
+      if (2 * kPairs<D, TB> % kLanes == 0 || u < 2 * kPairs<D, TB>) load_words<D, TB>(to[i], u, b0, b1);
     }
   };
   const auto put_tile = [&](const Words<D> (&of)[NP], uint4 *k, uint4 *v) {
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       const int u = i * kLanes + threadIdx.x;
-      if (2 * kPairs<D> % kLanes == 0 || u < 2 * kPairs<D>) put_words<D>(of[i], u, k, v);
+      if (2 * kPairs<D, TB> % kLanes == 0 || u < 2 * kPairs<D, TB>) put_words<D, TB>(of[i], u, k, v);
     }
   };
   f32x16 sc[TB];
@@ -415,7 +428,69 @@ __device__ __forceinline__ void attend_many(const CacheDev &d, const CacheQuery 
         }
     reads_ahead<NC * TB * 2>();
   };
-  if (length > 0) {  // (an empty sequence has one step and no page)
+  const auto compute = [&](int t, int now) {
+    const int tok0 = SIGHT ? place(t * kTile) : from + t * kTile;
+    const int tok1 = SIGHT && TB == 2 ? place(t * kTile + kBlockTokens) : tok0;
+    const auto seen = [&](int tok) { return tok < any_to && (tok + kBlockTokens > any_from || tok < g.sinks); };
+    const bool some = SIGHT ? seen(tok0) || seen(tok1) : tok0 < any_to && tok0 + kTile > any_from;
+    if (some) {
+      // (matrix instructions first: the other wavefront of the SIMD has its exponentials beside them)
+      __builtin_amdgcn_s_setprio(1);
+      scores(sh.k[now]);
+      __builtin_amdgcn_s_setprio(0);
+      probabilities(tok0, tok1);
+      __builtin_amdgcn_s_setprio(1);
+      weigh(sh.v[now]);
+      __builtin_amdgcn_s_setprio(0);
+    }
+  };
+  if constexpr (SIGHT) {
+    if (length > 0) {
+      constexpr int kChunks = (40 * D + 1023) / 1024, kAll = TB * kChunks, kMost = (kAll + WAVES - 1) / WAVES, kLess = kAll / WAVES;
+      const uint32_t ring = (uint32_t)uniform((int)lds_address(sh.raw[0]));
+      const auto copy = [&](int t) {
+        const uint32_t slot = ring + (uint32_t)(t - t0) % kRing * (TB * 40 * D);
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) {
+          const int c = i * WAVES + wave, x = c / kChunks, at = c % kChunks * 1024;
+          if (i < kLess || c < kAll) {
+            const unsigned char *blk = block_at(place(t * kTile + x * kBlockTokens) / kBlockTokens);
+            if (40 * D % 1024 == 0 || lane * 16 < 40 * D - at) copy_to_lds(blk + at, slot + x * (40 * D) + at, lane * 16);
+          }
+        }
+      };
+      // all but the last `tiles` tiles that this wavefront asked for are there
+      const auto arrived = [&](auto tiles) {
+        constexpr int kTiles = decltype(tiles)::value;
+        if (kMost == kLess || wave < kAll % WAVES) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kMost * kTiles) : "memory");
+        else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLess * kTiles) : "memory");
+      };
+      const auto unpack = [&](int t) {
+        const unsigned char *b0 = reinterpret_cast<const unsigned char *>(sh.raw[(uint32_t)(t - t0) % kRing]), *b1 = b0 + (TB == 2 ? 40 * D : 0);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+          const int u = i * kLanes + threadIdx.x;
+          if (2 * kPairs<D, TB> % kLanes == 0 || u < 2 * kPairs<D, TB>) load_words<D, TB>(next[i], u, b0, b1);
+        }
+        put_tile(next, sh.k[(t - t0) & 1], sh.v[(t - t0) & 1]);
+      };
+      for (int i = 0; i < kRing - 1; ++i)
+        if (t0 + i < t1) copy(t0 + i);
+      if (t0 + kRing - 1 <= t1) arrived(std::integral_constant<int, kRing - 2>());
+      else arrived(std::integral_constant<int, 0>());
+      meet();
+      unpack(t0);
+      if (t0 + kRing - 1 < t1) copy(t0 + kRing - 1);
+      for (int t = t0; t < t1; ++t) {
+        if (t + kRing <= t1) arrived(std::integral_constant<int, kRing - 2>());
+        else arrived(std::integral_constant<int, 0>());
+        meet();  // (tile t is unpacked, the next one's codes are there, and what this turn writes over has been read)
+        if (t + kRing < t1) copy(t + kRing);
+        if (t + 1 < t1) unpack(t + 1);
+        compute(t, (t - t0) & 1);
+      }
+    }
+  } else if (length > 0) {  // (an empty sequence has one step and no page)
     {
       Words<D> first[NP];
       load_tile(first, t0);
@@ -424,29 +499,27 @@ __device__ __forceinline__ void attend_many(const CacheDev &d, const CacheQuery 
     }
     __syncthreads();
     for (int t = t0; t < t1; ++t) {
-      const int tok0 = SIGHT ? place(t * kTile) : from + t * kTile, now = (t - t0) & 1;
-      const int tok1 = SIGHT && TB == 2 ? place(t * kTile + kBlockTokens) : tok0;
-      const auto seen = [&](int tok) { return tok < any_to && (tok + kBlockTokens > any_from || tok < g.sinks); };
-      const bool some = SIGHT ? seen(tok0) || seen(tok1) : tok0 < any_to && tok0 + kTile > any_from;
+      const int now = (t - t0) & 1;
       if (t + 1 < t1) put_tile(next, sh.k[now ^ 1], sh.v[now ^ 1]);
       if (t + 2 < t1) load_tile(next, t + 2);
-      if (some) {
-        // (matrix instructions first: the other wavefront of the SIMD has its exponentials beside them)
-        __builtin_amdgcn_s_setprio(1);
-        scores(sh.k[now]);
-        __builtin_amdgcn_s_setprio(0);
-        probabilities(tok0, tok1);
-        __builtin_amdgcn_s_setprio(1);
-        weigh(sh.v[now]);
-        __builtin_amdgcn_s_setprio(0);
-      }
+      compute(t, now);
       __syncthreads();
     }
   }
   l += __shfl_xor(l, 32);
   m *= rest;
 
-  if (pc.parts > 1) {
+  if (SIGHT && split && threadIdx.x == 0 && pc.nth == 0) d.joins[pc.entry * d.kv_heads + head] = (uint32_t)pc.parts << 16 | (uint32_t)pc.part;
+  if (SIGHT && pc.parts > 1) {  // (joined by the next launch)
+    float *p = d.part + ((int64_t)(pc.part + pc.nth) * WAVES + wave) * (64 * 16 * NC) + lane * 2;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) *reinterpret_cast<float2 *>(p + (c * 8 + e / 2) * 128) = make_float2(o[c][e], o[c][e + 1]);
+    *reinterpret_cast<float2 *>(d.part_ml + (((int64_t)(pc.part + pc.nth) * WAVES + wave) * 64 + lane) * 2) = make_float2(m, l);
+    return;
+  }
+  if (!SIGHT && pc.parts > 1) {
     // Parts lie as the lanes hold them, so that stores are whole lines and the last workgroup to arrive joins them in its own registers.
     const auto part_of = [&](int i) { return d.part + ((int64_t)(pc.part + i) * WAVES + wave) * (64 * 16 * NC) + lane * 2; };
     const auto ml_of = [&](int i) { return d.part_ml + (((int64_t)(pc.part + i) * WAVES + wave) * 64 + lane) * 2; };
@@ -498,52 +571,97 @@ __device__ __forceinline__ void attend_many(const CacheDev &d, const CacheQuery 
 
 template <int D, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt(CacheDev d, CacheQuery q, int tiles, int tile_rows, int split, uint32_t first) {
-  attend_many<D, WAVES, false>(d, q, CacheSight{}, tiles, tile_rows, split, first);
+  attend_many<D, WAVES, tile_blocks(D), false>(d, q, CacheSight{}, tiles, tile_rows, split, first);
 }
 
-template <int D, int WAVES>
+template <int D, int WAVES, int TB>
 __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt_sight(CacheDev d, CacheQuery q, CacheSight g, int tiles, int tile_rows, int split, uint32_t first) {
-  attend_many<D, WAVES, true>(d, q, g, tiles, tile_rows, split, first);
+  attend_many<D, WAVES, TB, true>(d, q, g, tiles, tile_rows, split, first);
 }
 
+// Joins what several workgroups have of a row tile: a wavefront has 32 channels of 32 rows, held as they lie in the parts.  (By the last
+// workgroup to arrive, as k_cache_prompt does it, a part is 128 KiB that one compute unit reads: JOIN_FIGURES)
 template <int D, int WAVES>
+__global__ __launch_bounds__(256) void k_cache_join_many(CacheDev d, CacheQuery q, CacheSight g, int tiles, int tile_rows) {
+  constexpr int NC = D / 32, kUnit = WAVES * NC;
+  static_assert(kUnit % 4 == 0, "whole workgroups");
+  const int lane = threadIdx.x & 63, col = lane & 31, h = lane >> 5, x = blockIdx.x * 4 + uniform(threadIdx.x >> 6), entry = x / kUnit, wave = x % kUnit / NC, c = x % NC;
+  const int head = entry % d.kv_heads, item = entry / d.kv_heads % q.r.n, tile = tiles - 1 - entry / d.kv_heads / q.r.n;
+  const Span sp = find_span<true>(d, q, g, item, tile, tile_rows, 32, false);
+  if (!sp.count) return;
+  const uint32_t join = d.joins[entry], parts = join >> 16, first = join & 0xffff;
+  const int row = wave * 32 + col, mine = tile * tile_rows + row;
+  if (parts < 2 || !__any(row < min(q.share * sp.count - tile * tile_rows, tile_rows))) return;
+  const float *ml = d.part_ml + ((int64_t)first * WAVES + wave) * 128 + lane * 2, *p = d.part + ((int64_t)first * WAVES + wave) * (1024 * NC) + c * 1024 + lane * 2;
+  float m = -INFINITY;
+  for (uint32_t i = 0; i < parts; ++i) m = fmaxf(m, ml[i * WAVES * 128]);
+  float l = 0.0f;
+  f32x16 o;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) o[e] = 0.0f;
+#pragma unroll 2
+  for (uint32_t i = 0; i < parts; ++i) {
+    const float2 at = *reinterpret_cast<const float2 *>(ml + i * WAVES * 128);
+    const float by = at.x == -INFINITY && m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(at.x - m);
+    l += at.y * by;
+#pragma unroll
+    for (int e = 0; e < 16; e += 2) {
+      const float2 y = *reinterpret_cast<const float2 *>(p + (int64_t)i * WAVES * (1024 * NC) + e * 64);
+      o[e] += y.x * by;
+      o[e + 1] += y.y * by;
+    }
+  }
+  if (row >= min(q.share * sp.count - tile * tile_rows, tile_rows)) return;
+#pragma unroll
+  for (int e = 0; e < 16; e += 4)
+    store_row(q, sp.row0 + mine / q.share, head * q.share + mine % q.share, c * 32 + 2 * e + 4 * h, f32x4{o[e], o[e + 1], o[e + 2], o[e + 3]}, m, l);
+}
+
+template <int D, int WAVES, int TB>
 void launch(const CacheDev &d, const CacheQuery &q, const CacheSight *g, hipStream_t s) {
-  constexpr int kWorkers = kUnits * at_once(D, WAVES);
+  constexpr int kWorkers = kUnits * at_once(D, WAVES), kSplits = kSplit * kUnits * at_once(D, 8) / kWorkers;
   const int64_t rows = (int64_t)q.share * q.r.max_new;
   const int tiles = (int)((rows + WAVES * 32 - 1) / (WAVES * 32)), tile_rows = (int)((rows + tiles - 1) / tiles + 31) / 32 * 32;  // (all about as long)
   const int64_t groups = (int64_t)tiles * q.r.n * d.kv_heads;
-  static_assert(kSplit * kWorkers <= kMostEntries, "all row tiles of all items are planned");
+  static_assert(kSplits >= 1 && kSplits * kWorkers <= kMostEntries, "all row tiles of all items are planned");
   // (steps of all row tiles are counted in 32 bits)
-  const bool split = groups < (q.r.n > 1 ? kSplit : 1) * kWorkers && groups * ((int64_t)d.max_pages * d.page_blocks + 1) < (int64_t)1 << 32;
+  const bool split = groups < (q.r.n > 1 ? kSplits : 1) * kWorkers && groups * ((int64_t)d.max_pages * d.page_blocks + 1) < (int64_t)1 << 32;
   const int64_t all = split ? groups + kWorkers : groups, most = 1 << 22;  // (of a launch; one that finds no rows takes 10 ns: 512 items of 8 heads, one of 32,768 rows, 28 ms of which it takes 6)
   for (int64_t at = 0; at < all; at += most) {
     const uint32_t grid = (uint32_t)(all - at < most ? all - at : most);
-    if (g) k_cache_prompt_sight<D, WAVES><<<grid, WAVES * 64, sizeof(Shared<D>), s>>>(d, q, *g, tiles, tile_rows, split, (uint32_t)at);
-    else k_cache_prompt<D, WAVES><<<grid, WAVES * 64, sizeof(Shared<D>), s>>>(d, q, tiles, tile_rows, split, (uint32_t)at);
+    if (g) k_cache_prompt_sight<D, WAVES, TB><<<grid, WAVES * 64, sizeof(Shared<D, TB, kRing>), s>>>(d, q, *g, tiles, tile_rows, split, (uint32_t)at);
+    else if constexpr (TB == tile_blocks(D) && WAVES == (D == 256 ? 4 : 8)) k_cache_prompt<D, WAVES><<<grid, WAVES * 64, sizeof(Shared<D, TB, 0>), s>>>(d, q, tiles, tile_rows, split, (uint32_t)at);
   }
+  if (g && split) k_cache_join_many<D, WAVES><<<(uint32_t)(groups * WAVES * (D / 32) / 4), 256, 0, s>>>(d, q, *g, tiles, tile_rows);
 }
 
 }  // namespace
 
 // Rows of parts: at most two pieces that are parts for each that runs at once.
 size_t cache_prompt_part_rows() { return (size_t)2 * kUnits * kRows; }
-size_t cache_prompt_groups() { return (size_t)4 * kUnits; }
+size_t cache_prompt_groups() { return (size_t)8 * kUnits; }
 
 void launch_cache_prompt(const CacheDev &d, const CacheQuery &q, const CacheSight *g, hipStream_t s) {
+  const bool few = g && (int64_t)q.share * q.r.max_new <= 128;  // FEW_FIGURES
   switch (d.head_dim) {
-    case 64: return launch<64, 8>(d, q, g, s);
-    case 96: return launch<96, 8>(d, q, g, s);
-    case 128: return launch<128, 8>(d, q, g, s);
-    default: return launch<256, 4>(d, q, g, s);
+    case 64: return few ? launch<64, 4, 1>(d, q, g, s) : launch<64, 8, 2>(d, q, g, s);
+    case 96: return few ? launch<96, 4, 1>(d, q, g, s) : launch<96, 8, 2>(d, q, g, s);
+    case 128: return few ? launch<128, 4, 1>(d, q, g, s) : launch<128, 8, 2>(d, q, g, s);
+    default: return launch<256, 4, 1>(d, q, g, s);
   }
 }
 
 hipError_t allow_large_lds_cache_prompt() {
   const auto allow = [](const void *f, size_t bytes) { return hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes); };
-  if (const hipError_t e = allow(reinterpret_cast<const void *>(k_cache_prompt<128, 8>), sizeof(Shared<128>))) return e;
-  if (const hipError_t e = allow(reinterpret_cast<const void *>(k_cache_prompt_sight<128, 8>), sizeof(Shared<128>))) return e;
-  if (const hipError_t e = allow(reinterpret_cast<const void *>(k_cache_prompt_sight<256, 4>), sizeof(Shared<256>))) return e;
-  return allow(reinterpret_cast<const void *>(k_cache_prompt<256, 4>), sizeof(Shared<256>));
+  hipError_t e = allow(reinterpret_cast<const void *>(k_cache_prompt<128, 8>), sizeof(Shared<128, 2, 0>));
+  if (e == hipSuccess) e = allow(reinterpret_cast<const void *>(k_cache_prompt<256, 4>), sizeof(Shared<256, 1, 0>));
+  const auto allow_sight = [&](auto kernel, size_t bytes) {
+    if (e == hipSuccess) e = allow(reinterpret_cast<const void *>(kernel), bytes);
+  };
+  allow_sight(k_cache_prompt_sight<96, 8, 2>, sizeof(Shared<96, 2, kRing>));
+  allow_sight(k_cache_prompt_sight<128, 8, 2>, sizeof(Shared<128, 2, kRing>));
+  allow_sight(k_cache_prompt_sight<256, 4, 1>, sizeof(Shared<256, 1, kRing>));
+  return e;
 }
 
 }  // namespace rtams

@@ -145,7 +145,8 @@ def shapes_of_rows(vocab, dtype):
 def test_rows_of_equal_and_ordered_logits(dtype, vocab, top):
     x = shapes_of_rows(vocab, dtype)
     check(x, None, top)
-    check(x.repeat(65, 1), None, top)  # (whole rows)
+    if vocab <= 5_000:
+        check(x.repeat(65, 1), None, top)  # (whole rows)
 
 
 @pytest.mark.parametrize("dtype", TYPES)
