@@ -26,7 +26,7 @@ constexpr int kLanes = 256, kWaves = 4, kStep = kWaves * kBlockTokens;
 
 // Workgroups that a compute unit runs at once: registers decide, and from 128 channels on LDS (40 * D * 8 bytes of blocks).
 constexpr int at_once(int head_dim, int tiles) {
-  return tiles == 4 ? (head_dim == 64 ? 2 : 1) : tiles == 2 ? (head_dim == 64 ? 3 : 2) : head_dim == 64 ? 5 : head_dim == 96 ? 4 : head_dim == 128 ? 3 : 1;
+  return tiles == 2 ? (head_dim == 64 ? 3 : 2) : head_dim == 64 ? 5 : head_dim == 96 ? 4 : head_dim == 128 ? 3 : 1;
 }
 
 // Whether parts of rows are joined by a launch of their own: a row tile of 32 rows or more is too much for the last workgroup to arrive, which
@@ -100,10 +100,13 @@ struct alignas(16) Shared {
   int last;
 };
 
+// Sequences of so many steps at most are not split where parts would be joined by another launch.  WHOLE_FIGURES
+constexpr int kWhole = 4;
+
 // Which piece is workgroup blockIdx.x's: the items' steps, the size of a piece, and the pieces of the items in front.  One wavefront's work, EACH
 // items to a lane (lane, lane + 64, ...); false where there is none left.
 template <int EACH, int ROWS, bool SIGHT, class S>
-__device__ bool find_piece(const CacheDev &d, const CacheQuery &q, const CacheSight &g, int tiles, uint32_t workers, S &sh) {
+__device__ bool find_piece(const CacheDev &d, const CacheQuery &q, const CacheSight &g, int tiles, uint32_t workers, bool whole, S &sh) {
   constexpr int kItems = 64 * EACH;
   const int lane = threadIdx.x & 63, n = q.r.n;
   Span sp[EACH];
@@ -120,12 +123,12 @@ __device__ bool find_piece(const CacheDev &d, const CacheQuery &q, const CacheSi
   // for twice as many parts as there are workers.  A head of s steps that is split, s > size, has fewer than 2 s / size parts, all of them fewer than
   // 2 all / size.)
   const uint32_t share = (all + workers - 1) / workers;
-  uint32_t size = share > 1 ? share : 1;
-  if (share > 1 && n <= kItems && n * d.kv_heads * tiles <= (int)workers / 2) {
+  uint32_t size = whole ? kWhole : share > 1 ? share : 1;
+  if (share > 1 && !whole && n <= kItems && n * d.kv_heads * tiles <= (int)workers / 2) {
 #pragma unroll
     for (int k = 0; k < EACH; ++k) sh.steps[64 * k + lane] = (float)sp[k].steps;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    size = piece_steps(sh.steps, n, d.kv_heads * tiles, share, workers);
+    size = piece_steps(sh.steps, n, d.kv_heads * tiles, share, workers, SIGHT ? 1 : 0);
   }
   const float one_over = 1.0f / (float)size;
   uint32_t before = 0, parts_before = 0;
@@ -135,8 +138,10 @@ __device__ bool find_piece(const CacheDev &d, const CacheQuery &q, const CacheSi
     for (int k = 0; k < EACH; ++k) {
       const uint32_t parts = div_up((uint32_t)sp[k].steps, size, one_over), pieces = parts * (uint32_t)(d.kv_heads * sp[k].tiles), shared = parts > 1 ? pieces : 0;
       const uint32_t upto = wave_running_sum(pieces), upto_shared = wave_running_sum(shared), x = blockIdx.x - (before + upto - pieces);
-      if (x < pieces) {  // (row tiles fastest: they read the same tokens)
-        const uint32_t t = x % (uint32_t)sp[k].tiles, y = x / (uint32_t)sp[k].tiles, head = y / parts;
+      if (x < pieces) {
+        // Row tiles of a piece read the same tokens: they are 8 workgroups apart, on the same die, whose L2 has them.  XCD_FIGURES
+        const uint32_t n_tiles = (uint32_t)sp[k].tiles, all_y = parts * (uint32_t)d.kv_heads, y0 = x / (8 * n_tiles) * 8, beside = min(8u, all_y - y0), rest = x - y0 * n_tiles;
+        const uint32_t t = rest / beside, y = y0 + rest - t * beside, head = y / parts;
         sh.piece = Piece{sp[k], base + 64 * k + lane, (int)head, (int)t, 0, 0, (int)parts, (int)(y % parts),
                          (int)(parts_before + upto_shared - shared + (head * sp[k].tiles + t) * parts)};
       }
@@ -183,7 +188,7 @@ struct Copies {
 };
 
 template <int D, int NR, bool SIGHT>
-__device__ __forceinline__ void attend(const CacheDev &d, const CacheQuery &q, const CacheSight &g, int tiles) {
+__device__ __forceinline__ void attend(const CacheDev &d, const CacheQuery &q, const CacheSight &g, int tiles, bool whole) {
   constexpr int NJ = D / 32, NT = D / 16;
   constexpr bool JOINED = joined(NR, SIGHT);
   extern __shared__ uint4 lds[];
@@ -191,7 +196,7 @@ __device__ __forceinline__ void attend(const CacheDev &d, const CacheQuery &q, c
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 15, b = lane >> 4;
 
   if (wave == 0) {
-    const bool found = q.r.n <= 64 ? find_piece<1, 16 * NR, SIGHT>(d, q, g, tiles, kUnits * at_once(D, NR), sh) : find_piece<kRound / 64, 16 * NR, SIGHT>(d, q, g, tiles, kUnits * at_once(D, NR), sh);
+    const bool found = q.r.n <= 64 ? find_piece<1, 16 * NR, SIGHT>(d, q, g, tiles, kUnits * at_once(D, NR), whole, sh) : find_piece<kRound / 64, 16 * NR, SIGHT>(d, q, g, tiles, kUnits * at_once(D, NR), whole, sh);
     if (lane == 0) sh.last = found;
   }
   __syncthreads();
@@ -408,12 +413,12 @@ __device__ __forceinline__ void attend(const CacheDev &d, const CacheQuery &q, c
 
 template <int D, int NR>
 __global__ __launch_bounds__(kLanes, at_once(D, NR)) void k_cache_attend(CacheDev d, CacheQuery q, int tiles) {
-  attend<D, NR, false>(d, q, CacheSight{}, tiles);
+  attend<D, NR, false>(d, q, CacheSight{}, tiles, false);
 }
 
 template <int D, int NR>
-__global__ __launch_bounds__(kLanes, at_once(D, NR)) void k_cache_sight(CacheDev d, CacheQuery q, CacheSight g, int tiles) {
-  attend<D, NR, true>(d, q, g, tiles);
+__global__ __launch_bounds__(kLanes, at_once(D, NR)) void k_cache_sight(CacheDev d, CacheQuery q, CacheSight g, int tiles, int whole) {
+  attend<D, NR, true>(d, q, g, tiles, whole);
 }
 
 // Joins parts of rows: 8 rows of 128 channels to a workgroup, or as much of others.
@@ -436,10 +441,14 @@ __global__ __launch_bounds__(kLanes) void k_cache_join(CacheDev d, CacheQuery q,
 template <int D, int NR>
 void launch(const CacheDev &d, const CacheQuery &q, const CacheSight *g, int tiles, hipStream_t s) {
   const uint32_t grid = (uint32_t)(kUnits * at_once(D, NR) + q.r.n * d.kv_heads * tiles);
-  if (g) {
-    k_cache_sight<D, NR><<<grid, kLanes, sizeof(Shared<D, NR>), s>>>(d, q, *g, tiles);
-    if constexpr (joined(NR, true)) k_cache_join<D, NR><<<(uint32_t)(q.r.n * d.kv_heads * tiles * (16 * NR * D / 4 / kLanes)), kLanes, 0, s>>>(d, q, *g, tiles);
-  } else if constexpr (NR < 4) k_cache_attend<D, NR><<<grid, kLanes, sizeof(Shared<D, NR>), s>>>(d, q, tiles);
+  if (!g) {
+    k_cache_attend<D, NR><<<grid, kLanes, sizeof(Shared<D, NR>), s>>>(d, q, tiles);
+    return;
+  }
+  const bool whole = joined(NR, true) && (int64_t)d.max_pages * d.page_tokens <= kWhole * kStep;
+  k_cache_sight<D, NR><<<grid, kLanes, sizeof(Shared<D, NR>), s>>>(d, q, *g, tiles, whole);
+  if constexpr (joined(NR, true))
+    if (!whole) k_cache_join<D, NR><<<(uint32_t)(q.r.n * d.kv_heads * tiles * (16 * NR * D / 4 / kLanes)), kLanes, 0, s>>>(d, q, *g, tiles);
 }
 
 // Up to 64 rows; a head's row tiles read its cache one beside the other, and the second finds it in the last-level cache.
@@ -466,18 +475,11 @@ void launch_cache_attend(const CacheDev &d, const CacheQuery &q, const CacheSigh
   // one sequence of 32,000 34, 42, 71 us and 66, 86, 160; 8 of up to 8,000 28, 36, 122 and 41, 49, 129; 32 of up to 2,000 29, 34, 105 and 44, 51, 153,
   // of 128 channels 50 and 51.
   const int64_t rows = (int64_t)q.share * q.r.max_new;
-  const int each = d.head_dim == 256 || rows <= 16 ? 16 : g && rows > 32 ? 64 : 32;
+  const int each = d.head_dim == 256 || rows <= 16 ? 16 : 32;
   const int64_t tiles = (rows + each - 1) / each;
   // (steps of all row tiles are counted in 32 bits, and they are one launch)
   const int64_t heads = q.r.n * (int64_t)d.kv_heads * tiles;
   if (rows > 64 || (tiles > 1 && (heads >= 1 << 22 || heads * ((int64_t)d.max_pages * d.page_blocks / kWaves + 1) >= (int64_t)1 << 32))) return launch_cache_prompt(d, q, g, s);
-  if (g && rows > 32 && d.head_dim < 256) {  // FOUR_FIGURES
-    switch (d.head_dim) {
-      case 64: return launch<64, 4>(d, q, g, 1, s);
-      case 96: return launch<96, 4>(d, q, g, 1, s);
-      default: return launch<128, 4>(d, q, g, 1, s);
-    }
-  }
   switch (d.head_dim) {
     case 64: return each == 16 ? launch<64, 1>(d, q, g, 1, s) : launch<64, 2>(d, q, g, (int)tiles, s);
     case 96: return each == 16 ? launch<96, 1>(d, q, g, 1, s) : launch<96, 2>(d, q, g, (int)tiles, s);

@@ -230,7 +230,8 @@ constexpr int kUnits = 256;  // compute units
 // Steps of a piece, of n items' steps.  Pieces are to run all at once, `workers` of them, and to leave the compute units alike much to do:
 // of sixteen sizes from an even share up to twice that, a quarter of the items to a lane, the one with the least steps for a
 // compute unit, which has pieces / 256 rounded up.
-__device__ inline uint32_t piece_steps(const float *steps, int n, int kv_heads, uint32_t share, uint32_t workers) {
+// beside: what a unit's first piece costs beyond the others that run beside it.
+__device__ inline uint32_t piece_steps(const float *steps, int n, int kv_heads, uint32_t share, uint32_t workers, uint32_t beside = 0) {
   const int lane = threadIdx.x & 63;
   const uint32_t more = (share + 15) / 16, size = share + (lane & 15) * more;
   const float one_over = __builtin_amdgcn_rcpf((float)size);
@@ -242,7 +243,7 @@ __device__ inline uint32_t piece_steps(const float *steps, int n, int kv_heads, 
   pieces += __shfl_xor(pieces, 16);
   pieces += __shfl_xor(pieces, 32);
   const uint32_t all = (uint32_t)pieces * (uint32_t)kv_heads;
-  float cost = all <= workers ? (float)((all + kUnits - 1) / kUnits) * (float)size : 3e38f;
+  float cost = all <= workers ? (float)((all + kUnits - 1) / kUnits + beside) * (float)size : 3e38f;
   const float mine = cost;
 #pragma unroll
   for (int o = 1; o < 16; o <<= 1) cost = fminf(cost, __shfl_xor(cost, o));
@@ -253,7 +254,7 @@ __device__ inline uint32_t piece_steps(const float *steps, int n, int kv_heads, 
 // Channels c .. c + 3 of a row of n parts, `stride` rows apart, joined in order.  before: an earlier launch wrote them.
 template <bool BEFORE>
 __device__ inline void join_parts(const CacheQuery &q, int64_t row, int head, int c, int n, const float *part, const float *ml, int head_dim, int stride) {
-  constexpr int kRun = 8;  // parts that are asked for at a time
+  constexpr int kRun = BEFORE ? 16 : 8;  // parts that are asked for at a time
   float top = -INFINITY, sum = 0.0f;
   f32x4 v{0, 0, 0, 0};
   for (int i0 = 0; i0 < n; i0 += kRun) {

@@ -182,7 +182,7 @@ __device__ inline bool find_piece(const CacheDev &d, const CacheQuery &q, const 
   for (int o = 1; o < 64; o <<= 1) longest = fmaxf(longest, __shfl_xor(longest, o));
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   // (never less than an even share: scratch has room for twice as many parts as there are workers, as in cache_attend.hip)
-  const uint32_t share = max(1u, (all * (uint32_t)d.kv_heads + workers - 1) / workers), size = share > 1 ? piece_steps(steps, n, d.kv_heads, share, workers) : 1;
+  const uint32_t share = max(1u, (all * (uint32_t)d.kv_heads + workers - 1) / workers), size = share > 1 ? piece_steps(steps, n, d.kv_heads, share, workers, SIGHT ? 1 : 0) : 1;
   // pieces from the longest on, by eighths: what comes last then fills what is left
   const float one_over = 1.0f / (float)size, per_class = kClasses / fminf((float)size, longest);
   uint32_t before = 0, parts_before = 0;
@@ -594,12 +594,13 @@ __global__ __launch_bounds__(256) void k_cache_join_many(CacheDev d, CacheQuery 
   if (parts < 2 || !__any(row < min(q.share * sp.count - tile * tile_rows, tile_rows))) return;
   const float *ml = d.part_ml + ((int64_t)first * WAVES + wave) * 128 + lane * 2, *p = d.part + ((int64_t)first * WAVES + wave) * (1024 * NC) + c * 1024 + lane * 2;
   float m = -INFINITY;
+#pragma unroll 8
   for (uint32_t i = 0; i < parts; ++i) m = fmaxf(m, ml[i * WAVES * 128]);
   float l = 0.0f;
   f32x16 o;
 #pragma unroll
   for (int e = 0; e < 16; ++e) o[e] = 0.0f;
-#pragma unroll 2
+#pragma unroll 4
   for (uint32_t i = 0; i < parts; ++i) {
     const float2 at = *reinterpret_cast<const float2 *>(ml + i * WAVES * 128);
     const float by = at.x == -INFINITY && m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(at.x - m);
