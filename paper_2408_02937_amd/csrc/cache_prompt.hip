@@ -2,8 +2,8 @@
 //
 // The formulas are those of cache_attend.hip; here arithmetic bounds: 4 * head_dim flops for a row and token.  A workgroup has
 // 32 rows for each wavefront (a row: a token's query head of those that share a kv head) and goes over the tokens that they see
-// 64 at a time (32 where head_dim is 256): all its lanes turn their codes into halves in LDS, once for all rows, while the loads of the next
-// tokens are under way; two buffers, one barrier.  Scores are S^T = K Q^T with Q in registers; a lane has one row's scores and its
+// 64 at a time (32 where head_dim is 256): their codes come to LDS as they are, by copies that run three tiles ahead, and all lanes turn them into
+// halves, again in LDS, once for all rows, a tile ahead of the products; one barrier a tile.  Scores are S^T = K Q^T with Q in registers; a lane has one row's scores and its
 // probabilities are the operand that O^T = V^T P^T takes.  The running maximum enters as the start of the scores' sums and moves
 // only where a score has left it far behind (kLag).  LDS holds operands in the order in which the lanes take them, 16 bytes each; the slots are
 // swapped so that writing meets no bank twice.  Where rows are too few to fill the chip the tokens are split, and the last
@@ -16,7 +16,13 @@
 // of 8,192 squared reaches 1,140 in bfloat16 and 1,084 in halves.  Vector instructions (exponentials, masks, codes) take 48 % of the cycles, matrix
 // instructions 41 %, and two wavefronts of a SIMD overlap them in part.  Heads of 64, 96, 128, 256 on one card: 455, 551, 640, 2,314 us; 604, 749, 859,
 // 475 TFLOP/s: the fewer the channels, the more exponentials for a flop; at 256 one wavefront fits a SIMD.  At 128 channels, on a card of 580 us:
-// 4 wavefronts a workgroup 710, wavefronts half a tile apart 610.
+// 4 wavefronts a workgroup 710, wavefronts half a tile apart 610.  (Codes that are loaded into registers a tile ahead: 609 us, with copies 607 on that card.)
+// What bounds it: a tile of 64 tokens takes a compute unit 2.5 us, of which products and exponentials alone take 1.9, 0.93 of them the matrix instructions' own
+// time; at their full rate they would read LDS at its own.  With the SIMD's two wavefronts changing places between matrix and vector instructions behind a
+// barrier each 252 us where 206 are taken here, with the next tile's scores between this one's exponentials 226 (252 rows behind 4 sequences of up to 60,063).
+//
+// With a sight (CacheSight: sinks, trees) a tile's tokens are counted without those between the sinks and the window; what a row sees of 32 tokens are
+// the bits of a word.  Parts of rows are joined by a launch of their own.  8,192 rows under a window of 1,000 with 64 sinks: 204 us for 133 GFLOP.
 #include "../../include/rtams_cache.h"
 
 #include <climits>
@@ -35,13 +41,15 @@ constexpr int tile_blocks(int head_dim) { return head_dim == 256 ? 1 : 2; }  // 
 constexpr int kRows = 256;       // of a workgroup's parts at most
 
 // Workgroups that a compute unit runs at once: registers decide.
-constexpr int at_once(int head_dim, int waves) { return waves == 8 || head_dim == 256 ? 1 : waves == 4 ? 2 : 3; }
+constexpr int at_once(int head_dim, int waves) { return waves == 8 || head_dim == 256 ? 1 : 2; }
 
-template <int D, int TB, int RING>
+constexpr int kRing = 4;  // tiles on their way or being unpacked
+
+template <int D, int TB>
 struct Staging {  // tiles in LDS: operands of 16 bytes
-  uint4 k[2][TB * 4 * D];  // [block][word][token]
-  uint4 v[2][TB * 4 * D];  // [block][32 channels][lane group][channel]
-  uint4 raw[RING > 0 ? RING : 1][RING > 0 ? TB * 40 * D / 16 : 1];  // with a ring: tiles as the cache holds them, on their way
+  uint4 k[2][TB * 4 * D];            // [block][word][token]
+  uint4 v[2][TB * 4 * D];            // [block][32 channels][lane group][channel]
+  uint4 raw[kRing][TB * 40 * D / 16];  // as the cache holds them
 };
 
 __device__ inline int key_slot(int word, int token) { return token ^ (((word >> 1) & 7) << 1); }
@@ -158,9 +166,9 @@ constexpr int kSplit = 4;
 constexpr int kMostEntries = 1024;  // row tiles of items that are planned
 constexpr int kClasses = 8;         // of their pieces, by length
 
-template <int D, int TB, int RING>
+template <int D, int TB>
 union Shared {
-  Staging<D, TB, RING> tile;
+  Staging<D, TB> tile;
   float steps[kMostEntries];  // in front of them
 };
 
@@ -216,9 +224,6 @@ __device__ __forceinline__ void reads_ahead() {
   __builtin_amdgcn_sched_group_barrier(kMfma, kAhead, 0);
 }
 
-// The copies of a workgroup's tiles into its ring, in chunks of 1 KiB, one to a wavefront after the other: a wavefront has as many of each tile.
-constexpr int kRing = 4;  // tiles on their way or in use
-
 // The other wavefronts' writes to LDS, and copies that they waited for, are there.  (Not __syncthreads: that would wait for all copies.)
 __device__ __forceinline__ void meet() {
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -231,9 +236,8 @@ __device__ __forceinline__ void attend_many(const CacheDev &d, const CacheQuery 
   constexpr int kLanes = WAVES * 64, NS = D / 16, NC = D / 32, NP = (2 * kPairs<D, TB> + kLanes - 1) / kLanes;
   constexpr int kTile = TB * kBlockTokens;
   extern __shared__ uint4 lds[];
-  constexpr int RING = SIGHT ? kRing : 0;
-  Shared<D, TB, RING> &shared = *reinterpret_cast<Shared<D, TB, RING> *>(lds);
-  Staging<D, TB, RING> &sh = shared.tile;
+  Shared<D, TB> &shared = *reinterpret_cast<Shared<D, TB> *>(lds);
+  Staging<D, TB> &sh = shared.tile;
   __shared__ Piece piece;
   __shared__ int flag;
   Piece pc;
@@ -319,24 +323,7 @@ __device__ __forceinline__ void attend_many(const CacheDev &d, const CacheQuery 
   };
   // (with a sight a tile's tokens are counted from the first one on, without those between the sinks and the window)
   const int sinks = SIGHT ? sink_blocks(g) : 0;
-  const auto place = [&](int at) { return at >= sinks ? at + from : at; };
-  Words<D> next[NP];
-  const auto load_tile = [&](Words<D> (&to)[NP], int t) {
-    const int block = (SIGHT ? place(t * kTile) : from + t * kTile) / kBlockTokens;
-    const unsigned char *b0 = block_at(block), *b1 = TB == 2 ? block_at(SIGHT ? place(t * kTile + kBlockTokens) / kBlockTokens : block + 1) : b0;
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const int u = i * kLanes + threadIdx.x;
-      if (2 * kPairs<D, TB> % kLanes == 0 || u < 2 * kPairs<D, TB>) load_words<D, TB>(to[i], u, b0, b1);
-    }
-  };
-  const auto put_tile = [&](const Words<D> (&of)[NP], uint4 *k, uint4 *v) {
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const int u = i * kLanes + threadIdx.x;
-      if (2 * kPairs<D, TB> % kLanes == 0 || u < 2 * kPairs<D, TB>) put_words<D, TB>(of[i], u, k, v);
-    }
-  };
+  const auto place = [&](int at) { return !SIGHT || at >= sinks ? at + from : at; };
   f32x16 sc[TB];
   half8 pf[TB][2];
   const auto scores = [&](const uint4 *kt) {
@@ -428,82 +415,67 @@ __device__ __forceinline__ void attend_many(const CacheDev &d, const CacheQuery 
         }
     reads_ahead<NC * TB * 2>();
   };
-  const auto compute = [&](int t, int now) {
-    const int tok0 = SIGHT ? place(t * kTile) : from + t * kTile;
-    const int tok1 = SIGHT && TB == 2 ? place(t * kTile + kBlockTokens) : tok0;
-    const auto seen = [&](int tok) { return tok < any_to && (tok + kBlockTokens > any_from || tok < g.sinks); };
-    const bool some = SIGHT ? seen(tok0) || seen(tok1) : tok0 < any_to && tok0 + kTile > any_from;
-    if (some) {
+  if (length > 0) {  // (an empty sequence has one step and no page)
+    // A tile is copied in chunks of 1 KiB, one to a wavefront after the other.
+    constexpr int kChunks = (40 * D + 1023) / 1024, kAll = TB * kChunks, kMost = (kAll + WAVES - 1) / WAVES, kLess = kAll / WAVES;
+    const uint32_t ring = (uint32_t)uniform((int)lds_address(sh.raw[0]));
+    const auto copy = [&](int t) {
+      const uint32_t slot = ring + (uint32_t)(t - t0) % kRing * (TB * 40 * D);
+#pragma unroll
+      for (int i = 0; i < kMost; ++i) {
+        const int c = i * WAVES + wave, x = c / kChunks, at = c % kChunks * 1024;
+        if (i < kLess || c < kAll) {
+          const unsigned char *blk = block_at(place(t * kTile + x * kBlockTokens) / kBlockTokens);
+          if (40 * D % 1024 == 0 || lane * 16 < 40 * D - at) copy_to_lds(blk + at, slot + x * (40 * D) + at, lane * 16);
+        }
+      }
+    };
+    // This wavefront's chunks are there, but those of the `later` tiles that it asked for last.
+    const auto arrived = [&](auto later) {
+      constexpr int kLater = decltype(later)::value;
+      if (kMost == kLess || wave < kAll % WAVES) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kMost * kLater) : "memory");
+      else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLess * kLater) : "memory");
+    };
+    const auto unpack = [&](int t) {
+      const unsigned char *b0 = reinterpret_cast<const unsigned char *>(sh.raw[(uint32_t)(t - t0) % kRing]), *b1 = b0 + (TB == 2 ? 40 * D : 0);
+      uint4 *const k = sh.k[(t - t0) & 1], *const v = sh.v[(t - t0) & 1];
+      Words<D> words[NP];
+      constexpr bool kWhole = 2 * kPairs<D, TB> % kLanes == 0;
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        const int u = i * kLanes + threadIdx.x;
+        if (kWhole || u < 2 * kPairs<D, TB>) load_words<D, TB>(words[i], u, b0, b1);
+      }
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        const int u = i * kLanes + threadIdx.x;
+        if (kWhole || u < 2 * kPairs<D, TB>) put_words<D, TB>(words[i], u, k, v);
+      }
+    };
+    for (int i = 0; i < kRing - 1; ++i)
+      if (t0 + i < t1) copy(t0 + i);
+    if (t0 + kRing - 1 <= t1) arrived(std::integral_constant<int, kRing - 2>());
+    else arrived(std::integral_constant<int, 0>());
+    meet();
+    unpack(t0);
+    if (t0 + kRing - 1 < t1) copy(t0 + kRing - 1);
+    for (int t = t0; t < t1; ++t) {
+      if (t + kRing <= t1) arrived(std::integral_constant<int, kRing - 2>());
+      else arrived(std::integral_constant<int, 0>());
+      meet();  // (tile t is unpacked, the next one's codes are there, and what this turn writes over has been read)
+      if (t + kRing < t1) copy(t + kRing);
+      if (t + 1 < t1) unpack(t + 1);
+      const int tok0 = place(t * kTile), tok1 = SIGHT && TB == 2 ? place(t * kTile + kBlockTokens) : tok0;
+      const auto seen = [&](int tok) { return tok < any_to && (tok + kBlockTokens > any_from || tok < g.sinks); };
+      if (SIGHT ? !(seen(tok0) || seen(tok1)) : !(tok0 < any_to && tok0 + kTile > any_from)) continue;
       // (matrix instructions first: the other wavefront of the SIMD has its exponentials beside them)
       __builtin_amdgcn_s_setprio(1);
-      scores(sh.k[now]);
+      scores(sh.k[(t - t0) & 1]);
       __builtin_amdgcn_s_setprio(0);
       probabilities(tok0, tok1);
       __builtin_amdgcn_s_setprio(1);
-      weigh(sh.v[now]);
+      weigh(sh.v[(t - t0) & 1]);
       __builtin_amdgcn_s_setprio(0);
-    }
-  };
-  if constexpr (SIGHT) {
-    if (length > 0) {
-      constexpr int kChunks = (40 * D + 1023) / 1024, kAll = TB * kChunks, kMost = (kAll + WAVES - 1) / WAVES, kLess = kAll / WAVES;
-      const uint32_t ring = (uint32_t)uniform((int)lds_address(sh.raw[0]));
-      const auto copy = [&](int t) {
-        const uint32_t slot = ring + (uint32_t)(t - t0) % kRing * (TB * 40 * D);
-#pragma unroll
-        for (int i = 0; i < kMost; ++i) {
-          const int c = i * WAVES + wave, x = c / kChunks, at = c % kChunks * 1024;
-          if (i < kLess || c < kAll) {
-            const unsigned char *blk = block_at(place(t * kTile + x * kBlockTokens) / kBlockTokens);
-            if (40 * D % 1024 == 0 || lane * 16 < 40 * D - at) copy_to_lds(blk + at, slot + x * (40 * D) + at, lane * 16);
-          }
-        }
-      };
-      // all but the last `tiles` tiles that this wavefront asked for are there
-      const auto arrived = [&](auto tiles) {
-        constexpr int kTiles = decltype(tiles)::value;
-        if (kMost == kLess || wave < kAll % WAVES) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kMost * kTiles) : "memory");
-        else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLess * kTiles) : "memory");
-      };
-      const auto unpack = [&](int t) {
-        const unsigned char *b0 = reinterpret_cast<const unsigned char *>(sh.raw[(uint32_t)(t - t0) % kRing]), *b1 = b0 + (TB == 2 ? 40 * D : 0);
-#pragma unroll
-        for (int i = 0; i < NP; ++i) {
-          const int u = i * kLanes + threadIdx.x;
-          if (2 * kPairs<D, TB> % kLanes == 0 || u < 2 * kPairs<D, TB>) load_words<D, TB>(next[i], u, b0, b1);
-        }
-        put_tile(next, sh.k[(t - t0) & 1], sh.v[(t - t0) & 1]);
-      };
-      for (int i = 0; i < kRing - 1; ++i)
-        if (t0 + i < t1) copy(t0 + i);
-      if (t0 + kRing - 1 <= t1) arrived(std::integral_constant<int, kRing - 2>());
-      else arrived(std::integral_constant<int, 0>());
-      meet();
-      unpack(t0);
-      if (t0 + kRing - 1 < t1) copy(t0 + kRing - 1);
-      for (int t = t0; t < t1; ++t) {
-        if (t + kRing <= t1) arrived(std::integral_constant<int, kRing - 2>());
-        else arrived(std::integral_constant<int, 0>());
-        meet();  // (tile t is unpacked, the next one's codes are there, and what this turn writes over has been read)
-        if (t + kRing < t1) copy(t + kRing);
-        if (t + 1 < t1) unpack(t + 1);
-        compute(t, (t - t0) & 1);
-      }
-    }
-  } else if (length > 0) {  // (an empty sequence has one step and no page)
-    {
-      Words<D> first[NP];
-      load_tile(first, t0);
-      if (t0 + 1 < t1) load_tile(next, t0 + 1);
-      put_tile(first, sh.k[0], sh.v[0]);
-    }
-    __syncthreads();
-    for (int t = t0; t < t1; ++t) {
-      const int now = (t - t0) & 1;
-      if (t + 1 < t1) put_tile(next, sh.k[now ^ 1], sh.v[now ^ 1]);
-      if (t + 2 < t1) load_tile(next, t + 2);
-      compute(t, now);
-      __syncthreads();
     }
   }
   l += __shfl_xor(l, 32);
@@ -579,8 +551,8 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt_s
   attend_many<D, WAVES, TB, true>(d, q, g, tiles, tile_rows, split, first);
 }
 
-// Joins what several workgroups have of a row tile: a wavefront has 32 channels of 32 rows, held as they lie in the parts.  (By the last
-// workgroup to arrive, as k_cache_prompt does it, a part is 128 KiB that one compute unit reads: JOIN_FIGURES)
+// Joins what several workgroups have of a row tile: a wavefront has 32 channels of 32 rows, held as they lie in the parts.  (Up to 32 parts of 128 KiB
+// are too much for the last workgroup to arrive, as in k_cache_prompt: 252 rows behind one sequence of 32,000 took 119 us so, and take 69.)
 template <int D, int WAVES>
 __global__ __launch_bounds__(256) void k_cache_join_many(CacheDev d, CacheQuery q, CacheSight g, int tiles, int tile_rows) {
   constexpr int NC = D / 32, kUnit = WAVES * NC;
@@ -630,8 +602,8 @@ void launch(const CacheDev &d, const CacheQuery &q, const CacheSight *g, hipStre
   const int64_t all = split ? groups + kWorkers : groups, most = 1 << 22;  // (of a launch; one that finds no rows takes 10 ns: 512 items of 8 heads, one of 32,768 rows, 28 ms of which it takes 6)
   for (int64_t at = 0; at < all; at += most) {
     const uint32_t grid = (uint32_t)(all - at < most ? all - at : most);
-    if (g) k_cache_prompt_sight<D, WAVES, TB><<<grid, WAVES * 64, sizeof(Shared<D, TB, kRing>), s>>>(d, q, *g, tiles, tile_rows, split, (uint32_t)at);
-    else if constexpr (TB == tile_blocks(D) && WAVES == (D == 256 ? 4 : 8)) k_cache_prompt<D, WAVES><<<grid, WAVES * 64, sizeof(Shared<D, TB, 0>), s>>>(d, q, tiles, tile_rows, split, (uint32_t)at);
+    if (g) k_cache_prompt_sight<D, WAVES, TB><<<grid, WAVES * 64, sizeof(Shared<D, TB>), s>>>(d, q, *g, tiles, tile_rows, split, (uint32_t)at);
+    else if constexpr (TB == tile_blocks(D) && WAVES == (D == 256 ? 4 : 8)) k_cache_prompt<D, WAVES><<<grid, WAVES * 64, sizeof(Shared<D, TB>), s>>>(d, q, tiles, tile_rows, split, (uint32_t)at);
   }
   if (g && split) k_cache_join_many<D, WAVES><<<(uint32_t)(groups * WAVES * (D / 32) / 4), 256, 0, s>>>(d, q, *g, tiles, tile_rows);
 }
@@ -640,10 +612,12 @@ void launch(const CacheDev &d, const CacheQuery &q, const CacheSight *g, hipStre
 
 // Rows of parts: at most two pieces that are parts for each that runs at once.
 size_t cache_prompt_part_rows() { return (size_t)2 * kUnits * kRows; }
-size_t cache_prompt_groups() { return (size_t)8 * kUnits; }
+size_t cache_prompt_groups() { return (size_t)4 * kUnits; }
 
 void launch_cache_prompt(const CacheDev &d, const CacheQuery &q, const CacheSight *g, hipStream_t s) {
-  const bool few = g && (int64_t)q.share * q.r.max_new <= 128;  // FEW_FIGURES
+  // Workgroups of 4 wavefronts, two to a unit, against 8: 128 rows of 128 channels, 8 heads, 16 sequences of up to 6,001, 4 of up to 60,063, 32 of up to 2,000,
+  // one of 32,000: 67, 148, 56, 67 us and 86, 156, 67, 59; of 64 channels 50, 109, 41, 59 and 67, 121, 52, 49; 252 rows of the first: 120 and 105.
+  const bool few = g && (int64_t)q.share * q.r.max_new <= 128;
   switch (d.head_dim) {
     case 64: return few ? launch<64, 4, 1>(d, q, g, s) : launch<64, 8, 2>(d, q, g, s);
     case 96: return few ? launch<96, 4, 1>(d, q, g, s) : launch<96, 8, 2>(d, q, g, s);
@@ -653,15 +627,16 @@ void launch_cache_prompt(const CacheDev &d, const CacheQuery &q, const CacheSigh
 }
 
 hipError_t allow_large_lds_cache_prompt() {
-  const auto allow = [](const void *f, size_t bytes) { return hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes); };
-  hipError_t e = allow(reinterpret_cast<const void *>(k_cache_prompt<128, 8>), sizeof(Shared<128, 2, 0>));
-  if (e == hipSuccess) e = allow(reinterpret_cast<const void *>(k_cache_prompt<256, 4>), sizeof(Shared<256, 1, 0>));
-  const auto allow_sight = [&](auto kernel, size_t bytes) {
-    if (e == hipSuccess) e = allow(reinterpret_cast<const void *>(kernel), bytes);
+  hipError_t e = hipSuccess;
+  const auto allow = [&](auto kernel, size_t bytes) {
+    if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
   };
-  allow_sight(k_cache_prompt_sight<96, 8, 2>, sizeof(Shared<96, 2, kRing>));
-  allow_sight(k_cache_prompt_sight<128, 8, 2>, sizeof(Shared<128, 2, kRing>));
-  allow_sight(k_cache_prompt_sight<256, 4, 1>, sizeof(Shared<256, 1, kRing>));
+  allow(k_cache_prompt<96, 8>, sizeof(Shared<96, 2>));
+  allow(k_cache_prompt<128, 8>, sizeof(Shared<128, 2>));
+  allow(k_cache_prompt<256, 4>, sizeof(Shared<256, 1>));
+  allow(k_cache_prompt_sight<96, 8, 2>, sizeof(Shared<96, 2>));
+  allow(k_cache_prompt_sight<128, 8, 2>, sizeof(Shared<128, 2>));
+  allow(k_cache_prompt_sight<256, 4, 1>, sizeof(Shared<256, 1>));
   return e;
 }
 
