@@ -305,15 +305,21 @@ __global__ __launch_bounds__(kPlanLanes) void k_cache_keep_plan(CacheDev d, Cach
       bad = 1;
       continue;
     }
-    for (int j = 0, before = -1, looked = -1; j < k; ++j) {
-      const int p = path[first + j], page = (base + j) / d.page_tokens;
-      bad |= p <= before || p >= count;
-      before = p;
-      if (p != j && page != looked) {  // (another sequence's rows are not written over)
-        bad |= d.refs[d.table[(int64_t)s * d.max_pages + page]] != 1;
-        looked = page;
+    int before = -1, moved = k;  // (the first row that moves: those behind it do)
+    for (int j = 0; j < k; j += 8) {
+      int p[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e] = path[first + min(j + e, k - 1)];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (j + e >= k) break;
+        bad |= p[e] <= before || p[e] >= count;
+        before = p[e];
+        if (p[e] != j + e) moved = min(moved, j + e);
       }
     }
+    // (another sequence's rows are not written over)
+    for (int page = (base + moved) / d.page_tokens; moved < k && page <= (base + k - 1) / d.page_tokens; ++page) bad |= d.refs[d.table[(int64_t)s * d.max_pages + page]] != 1;
     d.items[i] = CacheItem{s, base, pages_for(d, length), pages_for(d, (int64_t)base + k), (uint32_t)k, count, {}};
   }
   if (__syncthreads_or(bad)) return drop(d, RTAMS_EINVAL);

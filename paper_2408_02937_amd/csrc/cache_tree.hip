@@ -17,6 +17,36 @@ constexpr int kLanes = 256;
 constexpr int kMostRows = 1024;  // of a tree
 
 // ------------------------------------------------------------------ parents to ancestors
+// Up to 64 rows, a row to a lane of one wavefront: no LDS, no barriers.  48 trees of 31 rows: TREE_FIGURES
+__global__ __launch_bounds__(64) void k_cache_tree_few(CacheDev d, CacheRows r, const int32_t *parents, uint32_t *tree, int words, int32_t *positions) {
+  const int item = blockIdx.x, seq = cache_item_seq(r, item), j = threadIdx.x;
+  int64_t row0;
+  int count;
+  bool bad = !cache_item_rows(r, item, &row0, &count) || (uint32_t)seq >= (uint32_t)d.max_seqs;
+  const int length = d.lengths[bad ? 0 : seq];
+  bad = bad || count > length;
+  int up = !bad && j < count ? parents[row0 + j] : -1;
+  bad |= up < -1 || up >= j;
+  if (__any(bad)) {
+    if (j == 0) cache_raise(d, RTAMS_EINVAL);
+    return;
+  }
+  uint32_t low = j < 32 ? 1u << j : 0, high = j < 32 ? 0 : 1u << (j - 32);
+  while (__any(up >= 0)) {
+    const int from = max(up, 0);
+    const uint32_t more_low = (uint32_t)__shfl((int)low, from), more_high = (uint32_t)__shfl((int)high, from);
+    const int next = __shfl(up, from);
+    if (up >= 0) {
+      low |= more_low;
+      high |= more_high;
+      up = next;
+    }
+  }
+  if (j >= count) return;
+  for (int w = 0; w < words; ++w) tree[(row0 + j) * words + w] = w == 0 ? low : w == 1 ? high : 0;
+  if (positions) positions[row0 + j] = length - count + __popc(low) + __popc(high) - 1;
+}
+
 __global__ __launch_bounds__(kLanes) void k_cache_tree(CacheDev d, CacheRows r, const int32_t *parents, uint32_t *tree, int words, int32_t *positions) {
   extern __shared__ uint32_t kin[];  // [count][words]
   __shared__ int32_t points[2][kMostRows];
@@ -72,10 +102,11 @@ __global__ __launch_bounds__(kLanes) void k_cache_tree(CacheDev d, CacheRows r, 
 }
 
 // ------------------------------------------------------------------ the path of the choices
+// EACH rows to a lane.
+template <int EACH>
 __global__ __launch_bounds__(64) void k_cache_walk(CacheDev d, CacheRows r, const int32_t *parents, const int32_t *tokens, const int32_t *chosen, int32_t *path,
                                                    int32_t *kept, int32_t *next) {
-  constexpr int kEach = kMostRows / 64;
-  __shared__ int32_t choice[kMostRows];
+  __shared__ int32_t choice[64 * EACH];
   const int item = blockIdx.x, lane = threadIdx.x;
   int64_t row0;
   int count;
@@ -86,20 +117,24 @@ __global__ __launch_bounds__(64) void k_cache_walk(CacheDev d, CacheRows r, cons
     }
     return;
   }
-  for (int j = lane; j < count; j += 64) choice[j] = chosen[row0 + j];
+  int from[EACH], token[EACH];
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    const int j = i * 64 + lane;
+    from[i] = token[i] = -1;
+    if (j < count) {
+      from[i] = parents[row0 + j];
+      token[i] = tokens[row0 + j];
+      choice[j] = chosen[row0 + j];
+    }
+  }
   __syncthreads();
-  int from[kEach];  // the parent of row lane + 64 i, if it is what was chosen there
   bool bad = false;
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) {
-    const int j = i * 64 + lane;
-    from[i] = -1;
-    if (j < count) {
-      const int p = parents[row0 + j], t = tokens[row0 + j];
-      const bool right = p >= -1 && p < j;
-      bad |= !right;
-      if (right && p >= 0 && t >= 0 && choice[p] == t) from[i] = p;
-    }
+  for (int i = 0; i < EACH; ++i) {  // from: the parent of row lane + 64 i, if it is what was chosen there
+    const bool right = from[i] >= -1 && from[i] < i * 64 + lane;
+    bad |= !right;
+    if (!right || from[i] < 0 || token[i] < 0 || choice[right ? max(from[i], 0) : 0] != token[i]) from[i] = -1;
   }
   bad = __any(bad);
   int len = 0, last = -1;
@@ -109,7 +144,7 @@ __global__ __launch_bounds__(64) void k_cache_walk(CacheDev d, CacheRows r, cons
       if (lane == 0) path[row0 + len - 1] = last;
       int found = -1;
 #pragma unroll
-      for (int i = 0; i < kEach; ++i) {
+      for (int i = 0; i < EACH; ++i) {
         const uint64_t who = found < 0 && i * 64 < count ? __ballot(from[i] == last) : 0;
         if (who) found = i * 64 + __ffsll((unsigned long long)who) - 1;
       }
@@ -135,12 +170,13 @@ __global__ __launch_bounds__(kLanes) void k_cache_keep(CacheDev d, CacheRows r, 
   __shared__ int first_moved;
   const uint32_t u0 = first_unit + blockIdx.x, head = u0 % d.kv_heads, rest = u0 / d.kv_heads;
   const int layer = rest % d.layers, item = rest / d.layers;
-  if (!d.ctrl->ok) return;
+  const uint32_t ok = d.ctrl->ok;
   const CacheItem it = d.items[item];
+  const int64_t row0 = r.starts ? r.starts[item] : item;
+  if (!ok) return;
   const int base = uniform(it.src), kept = uniform(it.off), count = uniform(it.copy), seq = uniform(it.seq);
   if (threadIdx.x == 0) first_moved = kMostRows;
   __syncthreads();
-  const int64_t row0 = r.starts ? r.starts[item] : item;
   const int page0 = base / d.page_tokens;
   for (int j = threadIdx.x; j < kept; j += kLanes) {
     const int p = path[row0 + j];
@@ -219,12 +255,16 @@ __global__ __launch_bounds__(kLanes) void k_cache_keep(CacheDev d, CacheRows r, 
 }  // namespace
 
 void launch_cache_tree(const CacheDev &d, const CacheRows &r, const int32_t *parents, uint32_t *tree, int words, int32_t *positions, hipStream_t s) {
-  k_cache_tree<<<r.n, kLanes, (size_t)r.max_new * words * 4, s>>>(d, r, parents, tree, words, positions);
+  if (r.max_new <= 64) k_cache_tree_few<<<r.n, 64, 0, s>>>(d, r, parents, tree, words, positions);
+  else k_cache_tree<<<r.n, kLanes, (size_t)r.max_new * words * 4, s>>>(d, r, parents, tree, words, positions);
 }
 
 void launch_cache_walk(const CacheDev &d, const CacheRows &r, const int32_t *parents, const int32_t *tokens, const int32_t *chosen, int32_t *path, int32_t *kept,
                        int32_t *next, hipStream_t s) {
-  k_cache_walk<<<r.n, 64, 0, s>>>(d, r, parents, tokens, chosen, path, kept, next);
+  const auto go = [&](auto kernel) { kernel<<<r.n, 64, 0, s>>>(d, r, parents, tokens, chosen, path, kept, next); };
+  if (r.max_new <= 64) go(k_cache_walk<1>);
+  else if (r.max_new <= 256) go(k_cache_walk<4>);
+  else go(k_cache_walk<kMostRows / 64>);
 }
 
 void launch_cache_keep(const CacheDev &d, const CacheRows &r, const int32_t *path, const int32_t *kept, hipStream_t s) {
