@@ -5,6 +5,9 @@ requests is searched for; each request forks the sequence of its best passage (p
 page that is part full), appends its question (a short prompt) and decodes tokens in a recorded HIP graph; then its pages are
 freed.  Some passages are replaced in between, and the pages compacted.  The network is a stack of attention layers
 with random weights: what is timed is the path, not what it says.
+
+The same network answers by trees of drafted tokens too: each token's most likely followers, as `score` last gave them, make a tree behind
+the token that was chosen last; one pass attends to all of it, the path that the choices follow stays in the cache, the rest is cut.
 """
 from __future__ import annotations
 
@@ -14,6 +17,7 @@ import torch
 
 from . import rtams, synth
 from .cache import Cache
+from .logits import score
 
 
 class Stack:
@@ -28,21 +32,124 @@ class Stack:
         self.layers = [{"qkv": w(width, (heads + 2 * kv_heads) * head_dim), "out": w(width, width), "up": w(width, 2 * width),
                         "down": w(2 * width, width)} for _ in range(layers)]
 
-    def __call__(self, cache: Cache, ids: torch.Tensor, seqs: torch.Tensor, starts=None, max_new=None) -> torch.Tensor:
-        """The rows' states after all layers; room for them has been made."""
+    def __call__(self, cache: Cache, ids: torch.Tensor, seqs: torch.Tensor, starts=None, max_new=None, tree=None) -> torch.Tensor:
+        """The rows' states after all layers; room for them has been made.  tree: what drafted rows see of each other."""
         norm = lambda x: torch.nn.functional.layer_norm(x, x.shape[-1:])
         x = self.tokens[ids]
         for i, w in enumerate(self.layers):
             qkv = (norm(x) @ w["qkv"]).view(len(ids), -1, self.head_dim)  # queries, keys and values are views of one tensor
             q, k, v = qkv.split([self.heads, self.kv_heads, self.kv_heads], 1)
             cache.write(i, k, v, seqs, starts, max_new)
-            a = cache.attend(i, q, seqs, starts, max_new)
+            a = cache.attend(i, q, seqs, starts, max_new, tree=tree)
             x = x + a.view(len(ids), -1) @ w["out"]
             x = x + torch.nn.functional.gelu(norm(x) @ w["up"]) @ w["down"]
         return norm(x)
 
     def next_ids(self, x: torch.Tensor) -> torch.Tensor:
         return (x @ self.tokens.t()).argmax(-1)
+
+
+# A draft: node 0 is the token chosen last; node j follows node PARENTS[j] and is its RANKS[j]-th most likely follower.
+PARENTS = (-1, 0, 0, 1, 2, 3, 1)
+RANKS = (0, 0, 1, 0, 0, 0, 1)
+
+
+class Drafts:
+    """Answers by trees of drafted tokens: the state of some requests, and a step that can be recorded."""
+
+    def __init__(self, net: Stack, cache: Cache, seqs: torch.Tensor, ids: torch.Tensor, vocab: int):
+        dev, n, nodes = ids.device, len(ids), len(PARENTS)
+        self.net, self.cache, self.seqs, self.ids = net, cache, seqs, ids  # ids: the tokens chosen last, int32
+        self.followers = torch.zeros((n, vocab, max(RANKS) + 1), dtype=torch.int32, device=dev)  # of each request's tokens
+        self.parents = _ints(PARENTS * n, dev)
+        self.starts = _ints(range(0, n * nodes + 1, nodes), dev)
+        self.request = torch.arange(n, device=dev)
+        self.drafted = torch.zeros((n, nodes), dtype=torch.int32, device=dev)
+        self.chosen, self.path = (torch.zeros((n, nodes), dtype=torch.int32, device=dev) for _ in range(2))
+        self.kept = torch.zeros(n, dtype=torch.int32, device=dev)
+        self.logprobs = torch.zeros((n, nodes), device=dev)
+
+    def step(self) -> None:
+        args = (self.seqs, self.starts, len(PARENTS))
+        self.drafted[:, 0] = self.ids
+        for j in range(1, len(PARENTS)):
+            self.drafted[:, j] = self.followers[self.request, self.drafted[:, PARENTS[j]].long(), RANKS[j]]
+        self.cache.extend(self.seqs, self.starts)
+        tree, _ = self.cache.tree(self.parents, *args)
+        x = self.net(self.cache, self.drafted.flatten().long(), *args, tree=tree)
+        said = score(x @ self.net.tokens.t(), top=max(RANKS) + 1)
+        top = said.top.view(*self.drafted.shape, -1)
+        for j in range(len(PARENTS)):  # (one node after the other: of a token that is there twice the last one counts)
+            self.followers[self.request, self.drafted[:, j].long()] = top[:, j]
+        self.chosen.copy_(top[..., 0])
+        self.logprobs.copy_(said.top_logprobs[:, 0].view_as(self.logprobs))
+        path, kept, following = self.cache.walk(self.parents, self.drafted.flatten(), self.chosen.flatten(), self.starts, len(PARENTS))
+        self.cache.keep(path, kept, *args)
+        self.path.copy_(path.view_as(self.path))
+        self.kept.copy_(kept)
+        self.ids.copy_(following)
+
+
+def drafted_answers(net: Stack, requests: int, steps: int, page_tokens: int, vocab: int, record: bool = True, seed: int = 7) -> dict:
+    """Prompts answered a token at a time, and by drafts from the same pages."""
+    dev = net.tokens.device
+    rng = torch.Generator().manual_seed(seed)
+    text = torch.Generator(device=dev).manual_seed(seed)
+    counts = torch.randint(50, 240, (requests,), generator=rng).tolist()
+    longest = 240 + 4 * steps + len(PARENTS)  # a step keeps four tokens at most
+    wide = -(-longest // page_tokens)
+    cache = Cache(net.kv_heads, net.head_dim, layers=len(net.layers), page_tokens=page_tokens, pages=2 * requests * wide, max_seqs=2 * requests, max_pages=wide, device=dev)
+    plain, mine = _ints(range(requests), dev), _ints(range(requests, 2 * requests), dev)
+    st = _starts(counts, dev)
+    cache.extend(plain, st)
+    x = net(cache, torch.randint(0, vocab, (sum(counts),), device=dev, generator=text), plain, st, max(counts))
+    first = score(x[st[1:].long() - 1] @ net.tokens.t(), top=1).top[:, 0].contiguous()
+    cache.fork(plain, mine)
+
+    def timed(step, keep):
+        step()
+        keep(0)
+        torch.cuda.synchronize()
+        graph = None
+        if record:
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                step()
+        t0 = time.perf_counter()
+        for i in range(1, steps):
+            graph.replay() if graph else step()
+            keep(i)
+        torch.cuda.synchronize()
+        return (time.perf_counter() - t0) * 1e3 / max(1, steps - 1)
+
+    ids = first.clone()
+    one = torch.zeros((steps, requests), dtype=torch.int32, device=dev)
+
+    def step():
+        cache.extend(plain)
+        ids.copy_(score(net(cache, ids.long(), plain) @ net.tokens.t(), top=1).top[:, 0])
+
+    ms_one = timed(step, lambda i: one[i].copy_(ids))
+    d = Drafts(net, cache, mine, first.clone(), vocab)
+    chosen, path = (torch.zeros((steps, *d.drafted.shape), dtype=torch.int32, device=dev) for _ in range(2))
+    logprobs = torch.zeros((steps, *d.drafted.shape), device=dev)
+
+    def keep(i):
+        chosen[i], path[i], logprobs[i] = d.chosen, d.path, d.logprobs
+
+    ms = timed(d.step, keep)
+    assert cache.poll_error() == rtams.OK, cache.poll_error()
+    one, chosen, path, logprobs = one.t().tolist(), chosen.tolist(), path.tolist(), logprobs.tolist()
+    said = [[chosen[i][r][j] for i in range(steps) for j in path[i][r] if j >= 0] for r in range(requests)]
+    sure = [logprobs[i][r][j] for r in range(requests) for i in range(steps) for j in path[i][r] if j >= 0]
+    tokens = sum(len(x) for x in said)
+    alike = sum(next((i for i, (a, b) in enumerate(zip(x, y)) if a != b), min(len(x), len(y))) for x, y in zip(said, one))
+    out = {"requests": requests, "steps": steps, "nodes": len(PARENTS), "ms_per_step_of_one": ms_one, "ms_per_step": ms, "tokens_per_step": tokens / (steps * requests),
+           "tokens_per_s_of_one": requests / (ms_one * 1e-3), "tokens_per_s": tokens / steps / (ms * 1e-3), "mean_logprob": sum(sure) / max(1, len(sure)),
+           "alike_before_the_first_difference": alike / max(1, sum(min(len(x), len(y)) for x, y in zip(said, one))), "said_sum": sum(map(sum, said)),
+           "lengths": cache.lengths[requests:].tolist(), "prompts": counts, "said": said}
+    cache.close()
+    return out
 
 
 def _ints(values, device):
@@ -148,4 +255,6 @@ def answers_study(scale: float = 1.0, layers: int = 4, heads: int = 16, kv_heads
     out["tokens_per_s"] = requests / (last["ms_per_step"] * 1e-3)
     index.close()
     cache.close()
+    drafted = drafted_answers(net, requests, steps, page_tokens, vocab, record, seed)
+    out["drafted"] = {k: v for k, v in drafted.items() if k not in ("lengths", "prompts", "said")}
     return out
