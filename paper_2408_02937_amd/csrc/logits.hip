@@ -219,9 +219,20 @@ __device__ void take_best(const char *x, int vocab, int panel, float most, int t
     __syncthreads();
     return sh.count;
   };
-  // The top-th largest of the lanes' largest.
+  // The top-th largest of the lanes' largest; of few, the largest that a wavefront's own lanes have there (if they are as many), which some more reach.
   const auto near = [&]() {
     const uint32_t mine = most > bound ? ordered(most) : 0;
+    if (top <= 32) {
+      int above = 0;
+#pragma unroll
+      for (int j = 0; j < 64; ++j) above += (uint32_t)__builtin_amdgcn_readlane((int)mine, j) > mine;
+      const uint32_t reach = above >= top - 1 && mine ? mine : 0;  // (as many reach these)
+      const uint32_t best = last_lane(wave_reduce_last(reach, [](uint32_t a, uint32_t b) { return a > b ? a : b; }));
+      if ((threadIdx.x & 63) == 0) sh.waves[threadIdx.x >> 6] = best;
+      __syncthreads();
+      const uint32_t most_of = max(max(sh.waves[0], sh.waves[1]), max(sh.waves[2], sh.waves[3]));
+      if (most_of) return unordered(most_of);
+    }
     sh.most[threadIdx.x] = mine;
     if (threadIdx.x == 0) sh.near = ~0u;
     __syncthreads();
@@ -372,17 +383,17 @@ __global__ __launch_bounds__(kLanes, 4) void k_logits(LogitsDev q, int64_t first
     u32x4 raw[kVectors];
     const char *const from = x + (int64_t)panel * kSize;
     const uint32_t own = threadIdx.x * 16;
-    if (panel >= 0 && panel + kPanel <= q.vocab) {
+    if (panel + kPanel <= q.vocab) {
+      // (the first lane's first vector may begin in front of the row: it has another one until it is put together below)
 #pragma unroll
-      for (int v = 0; v < kVectors; ++v) raw[v] = *reinterpret_cast<const u32x4 *>(from + v * kLanes * 16 + own);
-    } else {  // whole vectors, then those that begin in front of the row or end behind it
+      for (int v = 0; v < kVectors; ++v) raw[v] = *reinterpret_cast<const u32x4 *>(from + v * kLanes * 16 + (v == 0 && first < 0 ? 16 : own));
+    } else {
 #pragma unroll
       for (int v = 0; v < kVectors; ++v) {
         const int at = first + v * kLanes * E;
         raw[v] = u32x4{kNone, kNone, kNone, kNone};
         if (at >= 0 && at + E <= q.vocab) raw[v] = *reinterpret_cast<const u32x4 *>(from + v * kLanes * 16 + own);
       }
-      if (first < 0) raw[0] = load_vector<TYPE>(x, first, q.vocab);
       const int last = (q.vocab - panel) / E;  // the panel's vector that the row's end is in
       if (last % kLanes == (int)threadIdx.x && (q.vocab - panel) % E && last < kVectors * kLanes) {
         const u32x4 end = load_vector<TYPE>(x, panel + last * E, q.vocab);
@@ -391,6 +402,7 @@ __global__ __launch_bounds__(kLanes, 4) void k_logits(LogitsDev q, int64_t first
           if (v == last / kLanes) raw[v] = end;
       }
     }
+    if (first < 0) raw[0] = load_vector<TYPE>(x, first, q.vocab);
     const int some = min(kVectors, (q.vocab - panel + kLanes * E - 1) / (kLanes * E));  // vectors that hold some: the others cost nothing
     const float most = largest_of<TYPE>(raw, some);
     move_to(a, fmaxf(a.m, most), q.c);
