@@ -363,7 +363,9 @@ int rtams_cache_attend_sight(rtams_cache *c, const rtams_cache_query *q, const r
   k.lse = q->d_lse;
   k.vec = ((uintptr_t)q->d_q | (uintptr_t)q->d_out) % 16 == 0 && (k.q_row | k.q_head | k.out_row | k.out_head) % 8 == 0;
   if (sight && (sight->sinks || sight->d_tree)) {
+    // (of what is longer than any sequence differences stay within 32 bits)
     const int most_tokens = c->cfg.max_pages * c->cfg.page_tokens;
+    if (k.window > most_tokens) k.window = most_tokens;
     const CacheSight g{sight->sinks < most_tokens ? sight->sinks : most_tokens, sight->tree_words, sight->d_tree};
     launch_cache_attend(c->dev, k, &g, s);
   } else {
@@ -411,6 +413,8 @@ int rtams_cache_keep(rtams_cache *c, int64_t n, const int32_t *d_seqs, const int
   if (!rc) rc = check_rows(c, 0, n, d_starts, rows, max_new);
   if (!rc) rc = check_tree(d_starts, rows, max_new, -1);
   if (rc || n == 0 || rows == 0) return rc;
+  if (n * c->cfg.layers * (int64_t)c->cfg.kv_heads >= (int64_t)1 << 32)
+    return fail(RTAMS_EINVAL, "%lld items, %d layers and %d heads are too many for one call", (long long)n, c->cfg.layers, c->cfg.kv_heads);
   if (!d_path || !d_kept) return fail(RTAMS_EINVAL, "path or kept are NULL");
   if (((uintptr_t)d_path | (uintptr_t)d_kept) % 4) return fail(RTAMS_EINVAL, "path or kept are not aligned to their type");
   hipStream_t s = static_cast<hipStream_t>(hip_stream);

@@ -129,6 +129,16 @@ def test_sinks_of_many_sequences():
     run(f, [min(x, i % 4) for i, x in enumerate(lengths)], 2, window=30, sinks=5)
 
 
+@pytest.mark.parametrize("count", [1, 6, 90])
+@pytest.mark.parametrize("tree", [False, True])
+def test_windows_longer_than_any_sequence(count, tree):
+    """What a window hides is a difference of positions: of the largest windows there are it must not leave 32 bits."""
+    f = Filled([300, 129], 2, 64, page=64, seed=27)
+    seen = [ancestors(random_tree(np.random.default_rng(count), count)) for _ in range(2)] if tree else None
+    for window in (2 ** 31 - 1, 2 ** 31 - 200, 1 << 30, 10_000):
+        run(f, [count] * 2, 4, seen, window=window, sinks=3)
+
+
 # ------------------------------------------------------------------ attention of trees
 @pytest.mark.parametrize("heads,kv,dim", SHAPES)
 @pytest.mark.parametrize("counts", [[1, 1, 1, 1], [2, 1, 3, 2], [5, 17, 0, 8], [40, 0, 64, 65], [130, 200, 1, 333]])
@@ -447,6 +457,16 @@ def test_many_items_are_kept():
         rows += list(range(at[i], at[i] + x - 4)) + [at[i] + x - 3, at[i] + x - 1]
     new = all_rows(c, [x - 2 for x in lengths], 1)[0]
     assert all(torch.equal(x[rows], y) for x, y in zip(old, new))
+
+
+def test_more_layers_and_heads_than_are_numbered_are_refused():
+    c = Cache(1024, 64, layers=1024, page_tokens=32, pages=1, max_seqs=4096, max_pages=1, device=DEV)
+    zeros = torch.zeros(4096, dtype=torch.int32, device=DEV)
+    with pytest.raises(rtams.RtamsError):
+        c.keep(zeros, zeros)
+    c.keep(zeros[:4], zeros[:4])  # (sequences that have no rows: seen on the device)
+    torch.cuda.synchronize()
+    assert c.poll_error() == rtams.EINVAL
 
 
 # ------------------------------------------------------------------ a step with all of them
