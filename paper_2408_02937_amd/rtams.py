@@ -37,6 +37,7 @@ SYMBOLS = [
     "rtams_cache_pool_bytes_for", "rtams_cache_scratch_bytes_for", "rtams_cache_create", "rtams_cache_destroy", "rtams_cache_layout",
     "rtams_cache_extend", "rtams_cache_write", "rtams_cache_read", "rtams_cache_attend", "rtams_cache_fork", "rtams_cache_trim",
     "rtams_cache_compact", "rtams_cache_free_pages", "rtams_cache_poll_error", "rtams_cache_clear_error",
+    "rtams_cache_attend_sight", "rtams_cache_tree", "rtams_cache_walk", "rtams_cache_keep", "rtams_logits_scratch_bytes_for", "rtams_logits_score",
 ]
 
 

@@ -52,3 +52,30 @@ def test_scratch_is_asked_for_where_rows_are_few():
     assert size(rows=1, vocab=200_000, top=8) == one // 16 * (16 + 64)
     assert L.rtams_logits_score(None, None) == rtams.EINVAL
     assert L.rtams_logits_score(C.byref(query(rows=0, d_logits=0)), None) == rtams.OK
+
+
+@pytest.fixture(scope="module")
+def records():
+    from tests.test_kernel_resources import code_objects, kernels
+    with open(rtams.LIB_PATH, "rb") as f:
+        blob = f.read()
+    return {k[".name"]: k for e in code_objects(blob) for k in kernels(e)}
+
+
+# wavefronts of a workgroup and workgroups that are to run at once on a compute unit: four SIMDs of 512 registers, 160 KiB of LDS.  Dynamic LDS of many
+# rows: two tiles of halves and four of codes, of 64 tokens (32 where workgroups have 4 wavefronts).
+@pytest.mark.parametrize("name,waves,groups,lds", [
+    ("13k_cache_sightILi64ELi1E", 4, 5, 21 * 1024), ("13k_cache_sightILi64ELi2E", 4, 3, 22 * 1024), ("13k_cache_sightILi96ELi1E", 4, 4, 31 * 1024),
+    ("13k_cache_sightILi96ELi2E", 4, 2, 32 * 1024), ("13k_cache_sightILi128ELi1E", 4, 3, 42 * 1024), ("13k_cache_sightILi128ELi2E", 4, 2, 42 * 1024),
+    ("13k_cache_sightILi256ELi1E", 4, 1, 83 * 1024),
+    ("20k_cache_prompt_sightILi64ELi8ELi2E", 8, 1, 52 * 1024), ("20k_cache_prompt_sightILi64ELi4ELi1E", 4, 2, 26 * 1024),
+    ("20k_cache_prompt_sightILi96ELi8ELi2E", 8, 1, 78 * 1024), ("20k_cache_prompt_sightILi96ELi4ELi1E", 4, 2, 39 * 1024),
+    ("20k_cache_prompt_sightILi128ELi8ELi2E", 8, 1, 104 * 1024), ("20k_cache_prompt_sightILi128ELi4ELi1E", 4, 2, 52 * 1024),
+    ("20k_cache_prompt_sightILi256ELi4ELi1E", 4, 1, 104 * 1024), ("14k_cache_promptILi128ELi8E", 8, 1, 104 * 1024), ("14k_cache_promptILi256ELi4E", 4, 1, 104 * 1024),
+    ("8k_logitsILi0E", 4, 4, 0), ("8k_logitsILi1E", 4, 4, 0), ("8k_logitsILi2E", 4, 4, 0),
+])
+def test_as_many_workgroups_run_at_once_as_are_planned_for(records, name, waves, groups, lds):
+    mine = [k for n, k in records.items() if name in n]
+    assert len(mine) == 1
+    assert (mine[0][".vgpr_count"] + 7) // 8 * 8 * ((waves * groups + 3) // 4) <= 512
+    assert groups * (mine[0][".group_segment_fixed_size"] + lds) <= 160 * 1024
