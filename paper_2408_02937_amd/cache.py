@@ -246,7 +246,7 @@ class Cache:
         pp, rows = self._ints(parents, "parents", None, stream), parents.shape[0]
         n, _, tp, max_new = self._items(None, starts, rows if starts is None else None, max_new, stream)
         kp, cp = self._ints(tokens, "tokens", rows, stream), self._ints(chosen, "chosen", rows, stream)
-        path, kept, following = self._new(parents, (rows,), stream), self._new(parents, (n,), stream), self._new(parents, (n,), stream)
+        path, kept, following = self._new(parents, (rows + 2 * n,), stream).split_with_sizes((rows, n, n))
         _chk(self._lib.rtams_cache_walk(self._h, n, tp, rows, max_new, pp, kp, cp, path.data_ptr(), kept.data_ptr(), following.data_ptr(), self._stream(stream)),
              "rtams_cache_walk")
         return path, kept, following
