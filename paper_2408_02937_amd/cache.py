@@ -234,7 +234,7 @@ class Cache:
         tree is what attend takes; rows of one depth stand at one position."""
         pp, rows = self._ints(parents, "parents", None, stream), parents.shape[0]
         n, sp, tp, max_new = self._items(seqs, starts, rows if seqs is None and starts is None else None, max_new, stream)
-        words = (min(max_new, rows) + 31) // 32
+        words = max(1, (min(max_new, rows) + 31) // 32)  # (one even without rows: attend takes the tree)
         tree, positions = self._new(parents, (rows, words), stream), self._new(parents, (rows,), stream)
         _chk(self._lib.rtams_cache_tree(self._h, n, sp, tp, rows, max_new, pp, tree.data_ptr(), words, positions.data_ptr(), self._stream(stream)), "rtams_cache_tree")
         return tree, positions

@@ -638,3 +638,17 @@ def test_refusals():
     assert tree.shape[0] == 0 and positions.shape[0] == 0 and kept.tolist() == [0, 0] and following.tolist() == [-1, -1]
     c.keep(empty, ints([0]), starts=ints([0, 0]), max_new=1)
     assert c.poll_error() == 0 and c.lengths.tolist() == [1100, 5, 0, 0]
+
+
+def test_a_batch_without_rows_goes_through_all_steps():
+    c = Cache(2, 64, page_tokens=32, pages=20, max_seqs=4, device=DEV)
+    c.extend(starts=ints([0, 40]))
+    none, starts = ints([]), ints([0, 0, 0])
+    tree, positions = c.tree(none, starts=starts, max_new=5)
+    out = c.attend(0, torch.zeros((0, 4, 64), device=DEV).half(), starts=starts, max_new=5, tree=tree)
+    path, kept, following = c.walk(none, none, none, starts, 5)
+    c.keep(path, kept, starts=starts, max_new=5)
+    torch.cuda.synchronize()
+    assert tree.shape == (0, 1) and positions.shape == (0,) and out.shape == (0, 4, 64)
+    assert kept.tolist() == [0, 0] and following.tolist() == [-1, -1]
+    assert c.poll_error() == 0 and c.lengths.tolist() == [40, 0, 0, 0]
