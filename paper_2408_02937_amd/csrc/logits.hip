@@ -496,13 +496,17 @@ __global__ __launch_bounds__(kLanes, 4) void k_logits(LogitsDev q, int64_t first
   }
 }
 
-// Joins the pieces of a row: sums, and the pieces' lists, which are in order.  A token's place is how many of each list are in front of it.
+// Joins the pieces of a row: sums, and the pieces' lists, which are in order.  A token's place is how many of each list are in front of it.  (Four lists are
+// searched side by side, since a search is a chain of reads of LDS: 64 rows of 8 lists of 20 in a recorded graph 23.5 us one by one, 22.9 so; eight at a time
+// 22.7, but of 4 lists 20.0 for 18.6.)
+constexpr int kSideBySide = 4;
+
 template <int TYPE>
 __global__ __launch_bounds__(kLanes) void k_logits_join(LogitsDev q, int64_t first_row) {
   __shared__ uint64_t lists[kMostPieces * kMostTop], best[kMostTop];
   __shared__ uint32_t count;
   const int64_t row = first_row + blockIdx.x;
-  const int lane = threadIdx.x & 63, n = q.pieces * q.top;
+  const int lane = threadIdx.x & 63, n = q.pieces * q.top, first_step = q.top ? 1 << (31 - __clz(q.top)) : 0;
   const float given = given_logit<TYPE>(q, row, threadIdx.x);
   if (threadIdx.x == 0) count = 0;
   for (int i = threadIdx.x; i < n; i += kLanes) lists[i] = q.part_best[row * n + i];
@@ -524,15 +528,17 @@ __global__ __launch_bounds__(kLanes) void k_logits_join(LogitsDev q, int64_t fir
     if (!key) continue;
     atomicAdd(&count, 1u);
     int place = i % q.top;
-    for (int b = 0; b < q.pieces && place < q.top; ++b) {
-      if (b == i / q.top) continue;
-      int lo = 0, hi = q.top;
-      while (lo < hi) {
-        const int mid = (lo + hi) / 2;
-        if (lists[b * q.top + mid] > key) lo = mid + 1;
-        else hi = mid;
-      }
-      place += lo;
+    const int own = i / q.top;
+    for (int b = 0; b < q.pieces && place < q.top; b += kSideBySide) {
+      int in_front[kSideBySide] = {};
+      for (int step = first_step; step; step >>= 1)
+#pragma unroll
+        for (int e = 0; e < kSideBySide; ++e) {
+          const int at = in_front[e] + step, list = min(b + e, q.pieces - 1);
+          if (at <= q.top && lists[list * q.top + at - 1] > key) in_front[e] = at;
+        }
+#pragma unroll
+      for (int e = 0; e < kSideBySide; ++e) place += b + e < q.pieces && b + e != own ? in_front[e] : 0;
     }
     if (place < q.top) best[place] = key;
   }
