@@ -2,8 +2,8 @@
 //
 // The formulas are those of cache_attend.hip; here arithmetic bounds: 4 * head_dim flops for a row and token.  A workgroup has
 // 32 rows for each wavefront (a row: a token's query head of those that share a kv head) and goes over the tokens that they see
-// 64 at a time (32 where head_dim is 256): their codes come to LDS as they are, by copies that run three tiles ahead, and all lanes turn them into
-// halves, again in LDS, once for all rows, a tile ahead of the products; one barrier a tile.  Scores are S^T = K Q^T with Q in registers; a lane has one row's scores and its
+// 64 at a time (32 where head_dim is 256): all its lanes turn their codes into halves in LDS, once for all rows, a tile ahead of the products, while the
+// next tiles' codes are on their way to registers or to LDS (by_copies); two buffers, one barrier a tile.  Scores are S^T = K Q^T with Q in registers; a lane has one row's scores and its
 // probabilities are the operand that O^T = V^T P^T takes.  The running maximum enters as the start of the scores' sums and moves
 // only where a score has left it far behind (kLag).  LDS holds operands in the order in which the lanes take them, 16 bytes each; the slots are
 // swapped so that writing meets no bank twice.  Where rows are too few to fill the chip the tokens are split, and the last
@@ -12,11 +12,11 @@
 // The scale's power of two is in the query, exact as an operand; what is left of it multiplies scores in 32 bits (in the query and rounded there:
 // 576 us instead of 580, and half outputs 1.6 to 1.8 times as far from 64 bits as their own rounding alone, not 1.5 to 1.6).
 //
-// Measured: a prompt of 8,192 tokens, 32 heads of 128 over 8: 575 to 640 us from card to card for 550 GFLOP, 860 to 957 TFLOP/s where a plain product
+// Measured: a prompt of 8,192 tokens, 32 heads of 128 over 8: 567 to 640 us from card to card for 550 GFLOP, 860 to 970 TFLOP/s where a plain product
 // of 8,192 squared reaches 1,140 in bfloat16 and 1,084 in halves.  Vector instructions (exponentials, masks, codes) take 48 % of the cycles, matrix
-// instructions 41 %, and two wavefronts of a SIMD overlap them in part.  Heads of 64, 96, 128, 256 on one card: 455, 551, 640, 2,314 us; 604, 749, 859,
-// 475 TFLOP/s: the fewer the channels, the more exponentials for a flop; at 256 one wavefront fits a SIMD.  At 128 channels, on a card of 580 us:
-// 4 wavefronts a workgroup 710, wavefronts half a tile apart 610.  (Codes that are loaded into registers a tile ahead: 609 us, with copies 607 on that card.)
+// instructions 41 %, and two wavefronts of a SIMD overlap them in part.  Heads of 64, 96, 128, 256 on one card: 386, 484, 568, 2,312 us; 712, 852, 968,
+// 476 TFLOP/s: the fewer the channels, the more exponentials for a flop; at 256 one wavefront fits a SIMD.  At 128 channels, on a card of 580 us:
+// 4 wavefronts a workgroup 710, wavefronts half a tile apart 610.
 // What bounds it: a tile of 64 tokens takes a compute unit 2.5 us, of which products and exponentials alone take 1.9, 0.93 of them the matrix instructions' own
 // time; at their full rate they would read LDS at its own.  With the SIMD's two wavefronts changing places between matrix and vector instructions behind a
 // barrier each 252 us where 206 are taken here, with the next tile's scores between this one's exponentials 226 (252 rows behind 4 sequences of up to 60,063).
@@ -45,10 +45,19 @@ constexpr int at_once(int head_dim, int waves) { return waves == 8 || head_dim =
 
 constexpr int kRing = 4;  // tiles on their way or being unpacked
 
-template <int D, int TB>
+// Whether codes come to LDS as they are, by copies that run three tiles ahead; others are loaded into registers two tiles ahead.  Without a sight, in registers
+// and by copies, one card: a prompt of 8,192 tokens, 32 heads of 64, 96, 128, 256 channels over 8: 398 and 386, 483 and 483, 567 and 570, 2,312 and 2,352 us;
+// 600 rows behind each of 8 sequences of up to 5,000, 8 heads: 97 and 94, 113 and 112, 123 and 127, 347 and 351.  (With a sight the blocks of a tile may lie
+// apart; there they are copied one by one.)
+constexpr bool by_copies(int head_dim, bool sight) { return sight || head_dim == 64; }
+
+template <int D, int TB, bool RING>
 struct Staging {  // tiles in LDS: operands of 16 bytes
-  uint4 k[2][TB * 4 * D];            // [block][word][token]
-  uint4 v[2][TB * 4 * D];            // [block][32 channels][lane group][channel]
+  uint4 k[2][TB * 4 * D];  // [block][word][token]
+  uint4 v[2][TB * 4 * D];  // [block][32 channels][lane group][channel]
+};
+template <int D, int TB>
+struct Staging<D, TB, true> : Staging<D, TB, false> {
   uint4 raw[kRing][TB * 40 * D / 16];  // as the cache holds them
 };
 
@@ -166,9 +175,9 @@ constexpr int kSplit = 4;
 constexpr int kMostEntries = 1024;  // row tiles of items that are planned
 constexpr int kClasses = 8;         // of their pieces, by length
 
-template <int D, int TB>
+template <int D, int TB, bool RING>
 union Shared {
-  Staging<D, TB> tile;
+  Staging<D, TB, RING> tile;
   float steps[kMostEntries];  // in front of them
 };
 
@@ -236,8 +245,9 @@ __device__ __forceinline__ void attend_many(const CacheDev &d, const CacheQuery 
   constexpr int kLanes = WAVES * 64, NS = D / 16, NC = D / 32, NP = (2 * kPairs<D, TB> + kLanes - 1) / kLanes;
   constexpr int kTile = TB * kBlockTokens;
   extern __shared__ uint4 lds[];
-  Shared<D, TB> &shared = *reinterpret_cast<Shared<D, TB> *>(lds);
-  Staging<D, TB> &sh = shared.tile;
+  constexpr bool RING = by_copies(D, SIGHT);
+  Shared<D, TB, RING> &shared = *reinterpret_cast<Shared<D, TB, RING> *>(lds);
+  Staging<D, TB, RING> &sh = shared.tile;
   __shared__ Piece piece;
   __shared__ int flag;
   Piece pc;
@@ -416,66 +426,110 @@ __device__ __forceinline__ void attend_many(const CacheDev &d, const CacheQuery 
     reads_ahead<NC * TB * 2>();
   };
   if (length > 0) {  // (an empty sequence has one step and no page)
-    // A tile is copied in chunks of 1 KiB, one to a wavefront after the other.
-    constexpr int kChunks = (40 * D + 1023) / 1024, kAll = TB * kChunks, kMost = (kAll + WAVES - 1) / WAVES, kLess = kAll / WAVES;
-    const uint32_t ring = (uint32_t)uniform((int)lds_address(sh.raw[0]));
-    const auto copy = [&](int t) {
-      const uint32_t slot = ring + (uint32_t)(t - t0) % kRing * (TB * 40 * D);
+    if constexpr (RING) {
+      // A tile is copied in chunks of 1 KiB, one to a wavefront after the other.
+      constexpr int kChunks = (40 * D + 1023) / 1024, kAll = TB * kChunks, kMost = (kAll + WAVES - 1) / WAVES, kLess = kAll / WAVES;
+      const uint32_t ring = (uint32_t)uniform((int)lds_address(sh.raw[0]));
+      const auto copy = [&](int t) {
+        const uint32_t slot = ring + (uint32_t)(t - t0) % kRing * (TB * 40 * D);
 #pragma unroll
-      for (int i = 0; i < kMost; ++i) {
-        const int c = i * WAVES + wave, x = c / kChunks, at = c % kChunks * 1024;
-        if (i < kLess || c < kAll) {
-          const unsigned char *blk = block_at(place(t * kTile + x * kBlockTokens) / kBlockTokens);
-          if (40 * D % 1024 == 0 || lane * 16 < 40 * D - at) copy_to_lds(blk + at, slot + x * (40 * D) + at, lane * 16);
+        for (int i = 0; i < kMost; ++i) {
+          const int c = i * WAVES + wave, x = c / kChunks, at = c % kChunks * 1024;
+          if (i < kLess || c < kAll) {
+            const unsigned char *blk = block_at(place(t * kTile + x * kBlockTokens) / kBlockTokens);
+            if (40 * D % 1024 == 0 || lane * 16 < 40 * D - at) copy_to_lds(blk + at, slot + x * (40 * D) + at, lane * 16);
+          }
         }
-      }
-    };
-    // This wavefront's chunks are there, but those of the `later` tiles that it asked for last.
-    const auto arrived = [&](auto later) {
-      constexpr int kLater = decltype(later)::value;
-      if (kMost == kLess || wave < kAll % WAVES) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kMost * kLater) : "memory");
-      else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLess * kLater) : "memory");
-    };
-    const auto unpack = [&](int t) {
-      const unsigned char *b0 = reinterpret_cast<const unsigned char *>(sh.raw[(uint32_t)(t - t0) % kRing]), *b1 = b0 + (TB == 2 ? 40 * D : 0);
-      uint4 *const k = sh.k[(t - t0) & 1], *const v = sh.v[(t - t0) & 1];
-      Words<D> words[NP];
-      constexpr bool kWhole = 2 * kPairs<D, TB> % kLanes == 0;
+      };
+      // This wavefront's chunks are there, but those of the `later` tiles that it asked for last.
+      const auto arrived = [&](auto later) {
+        constexpr int kLater = decltype(later)::value;
+        if (kMost == kLess || wave < kAll % WAVES) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kMost * kLater) : "memory");
+        else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLess * kLater) : "memory");
+      };
+      const auto unpack = [&](int t) {
+        const unsigned char *b0 = reinterpret_cast<const unsigned char *>(sh.raw[(uint32_t)(t - t0) % kRing]), *b1 = b0 + (TB == 2 ? 40 * D : 0);
+        uint4 *const k = sh.k[(t - t0) & 1], *const v = sh.v[(t - t0) & 1];
+        Words<D> words[NP];
+        constexpr bool kWhole = 2 * kPairs<D, TB> % kLanes == 0;
 #pragma unroll
-      for (int i = 0; i < NP; ++i) {
-        const int u = i * kLanes + threadIdx.x;
-        if (kWhole || u < 2 * kPairs<D, TB>) load_words<D, TB>(words[i], u, b0, b1);
-      }
+        for (int i = 0; i < NP; ++i) {
+          const int u = i * kLanes + threadIdx.x;
+          if (kWhole || u < 2 * kPairs<D, TB>) load_words<D, TB>(words[i], u, b0, b1);
+        }
 #pragma unroll
-      for (int i = 0; i < NP; ++i) {
-        const int u = i * kLanes + threadIdx.x;
-        if (kWhole || u < 2 * kPairs<D, TB>) put_words<D, TB>(words[i], u, k, v);
-      }
-    };
-    for (int i = 0; i < kRing - 1; ++i)
-      if (t0 + i < t1) copy(t0 + i);
-    if (t0 + kRing - 1 <= t1) arrived(std::integral_constant<int, kRing - 2>());
-    else arrived(std::integral_constant<int, 0>());
-    meet();
-    unpack(t0);
-    if (t0 + kRing - 1 < t1) copy(t0 + kRing - 1);
-    for (int t = t0; t < t1; ++t) {
-      if (t + kRing <= t1) arrived(std::integral_constant<int, kRing - 2>());
+        for (int i = 0; i < NP; ++i) {
+          const int u = i * kLanes + threadIdx.x;
+          if (kWhole || u < 2 * kPairs<D, TB>) put_words<D, TB>(words[i], u, k, v);
+        }
+      };
+      for (int i = 0; i < kRing - 1; ++i)
+        if (t0 + i < t1) copy(t0 + i);
+      if (t0 + kRing - 1 <= t1) arrived(std::integral_constant<int, kRing - 2>());
       else arrived(std::integral_constant<int, 0>());
-      meet();  // (tile t is unpacked, the next one's codes are there, and what this turn writes over has been read)
-      if (t + kRing < t1) copy(t + kRing);
-      if (t + 1 < t1) unpack(t + 1);
-      const int tok0 = place(t * kTile), tok1 = SIGHT && TB == 2 ? place(t * kTile + kBlockTokens) : tok0;
-      const auto seen = [&](int tok) { return tok < any_to && (tok + kBlockTokens > any_from || tok < g.sinks); };
-      if (SIGHT ? !(seen(tok0) || seen(tok1)) : !(tok0 < any_to && tok0 + kTile > any_from)) continue;
-      // (matrix instructions first: the other wavefront of the SIMD has its exponentials beside them)
-      __builtin_amdgcn_s_setprio(1);
-      scores(sh.k[(t - t0) & 1]);
-      __builtin_amdgcn_s_setprio(0);
-      probabilities(tok0, tok1);
-      __builtin_amdgcn_s_setprio(1);
-      weigh(sh.v[(t - t0) & 1]);
-      __builtin_amdgcn_s_setprio(0);
+      meet();
+      unpack(t0);
+      if (t0 + kRing - 1 < t1) copy(t0 + kRing - 1);
+      for (int t = t0; t < t1; ++t) {
+        if (t + kRing <= t1) arrived(std::integral_constant<int, kRing - 2>());
+        else arrived(std::integral_constant<int, 0>());
+        meet();  // (tile t is unpacked, the next one's codes are there, and what this turn writes over has been read)
+        if (t + kRing < t1) copy(t + kRing);
+        if (t + 1 < t1) unpack(t + 1);
+        const int tok0 = place(t * kTile), tok1 = SIGHT && TB == 2 ? place(t * kTile + kBlockTokens) : tok0;
+        const auto seen = [&](int tok) { return tok < any_to && (tok + kBlockTokens > any_from || tok < g.sinks); };
+        if (SIGHT ? !(seen(tok0) || seen(tok1)) : !(tok0 < any_to && tok0 + kTile > any_from)) continue;
+        // (matrix instructions first: the other wavefront of the SIMD has its exponentials beside them)
+        __builtin_amdgcn_s_setprio(1);
+        scores(sh.k[(t - t0) & 1]);
+        __builtin_amdgcn_s_setprio(0);
+        probabilities(tok0, tok1);
+        __builtin_amdgcn_s_setprio(1);
+        weigh(sh.v[(t - t0) & 1]);
+        __builtin_amdgcn_s_setprio(0);
+      }
+    } else {
+      Words<D> next[NP];
+      constexpr bool kWhole = 2 * kPairs<D, TB> % kLanes == 0;
+      const auto load_tile = [&](Words<D> (&to)[NP], int t) {
+        const int block = (from + t * kTile) / kBlockTokens;
+        const unsigned char *b0 = block_at(block), *b1 = TB == 2 ? block_at(block + 1) : b0;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+          const int u = i * kLanes + threadIdx.x;
+          if (kWhole || u < 2 * kPairs<D, TB>) load_words<D, TB>(to[i], u, b0, b1);
+        }
+      };
+      const auto put_tile = [&](const Words<D> (&of)[NP], uint4 *k, uint4 *v) {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+          const int u = i * kLanes + threadIdx.x;
+          if (kWhole || u < 2 * kPairs<D, TB>) put_words<D, TB>(of[i], u, k, v);
+        }
+      };
+      {
+        Words<D> first[NP];
+        load_tile(first, t0);
+        if (t0 + 1 < t1) load_tile(next, t0 + 1);
+        put_tile(first, sh.k[0], sh.v[0]);
+      }
+      __syncthreads();
+      for (int t = t0; t < t1; ++t) {
+        const int tok0 = from + t * kTile, now = (t - t0) & 1;
+        const bool some = tok0 < any_to && tok0 + kTile > any_from;
+        if (t + 1 < t1) put_tile(next, sh.k[now ^ 1], sh.v[now ^ 1]);
+        if (t + 2 < t1) load_tile(next, t + 2);
+        if (some) {
+          __builtin_amdgcn_s_setprio(1);
+          scores(sh.k[now]);
+          __builtin_amdgcn_s_setprio(0);
+          probabilities(tok0, tok0);
+          __builtin_amdgcn_s_setprio(1);
+          weigh(sh.v[now]);
+          __builtin_amdgcn_s_setprio(0);
+        }
+        __syncthreads();
+      }
     }
   }
   l += __shfl_xor(l, 32);
@@ -602,8 +656,8 @@ void launch(const CacheDev &d, const CacheQuery &q, const CacheSight *g, hipStre
   const int64_t all = split ? groups + kWorkers : groups, most = 1 << 22;  // (of a launch; one that finds no rows takes 10 ns: 512 items of 8 heads, one of 32,768 rows, 28 ms of which it takes 6)
   for (int64_t at = 0; at < all; at += most) {
     const uint32_t grid = (uint32_t)(all - at < most ? all - at : most);
-    if (g) k_cache_prompt_sight<D, WAVES, TB><<<grid, WAVES * 64, sizeof(Shared<D, TB>), s>>>(d, q, *g, tiles, tile_rows, split, (uint32_t)at);
-    else if constexpr (TB == tile_blocks(D) && WAVES == (D == 256 ? 4 : 8)) k_cache_prompt<D, WAVES><<<grid, WAVES * 64, sizeof(Shared<D, TB>), s>>>(d, q, tiles, tile_rows, split, (uint32_t)at);
+    if (g) k_cache_prompt_sight<D, WAVES, TB><<<grid, WAVES * 64, sizeof(Shared<D, TB, true>), s>>>(d, q, *g, tiles, tile_rows, split, (uint32_t)at);
+    else if constexpr (TB == tile_blocks(D) && WAVES == (D == 256 ? 4 : 8)) k_cache_prompt<D, WAVES><<<grid, WAVES * 64, sizeof(Shared<D, TB, by_copies(D, false)>), s>>>(d, q, tiles, tile_rows, split, (uint32_t)at);
   }
   if (g && split) k_cache_join_many<D, WAVES><<<(uint32_t)(groups * WAVES * (D / 32) / 4), 256, 0, s>>>(d, q, *g, tiles, tile_rows);
 }
@@ -631,12 +685,12 @@ hipError_t allow_large_lds_cache_prompt() {
   const auto allow = [&](auto kernel, size_t bytes) {
     if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
   };
-  allow(k_cache_prompt<96, 8>, sizeof(Shared<96, 2>));
-  allow(k_cache_prompt<128, 8>, sizeof(Shared<128, 2>));
-  allow(k_cache_prompt<256, 4>, sizeof(Shared<256, 1>));
-  allow(k_cache_prompt_sight<96, 8, 2>, sizeof(Shared<96, 2>));
-  allow(k_cache_prompt_sight<128, 8, 2>, sizeof(Shared<128, 2>));
-  allow(k_cache_prompt_sight<256, 4, 1>, sizeof(Shared<256, 1>));
+  allow(k_cache_prompt<96, 8>, sizeof(Shared<96, 2, by_copies(96, false)>));
+  allow(k_cache_prompt<128, 8>, sizeof(Shared<128, 2, by_copies(128, false)>));
+  allow(k_cache_prompt<256, 4>, sizeof(Shared<256, 1, by_copies(256, false)>));
+  allow(k_cache_prompt_sight<96, 8, 2>, sizeof(Shared<96, 2, true>));
+  allow(k_cache_prompt_sight<128, 8, 2>, sizeof(Shared<128, 2, true>));
+  allow(k_cache_prompt_sight<256, 4, 1>, sizeof(Shared<256, 1, true>));
   return e;
 }
 
