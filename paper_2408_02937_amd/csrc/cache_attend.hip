@@ -142,8 +142,13 @@ __device__ bool find_piece(const CacheDev &d, const CacheQuery &q, const CacheSi
       if (x < pieces) {
         // Row tiles of a piece read the same tokens: they are 8 workgroups apart, on the same die, whose L2 has them.  (64 rows of 128 channels, 8 heads,
         // 16 sequences of up to 6,001, 4 of up to 60,063, one of 32,000: side by side 52, 89, 33 us, so 51, 87, 32.)
-        const uint32_t n_tiles = (uint32_t)sp[k].tiles, all_y = parts * (uint32_t)d.kv_heads, y0 = x / (8 * n_tiles) * 8, beside = min(8u, all_y - y0), rest = x - y0 * n_tiles;
-        const uint32_t t = rest / beside, y = y0 + rest - t * beside, head = y / parts;
+        uint32_t t = 0, y = x;
+        if (tiles > 1) {  // (of one there is nothing to divide: a token over 100, 128 channels, 6.06 us, so 5.92)
+          const uint32_t n_tiles = (uint32_t)sp[k].tiles, all_y = parts * (uint32_t)d.kv_heads, y0 = x / (8 * n_tiles) * 8, beside = min(8u, all_y - y0), rest = x - y0 * n_tiles;
+          t = rest / beside;
+          y = y0 + rest - t * beside;
+        }
+        const uint32_t head = y / parts;
         sh.piece = Piece{sp[k], base + 64 * k + lane, (int)head, (int)t, 0, 0, (int)parts, (int)(y % parts),
                          (int)(parts_before + upto_shared - shared + (head * sp[k].tiles + t) * parts)};
       }
