@@ -9,8 +9,8 @@
 // bytes each: all of a panel's loads go out before the first is needed, and a lane's largest is known before its first power, so that sums are scaled
 // once a panel.  The most likely tokens: of the first panel the k-th largest of the lanes' largest is a bound that the k largest of all reach, and few
 // others do; the lanes that have some are listed, all lanes look through their vectors, and what reaches the bound goes to LDS and is ranked there.  Later
-// panels are held against the k-th so far.  Where too many reach the bound (one lane has them all, or they are equal) it is found by bisection, and of
-// those equal to it the lowest tokens are counted off.
+// panels are held against the k-th so far.  Where too many reach the bound, those above it are taken and of those equal to it the lowest tokens counted off;
+// where too many are above it (a few lanes have them all) a better one is found by bisection.
 #include "../../include/rtams_logits.h"
 
 #include "host.h"
@@ -197,14 +197,16 @@ __device__ void take_best(const char *x, int vocab, int panel, float most, int t
   const int lanes = __syncthreads_count(most > bound);
   if (!lanes) return;
   const int have = sh.have;
-  // Those that reach `least` go behind the best so far, as far as there is room; how many they are.
+  // Those that reach `least` go behind the best so far, as far as there is room; how many they are (where there is none left, more than kRoom).
   const auto collect = [&](float least) {
     if (threadIdx.x == 0) sh.count = sh.lanes = 0;
     __syncthreads();
     if (most >= least) sh.listed[atomicAdd(&sh.lanes, 1u)] = (uint16_t)threadIdx.x;
     __syncthreads();
     const uint32_t all = sh.lanes * kVectors;
+    const bool crowded = all > kLanes / 2 * kVectors;  // (32,768 equal ones one after the other take 15 us)
     for (uint32_t u = threadIdx.x; u < all; u += kLanes) {
+      if (crowded && __hip_atomic_load(&sh.count, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) > kRoom) break;
       const int at = panel + ((int)(u % kVectors) * kLanes + sh.listed[u / kVectors]) * E;
       const u32x4 raw = load_vector<TYPE>(x, at, vocab);
 #pragma unroll
@@ -219,10 +221,10 @@ __device__ void take_best(const char *x, int vocab, int panel, float most, int t
     __syncthreads();
     return sh.count;
   };
-  // The top-th largest of the lanes' largest; of few, the largest that a wavefront's own lanes have there (if they are as many), which some more reach.
-  const auto near = [&]() {
+  // The top-th largest of the lanes' largest; own: of few, the largest that a wavefront's own lanes have there (if they are as many), which some more reach.
+  const auto near = [&](bool own) {
     const uint32_t mine = most > bound ? ordered(most) : 0;
-    if (top <= 32) {
+    if (own) {
       int above = 0;
 #pragma unroll
       for (int j = 0; j < 64; ++j) above += (uint32_t)__builtin_amdgcn_readlane((int)mine, j) > mine;
@@ -247,52 +249,51 @@ __device__ void take_best(const char *x, int vocab, int panel, float most, int t
     return unordered(sh.near);
   };
   float from = unordered(ordered(bound) + 1);  // the least that exceeds it (of -inf the least number)
-  if (have < top && lanes >= top) from = near();
+  const bool many = lanes >= top, own = top <= 32;
+  if (have < top && many) from = near(own);
   uint32_t all = collect(from);
-  if (all > kRoom && have == top && lanes >= top) {
-    from = near();
+  if (all > kRoom && many && (have == top || own)) {
+    from = near(own && have == top);
     all = collect(from);
   }
   if (all <= kRoom) return rank(have + (int)all, top, sh);
+  // Of a row that is masked with a number (its type's lowest) and allows less than that many tokens, `from` is that number, which nearly all are
+  // equal to: those above it come first.  (1,000 rows of 32,768 halves, 19 tokens allowed, the best 20: 38 us, where a
+  // mask of -inf takes 19 and a search for `from` bit by bit 260.)
+  float over = unordered(ordered(from) + 1);
+  __syncthreads();  // (the count has been read)
+  all = collect(over);
+  if (all >= (uint32_t)top && all <= kRoom) return rank(have + (int)all, top, sh);
   const int first = panel + (int)threadIdx.x * E;
-  const auto each = [&](float least, auto f) {  // f(token, logit) in the order of the lane's tokens
-    if (!(most >= least)) return;
+  const auto reaching = [&](float least) {  // how many do, in all lanes
+    uint32_t n = 0;
+    if (most >= least) {
 #pragma unroll 1
-    for (int v = 0; v < kVectors; ++v) {
-      const int at = first + v * kLanes * E;
-      const u32x4 raw = load_vector<TYPE>(x, at, vocab);
+      for (int v = 0; v < kVectors; ++v) {
+        const u32x4 raw = load_vector<TYPE>(x, first + v * kLanes * E, vocab);
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const float l = logit<TYPE>(raw, e);
-        if (l >= least) f(at + e, l);
+        for (int e = 0; e < E; ++e) n += logit<TYPE>(raw, e) >= least;
       }
     }
-  };
-  const auto reaching = [&](float least, uint32_t *mine) {  // how many do, in all lanes
-    uint32_t n = 0;
-    each(least, [&](int, float) { ++n; });
-    *mine = n;
     return sum_lanes(n, sh);
   };
-  const auto append = [&](float least, uint32_t n) {  // n in this lane
-    if (threadIdx.x == 0) sh.count = have;
+  if (all > kRoom) {
+    // the top-th largest, exactly: the highest that as many reach
+    const uint32_t highest = last_lane(wave_reduce_last(most > over ? ordered(most) : 0, [](uint32_t a, uint32_t b) { return a > b ? a : b; }));
     __syncthreads();
-    uint32_t at = n ? atomicAdd(&sh.count, n) : 0;
-    if (n) each(least, [&](int token, float l) { sh.best[at++] = key_of(l, token); });
+    if ((threadIdx.x & 63) == 0) sh.waves[threadIdx.x >> 6] = highest;
     __syncthreads();
-  };
-  uint32_t mine = 0;
-  // the top-th largest, exactly: the highest that as many reach
-  uint32_t low = ordered(from), high = ordered(INFINITY);
-  while (low < high) {
-    const uint32_t mid = low + (high - low + 1) / 2;
-    uint32_t n;
-    if (reaching(unordered(mid), &n) >= (uint32_t)top) low = mid;
-    else high = mid - 1;
+    uint32_t low = ordered(over), high = max(max(sh.waves[0], sh.waves[1]), max(sh.waves[2], sh.waves[3]));
+    while (low < high) {
+      const uint32_t mid = low + (high - low + 1) / 2;
+      if (reaching(unordered(mid)) >= (uint32_t)top) low = mid;
+      else high = mid - 1;
+    }
+    from = unordered(low);
+    over = unordered(low + 1);
+    all = collect(over);
   }
-  const float equal = unordered(low), over = unordered(low + 1);
-  all = reaching(over, &mine);
-  append(over, mine);
+  const float equal = from;
   uint32_t filled = have + all, need = top - all;
 #pragma unroll 1
   for (int v = 0; v < kVectors && need; ++v) {  // in the order of the tokens
