@@ -28,6 +28,9 @@
  * number of rows.)  After an extend that was dropped, writes are dropped too until an extend succeeds or
  * rtams_cache_clear_error is called.
  *
+ * Devices.  A cache is its pool's device's, and so are the streams of its calls (NULL: that device's default stream), whichever device is the thread's
+ * current one.
+ *
  * Streams.  The calls of one cache run one after another; a call on another stream than the one before is ordered behind
  * it with an event.  A stream must live until the cache has been used on another one or destroyed.  Recorded calls
  * (stream capture) are ordered by their graph alone: the caller orders its launches with other calls.

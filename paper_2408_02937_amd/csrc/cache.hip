@@ -20,6 +20,7 @@ struct rtams_cache {
   bool have_stream = false;
   hipEvent_t done = nullptr;
   bool forked = false;  // sequences may share pages
+  int device = 0;       // where the pool is
 };
 
 namespace {
@@ -91,8 +92,38 @@ __global__ void k_cache_clear_words(uint32_t *p, uint64_t n) {
   for (uint64_t i = blockIdx.x * (uint64_t)blockDim.x + threadIdx.x; i < n; i += (uint64_t)gridDim.x * blockDim.x) p[i] = 0;
 }
 
+// Makes a device the thread's current one until the end of a call, if another is: the default stream is the current device's, and a kernel that is
+// launched there finds none of the cache's memory.
+class OnDevice {
+ public:
+  explicit OnDevice(int device) {
+    ok = hipGetDevice(&was_) == hipSuccess && (was_ == device || hipSetDevice(device) == hipSuccess);
+    back_ = ok && was_ != device;
+  }
+  ~OnDevice() {
+    if (back_) (void)hipSetDevice(was_);
+  }
+  OnDevice(const OnDevice &) = delete;
+  OnDevice &operator=(const OnDevice &) = delete;
+  bool ok;
+
+ private:
+  int was_ = 0;
+  bool back_;
+};
+
+int device_of(const void *memory) {
+  hipPointerAttribute_t at{};
+  int device = 0;
+  if (hipPointerGetAttributes(&at, memory) == hipSuccess && at.type == hipMemoryTypeDevice) return at.device;
+  (void)hipGetLastError();
+  (void)hipGetDevice(&device);
+  return device;
+}
+
 // Orders the call behind the cache's work on another stream.  (Not a recorded call, which the graph orders.)
-int cache_enter(rtams_cache *c, hipStream_t s, bool *recorded = nullptr) {
+int cache_enter(rtams_cache *c, hipStream_t s, const OnDevice &on, bool *recorded = nullptr) {
+  if (!on.ok) return fail(RTAMS_EHIP, "device %d could not be made the current one", c->device);
   hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
   if (hipStreamIsCapturing(s, &capture) != hipSuccess) (void)hipGetLastError();
   if (recorded) *recorded = capture == hipStreamCaptureStatusActive;
@@ -188,6 +219,8 @@ int rtams_cache_create(const rtams_cache_config *cfg, rtams_cache **out) {
   rtams_cache *c = new (std::nothrow) rtams_cache;
   if (!c) return fail(RTAMS_EINVAL, "out of host memory");
   c->cfg = *cfg;
+  c->device = device_of(cfg->d_pool);
+  const OnDevice on(c->device);
   CacheDev &d = c->dev;
   char *p = static_cast<char *>(cfg->d_pool);
   d.layers = cfg->layers;
@@ -222,6 +255,7 @@ int rtams_cache_create(const rtams_cache_config *cfg, rtams_cache **out) {
   q += up(cache_part_ml_floats(cfg->head_dim) * 4, kAlign);
   d.part = reinterpret_cast<float *>(q);
   auto bail = [&](int code) { rtams_cache_destroy(c); return code; };
+  if (!on.ok) return bail(fail(RTAMS_EHIP, "device %d could not be made the current one", c->device));
   if (allow_large_lds_cache_attend() != hipSuccess || allow_large_lds_cache_prompt() != hipSuccess || allow_large_lds_cache_tree() != hipSuccess) return bail(fail(RTAMS_EHIP, "hipFuncSetAttribute failed"));
   void *hm = nullptr, *dm = nullptr;
   if (hipHostMalloc(&hm, sizeof(CacheMirror), hipHostMallocMapped) != hipSuccess) return bail(fail(RTAMS_EHIP, "hipHostMalloc failed"));
@@ -239,6 +273,7 @@ int rtams_cache_create(const rtams_cache_config *cfg, rtams_cache **out) {
 
 int rtams_cache_destroy(rtams_cache *c) {
   if (!c) return RTAMS_OK;
+  const OnDevice on(c->device);
   if (c->have_stream) (void)hipStreamSynchronize(c->stream);
   if (c->done) (void)hipEventDestroy(c->done);
   if (c->mirror) (void)hipHostFree(c->mirror);
@@ -262,8 +297,9 @@ int rtams_cache_extend(rtams_cache *c, int64_t n, const int32_t *d_seqs, const i
   if (rc || n == 0) return rc;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   std::lock_guard<std::mutex> g(c->mutex);
+  const OnDevice on(c->device);
   bool recorded = false;
-  if ((rc = cache_enter(c, s, &recorded))) return rc;
+  if ((rc = cache_enter(c, s, on, &recorded))) return rc;
   CacheRows r = items_of(n, d_seqs, d_starts, 0x7fffffff, 0x7fffffff);
   // (without a fork before this call no page can be shared; a recorded call may be launched behind a later fork)
   launch_cache_extend(c->dev, r, c->forked || recorded, s);
@@ -286,7 +322,8 @@ int rtams_cache_write(rtams_cache *c, int32_t layer, int64_t n, const int32_t *d
   if (((uintptr_t)d_k | (uintptr_t)d_v) % 2) return fail(RTAMS_EINVAL, "keys and values must be 2-byte aligned");
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   std::lock_guard<std::mutex> g(c->mutex);
-  if ((rc = cache_enter(c, s))) return rc;
+  const OnDevice on(c->device);
+  if ((rc = cache_enter(c, s, on))) return rc;
   const bool vec = ((uintptr_t)d_k | (uintptr_t)d_v) % 16 == 0 && row_stride % 8 == 0 && head_stride % 8 == 0;
   launch_cache_write(c->dev, items_of(n, d_seqs, d_starts, rows, max_new), layer, d_k, d_v, row_stride, head_stride, type == RTAMS_TYPE_F16, vec, s);
   return launched("write");
@@ -303,7 +340,8 @@ int rtams_cache_read(rtams_cache *c, int32_t layer, int64_t n, const int32_t *d_
   if (((uintptr_t)d_k | (uintptr_t)d_v) % 16) return fail(RTAMS_EINVAL, "keys and values must be 16-byte aligned");
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   std::lock_guard<std::mutex> g(c->mutex);
-  if ((rc = cache_enter(c, s))) return rc;
+  const OnDevice on(c->device);
+  if ((rc = cache_enter(c, s, on))) return rc;
   launch_cache_read(c->dev, items_of(n, d_seqs, d_starts, rows, max_new), layer, d_k, d_v, type, s);
   return launched("read");
 }
@@ -340,7 +378,8 @@ int rtams_cache_attend_sight(rtams_cache *c, const rtams_cache_query *q, const r
     return fail(RTAMS_EINVAL, "%lld items of up to %lld rows, %d heads, are too many for one call", (long long)n, (long long)most, q->q_heads);
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   std::lock_guard<std::mutex> g(c->mutex);
-  if ((rc = cache_enter(c, s))) return rc;
+  const OnDevice on(c->device);
+  if ((rc = cache_enter(c, s, on))) return rc;
   CacheQuery k{};
   k.r = items_of(n, d_seqs, d_starts, rows, q->max_new);
   k.layer = q->layer;
@@ -385,7 +424,8 @@ int rtams_cache_tree(rtams_cache *c, int64_t n, const int32_t *d_seqs, const int
   if (((uintptr_t)d_parents | (uintptr_t)d_tree | (uintptr_t)d_positions) % 4) return fail(RTAMS_EINVAL, "parents, tree or positions are not aligned to their type");
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   std::lock_guard<std::mutex> g(c->mutex);
-  if ((rc = cache_enter(c, s))) return rc;
+  const OnDevice on(c->device);
+  if ((rc = cache_enter(c, s, on))) return rc;
   launch_cache_tree(c->dev, items_of(n, d_seqs, d_starts, rows, max_new), d_parents, d_tree, tree_words, d_positions, s);
   return launched("tree");
 }
@@ -402,7 +442,8 @@ int rtams_cache_walk(rtams_cache *c, int64_t n, const int32_t *d_starts, int64_t
     return fail(RTAMS_EINVAL, "an array is not aligned to its type");
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   std::lock_guard<std::mutex> g(c->mutex);
-  if ((rc = cache_enter(c, s))) return rc;
+  const OnDevice on(c->device);
+  if ((rc = cache_enter(c, s, on))) return rc;
   launch_cache_walk(c->dev, items_of(n, nullptr, d_starts, rows, max_new), d_parents, d_tokens, d_chosen, d_path, d_kept, d_next, s);
   return launched("walk");
 }
@@ -419,7 +460,8 @@ int rtams_cache_keep(rtams_cache *c, int64_t n, const int32_t *d_seqs, const int
   if (((uintptr_t)d_path | (uintptr_t)d_kept) % 4) return fail(RTAMS_EINVAL, "path or kept are not aligned to their type");
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   std::lock_guard<std::mutex> g(c->mutex);
-  if ((rc = cache_enter(c, s))) return rc;
+  const OnDevice on(c->device);
+  if ((rc = cache_enter(c, s, on))) return rc;
   launch_cache_keep(c->dev, items_of(n, d_seqs, d_starts, rows, max_new), d_path, d_kept, s);
   return launched("keep");
 }
@@ -430,7 +472,8 @@ int rtams_cache_fork(rtams_cache *c, int64_t n, const int32_t *d_src, const int3
   if (!d_src || !d_dst) return fail(RTAMS_EINVAL, "sources or destinations are NULL");
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   std::lock_guard<std::mutex> g(c->mutex);
-  if ((rc = cache_enter(c, s))) return rc;
+  const OnDevice on(c->device);
+  if ((rc = cache_enter(c, s, on))) return rc;
   c->forked |= copy == 0;
   launch_cache_fork(c->dev, (int32_t)n, d_src, d_dst, copy != 0, s);
   return launched("fork");
@@ -441,7 +484,8 @@ int rtams_cache_trim(rtams_cache *c, int64_t n, const int32_t *d_seqs, const int
   if (rc || n == 0) return rc;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   std::lock_guard<std::mutex> g(c->mutex);
-  if ((rc = cache_enter(c, s))) return rc;
+  const OnDevice on(c->device);
+  if ((rc = cache_enter(c, s, on))) return rc;
   launch_cache_trim(c->dev, (int32_t)n, d_seqs, d_lengths, s);
   return launched("trim");
 }
@@ -450,7 +494,8 @@ int rtams_cache_compact(rtams_cache *c, void *hip_stream) {
   if (!c) return fail(RTAMS_EINVAL, "cache is NULL");
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   std::lock_guard<std::mutex> g(c->mutex);
-  int rc = cache_enter(c, s);
+  const OnDevice on(c->device);
+  int rc = cache_enter(c, s, on);
   if (rc) return rc;
   launch_cache_compact(c->dev, s);
   return launched("compact");
@@ -459,6 +504,7 @@ int rtams_cache_compact(rtams_cache *c, void *hip_stream) {
 int rtams_cache_free_pages(rtams_cache *c, int64_t *out) {
   if (!c || !out) return fail(RTAMS_EINVAL, "cache or out is NULL");
   std::lock_guard<std::mutex> g(c->mutex);
+  const OnDevice on(c->device);
   if (c->have_stream) HIP_TRY(hipStreamSynchronize(c->stream));
   uint32_t v = 0;
   HIP_TRY(hipMemcpy(&v, &c->dev.ctrl->free, 4, hipMemcpyDeviceToHost));
@@ -477,6 +523,7 @@ int rtams_cache_poll_error(rtams_cache *c) {
 int rtams_cache_clear_error(rtams_cache *c) {
   if (!c) return fail(RTAMS_EINVAL, "cache is NULL");
   std::lock_guard<std::mutex> g(c->mutex);
+  const OnDevice on(c->device);
   if (c->have_stream) HIP_TRY(hipStreamSynchronize(c->stream));
   k_cache_clear_stop<<<1, 1, 0, c->stream>>>(c->dev);
   int rc = launched("clear_error");
