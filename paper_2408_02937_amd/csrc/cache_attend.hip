@@ -29,8 +29,10 @@ constexpr int at_once(int head_dim, int tiles) {
   return tiles == 2 ? (head_dim == 64 ? 3 : 2) : head_dim == 64 ? 5 : head_dim == 96 ? 4 : head_dim == 128 ? 3 : 1;
 }
 
-// Whether parts of rows are joined by a launch of their own: of tiles of 32 rows they are too much for the last workgroup to arrive.  One sequence of 32,000,
-// 32 rows of 128 channels, 64 parts: 66 us joined so, 32 by a launch; 4 of up to 60,063: 73 and 57; 32 of up to 2,000: 30 and 30.
+// Whether parts of rows are joined by a launch of their own and not by the last workgroup to arrive: those of tiles of 32 rows with a sight.  Few long sequences gain,
+// many short ones lose.  8 heads, 32 rows of a head, by the last to arrive (without a sight) and by a launch (the same rows as a tree that is a chain): one
+// sequence of 32,000, 4 of up to 60,063, 16 of up to 6,001, 32 of up to 2,000: of 128 channels 65, 63, 34, 29 and 30, 56, 34, 30 us; of 64 channels 39, 46, 24, 20
+// and 28, 41, 25, 22.  The split does not hang on the sight: without one the join is what it was before there were any.
 constexpr bool joined(int tiles, bool sight) { return sight && tiles > 1; }
 
 struct Span {  // what an item asks for
@@ -100,8 +102,9 @@ struct alignas(16) Shared {
   int last;
 };
 
-// Sequences of so many steps at most are not split where parts would be joined by another launch: five rows behind 200 tokens
-// take 8.7 us, 11.9 in parts.
+// Where no sequence of the cache can be longer than so many steps, none is split if parts would be joined by another launch: the host, which launches it, knows what
+// a page table has room for and not what sequences hold.  Five rows behind 200 tokens, 2 heads of 64 channels, 8 of 128: in a cache of up to 512 tokens a
+// sequence 8.3 and 10.7 us; where there may be more, in two parts with the join's launch, 10.4 and 12.8.
 constexpr int kWhole = 4;
 
 // Which piece is workgroup blockIdx.x's: the items' steps, the size of a piece, and the pieces of the items in front.  One wavefront's work, EACH

@@ -22,7 +22,8 @@
 // barrier each 252 us where 206 are taken here, with the next tile's scores between this one's exponentials 226 (252 rows behind 4 sequences of up to 60,063).
 //
 // With a sight (CacheSight: sinks, trees) a tile's tokens are counted without those between the sinks and the window; what a row sees of 32 tokens are
-// the bits of a word.  Parts of rows are joined by a launch of their own.  8,192 rows under a window of 1,000 with 64 sinks: 204 us for 133 GFLOP.
+// the bits of a word.  Parts of rows are joined by a launch of their own.  8,192 rows under a window of 1,000 with 64 sinks: 201 us for 133 GFLOP; vector
+// instructions have 0.38 of the cycles, matrix instructions 0.28, LDS 0.26 of a unit's.
 #include "../../include/rtams_cache.h"
 
 #include <climits>
@@ -606,7 +607,8 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : 2) void k_cache_prompt_s
 }
 
 // Joins what several workgroups have of a row tile: a wavefront has 32 channels of 32 rows, held as they lie in the parts.  (Up to 32 parts of 128 KiB
-// are too much for the last workgroup to arrive, as in k_cache_prompt: 252 rows behind one sequence of 32,000 took 119 us so, and take 69.)
+// are too much for the last workgroup to arrive, as in k_cache_prompt; a few are not.  252 rows of 128 channels, 8 heads, behind one sequence of 32,000, 4 of up to
+// 60,063, 16 of up to 6,001, 32 of up to 2,000: 117, 206, 94, 72 us so, without a sight, and 68, 200, 103, 81 here, as a tree that is a chain.)
 template <int D, int WAVES>
 __global__ __launch_bounds__(256) void k_cache_join_many(CacheDev d, CacheQuery q, CacheSight g, int tiles, int tile_rows) {
   constexpr int NC = D / 32, kUnit = WAVES * NC;
@@ -669,8 +671,9 @@ size_t cache_prompt_part_rows() { return (size_t)2 * kUnits * kRows; }
 size_t cache_prompt_groups() { return (size_t)4 * kUnits; }
 
 void launch_cache_prompt(const CacheDev &d, const CacheQuery &q, const CacheSight *g, hipStream_t s) {
-  // Workgroups of 4 wavefronts, two to a unit, against 8: 128 rows of 128 channels, 8 heads, 16 sequences of up to 6,001, 4 of up to 60,063, 32 of up to 2,000,
-  // one of 32,000: 67, 148, 56, 67 us and 86, 156, 67, 59; of 64 channels 50, 109, 41, 59 and 67, 121, 52, 49; 252 rows of the first: 120 and 105.
+  // With a sight 65 to 128 rows have workgroups of 4 wavefronts, two to a unit, against 8: 128 rows of 128 channels, 8 heads, 16 sequences of up to 6,001, 4 of up to 60,063, 32 of up to 2,000,
+  // one of 32,000: 67, 148, 56, 67 us and 86, 156, 67, 59; of 64 channels 50, 109, 41, 59 and 67, 121, 52, 49; 252 rows of the first: 120 and 105.  Without a
+  // sight they have 8, and the join of k_cache_prompt: the same 128 rows of 128 channels 72, 149, 56, 105 us, as a tree that is a chain 65, 143, 52, 66.
   const bool few = g && (int64_t)q.share * q.r.max_new <= 128;
   switch (d.head_dim) {
     case 64: return few ? launch<64, 4, 1>(d, q, g, s) : launch<64, 8, 2>(d, q, g, s);
