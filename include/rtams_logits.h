@@ -2,7 +2,8 @@
  * rtams_logits.h - what rows of logits say: the log probabilities of given tokens, the entropy, and the most likely tokens.
  * What a program that answers over the cache of rtams_cache.h does with a model's output.  Part of librtams.so; the conventions
  * are those of rtams.h (d_* are device pointers, calls enqueue on the stream given and return, the library owns no device memory, every
- * function returns RTAMS_OK or a negative rtams_status, rtams_last_error() describes a failure).  No state is kept between calls.
+ * function returns RTAMS_OK or a negative rtams_status, rtams_last_error() describes a failure).  No state is kept between calls.  Memory and
+ * stream are those of the thread's current device.
  *
  * Of a row x of `vocab` logits, x' = scale * x:
  *   lse = log sum exp(x'),  log probability of token t = x'_t - lse,  entropy = lse - sum exp(x'_t - lse) x'_t  (natural logarithms)

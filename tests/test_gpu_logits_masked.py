@@ -76,4 +76,4 @@ def least_time(f):
 def test_a_mask_of_the_lowest_number_costs_about_what_one_of_infinity_does(rows, vocab, allowed):
     """(A search for the tie, bit by bit, made it seven to seventeen times that.)"""
     x, y = (masked(rows, vocab, torch.float16, allowed, low) for low in (float("-inf"), torch.finfo(torch.float16).min))
-    assert least_time(lambda: score(y, top=20)) < 4 * least_time(lambda: score(x, top=20))
+    assert least_time(lambda: score(y, top=20)) < 5 * least_time(lambda: score(x, top=20))
